@@ -12,8 +12,8 @@ A case is one of seven kinds:
   drop      Y = D(X), dropout by itself (forward and backward are the same call)
 D keeps the element in row i, column j where the 16-bit number of (seed, offset, i, j) is at least t = round(65536 p), and
 multiplies it by 65536 / (65536 - t); the numbers are Philox 4x32-10's (Salmon, Moraes, Dror and Shaw, "Parallel random
-numbers: as easy as 1, 2, 3", 2011) for the counter (4 (j div 32) + (j div 4) mod 4, i, offset) and the key `seed`: number
-4 ((j div 16) mod 2) + j mod 4 of the eight in its four words, low half first.
+numbers: as easy as 1, 2, 3", 2011) for the counter (j div 8, i, offset) and the key `seed`: number j mod 8 of the eight in
+its four words, low half first.
 """
 import math
 
@@ -190,18 +190,17 @@ def _keep(rows, cols, drop, seed, offset):
     """What dropout multiplies by: 0 or 65536 / (65536 - t)."""
     t = int(drop * 65536 + 0.5)
     low = 0xFFFFFFFF
-    blocks = -(-cols // 32)
-    c0 = torch.arange(4 * blocks, device=DEVICE)[None, :].expand(rows, -1)
-    c1 = torch.arange(rows, device=DEVICE)[:, None].expand(-1, 4 * blocks)
+    calls = -(-cols // 8)
+    c0 = torch.arange(calls, device=DEVICE)[None, :].expand(rows, -1)
+    c1 = torch.arange(rows, device=DEVICE)[:, None].expand(-1, calls)
     c2, c3 = torch.full_like(c0, offset & low), torch.full_like(c0, offset >> 32)
     k0, k1 = seed & low, seed >> 32
     for _ in range(10):
         p, q = c0 * 0xD2511F53, c2 * 0xCD9E8D57
         c0, c1, c2, c3 = (q >> 32 & low) ^ c1 ^ k0, q & low, (p >> 32 & low) ^ c3 ^ k1, p & low
         k0, k1 = k0 + 0x9E3779B9 & low, k1 + 0xBB67AE85 & low
-    w = torch.stack((c0, c1, c2, c3), -1).view(rows, blocks, 4, 4)
-    u = torch.stack((w & 0xFFFF, w >> 16), -1).view(rows, blocks, 4, 2, 4)   # [row][block][quarter][j div 16][j mod 4]
-    u = u.transpose(2, 3).reshape(rows, 32 * blocks)[:, :cols]
+    w = torch.stack((c0, c1, c2, c3), -1)
+    u = torch.stack((w & 0xFFFF, w >> 16), -1).view(rows, 8 * calls)[:, :cols]
     return torch.where(u >= t, 65536 / (65536 - t), 0.0)
 
 
@@ -350,19 +349,20 @@ def work(case):
 # ---- the definitions in 64 bits, by differentiation
 
 def _numbers(rows, cols, seed, offset):
-    """The 16-bit number of every element, in numpy: words by column group, then spread over the columns."""
+    """The 16-bit number of every element, in numpy: the calls' words, then each column's half of one."""
     m32, s32 = np.uint64(0xFFFFFFFF), np.uint64(32)
-    groups = 4 * (-(-cols // 32))
-    x = [np.tile(np.arange(groups, dtype=np.uint64), rows), np.repeat(np.arange(rows, dtype=np.uint64), groups),
-         np.full(rows * groups, offset & 0xFFFFFFFF, np.uint64), np.full(rows * groups, offset >> 32, np.uint64)]
+    calls = -(-cols // 8)
+    x = [np.tile(np.arange(calls, dtype=np.uint64), rows), np.repeat(np.arange(rows, dtype=np.uint64), calls),
+         np.full(rows * calls, offset & 0xFFFFFFFF, np.uint64), np.full(rows * calls, offset >> 32, np.uint64)]
     key = [seed & 0xFFFFFFFF, seed >> 32]
     for r in range(10):
         a, b = np.uint64(0xD2511F53) * x[0], np.uint64(0xCD9E8D57) * x[2]
         x = [(b >> s32) ^ x[1] ^ np.uint64(key[0]), b & m32, (a >> s32) ^ x[3] ^ np.uint64(key[1]), a & m32]
         key = [(key[0] + 0x9E3779B9) % 2 ** 32, (key[1] + 0xBB67AE85) % 2 ** 32]
-    halves = np.stack([v for w in x for v in (w & np.uint64(0xFFFF), w >> np.uint64(16))]).reshape(8, rows, groups)
-    j = np.arange(cols)
-    return halves[4 * (j // 16 % 2) + j % 4, :, j // 32 * 4 + j // 4 % 4].T
+    found = np.empty((rows, calls, 8), np.int64)
+    for n in range(8):
+        found[:, :, n] = (x[n // 2] >> np.uint64(16 * (n % 2)) & np.uint64(0xFFFF)).reshape(rows, calls)
+    return found.reshape(rows, 8 * calls)[:, :cols]
 
 
 def exact(case, seed):
