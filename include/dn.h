@@ -16,7 +16,8 @@
  * "Performance Analysis" and "Conclusions").
  *
  * Conventions
- *   - All arithmetic and all tensors are fp32, row-major, contiguous.
+ *   - All arithmetic and all tensors are fp32, row-major, contiguous (dn_linear_*, dn_ffn_*, dn_norm_* and dn_dropout
+ *     also take f16 and bf16 tensors).
  *   - Layers l = 1..L, widths n_0 (input) .. n_L (output).  W_l is
  *     [n_l][n_{l-1}], b_l is [n_l].  A batch of B samples is [B][n].
  *   - Labels are int32 class ids in [0, n_L); targets are their one-hot rows
@@ -71,8 +72,16 @@ typedef enum {
     DN_ACT_SIGMOID = 1,
     DN_ACT_TANH = 2,
     DN_ACT_RELU = 3,
-    DN_ACT_SOFTMAX = 4 /* last layer only, and only with DN_LOSS_CROSS_ENTROPY */
+    DN_ACT_SOFTMAX = 4, /* last layer only, and only with DN_LOSS_CROSS_ENTROPY */
+    DN_ACT_SILU = 5,    /* z / (1 + exp(-z)); dn_linear_* and dn_ffn_* only */
+    DN_ACT_GELU = 6     /* z times the normal distribution function of z; dn_linear_* and dn_ffn_* only */
 } dn_act;
+
+/* Element types of the residual feed-forward block's operators (everything else is fp32). */
+typedef enum { DN_F32 = 0, DN_F16 = 1, DN_BF16 = 2 } dn_type;
+
+/* Norms of a row v of d elements: v / sqrt(mean(v^2) + eps) w, or (v - mean(v)) / sqrt(var(v) + eps) w + shift. */
+typedef enum { DN_NORM_NONE = 0, DN_NORM_RMS = 1, DN_NORM_LAYER = 2 } dn_norm_kind;
 
 typedef enum {
     DN_LOSS_MSE = 0,          /* per sample 1/2 sum_k (a_k - y_k)^2 */
@@ -382,6 +391,122 @@ dn_status dn_cnn_get_filter_grads(dn_cnn *net, int32_t block, float *dW_host, fl
 dn_status dn_cnn_forward(dn_cnn *net, const float *X_dev, int32_t batch, float *out_dev);
 dn_status dn_cnn_train_epoch(dn_cnn *net, const float *X_dev, const int32_t *labels_dev, int64_t n_samples,
                              int32_t batch, float lr, float momentum, float *mean_loss_host);
+
+/* ---- the residual feed-forward block ---------------------------------------------
+ * What a deep stack of fully connected layers is trained and served with today, as stateless calls like those above: a
+ * dense layer with everything in its epilogue (dn_linear_*), the gated feed-forward block (dn_ffn_*), the norms and the
+ * residual stream between two blocks (dn_norm_*), and dropout (dn_dropout; the first two hold it too).  dn_input_gradient
+ * gives the derivative that a classifier on top of the blocks hands down to them, dn_sgd_step updates their fp32 parameters.
+ *
+ * Types: every tensor of a call is of the descriptor's `type` (DN_F32, DN_F16, DN_BF16); parameter gradients are of it
+ * too or, with grad_type DN_F32, fp32.  Sums and statistics are held in fp32 and results rounded once; what a call keeps between
+ * two products (the gated hidden layer, its deltas) is rounded to `type` as the caller's own tensors are.
+ *
+ * Tensors are row-major device memory of the caller's, rows of X, W, R, Y and dY any distance apart (ld*, in elements; 0:
+ * contiguous), everything else contiguous.  Any alignment of an element will do; rows at multiples of 16 bytes
+ * whose lengths are multiples of 16 bytes too are faster.  A result may be the residual itself (Y = R), no other two
+ * tensors of a call may overlap.
+ * Workspaces: device memory, 256-byte aligned, as many bytes as the query says (0: none, NULL will do); the query returns
+ * (size_t)-1 for a descriptor that the call would refuse.  Nothing in them outlives a call.
+ * Results are the same bits for the same call whatever else runs (no atomics).
+ *
+ * Dropout: the element in row i, column j is kept if its number is at least t, the nearest whole number to 65536 p, and
+ * then multiplied by 65536 / (65536 - t); it becomes 0 otherwise.  The numbers are 16-bit ones from the counter-based
+ * generator Philox 4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) with the key
+ * `seed` and the counter (j div 8, i, offset): number j mod 8 of the eight in its four words, low halves first.  No mask is
+ * stored; the backward calls compute it again from the same seed and offset.  A step that needs several masks takes another
+ * offset for each.
+ *
+ * Errors: INVALID_ARG (NULL, an enum out of range, drop not in [0, 1), a scale or eps that is not finite, eps < 0, a
+ * workspace that is NULL or misaligned where one is needed, a pointer that is no multiple of its element), SHAPE (rows or
+ * widths < 1, rows of more than 8 MB, ld smaller than the row, d above 16384 in dn_norm_*, a workspace too small),
+ * UNSUPPORTED (softmax as the activation), DEVICE.
+ */
+
+/*
+ * Dense layer:  Z = X W^T + bias,  Y = R + D(f(Z)).
+ *   X [rows][n_in], W [n_out][n_in], bias [n_out] or NULL, R [rows][n_out] or NULL (no residual)
+ *   Y [rows][n_out]; Z [rows][n_out] receives the net inputs for the backward pass, or NULL
+ * Backward:  delta = D(dY) f'(Z),  dX = delta W,  dW = grad_scale delta^T X,  dbias = grad_scale (column sums of delta);
+ * the residual's derivative is dY itself.  grad_scale = 1 / rows gives batch means, as the dense nets use them.
+ *   Z may be NULL where f is DN_ACT_LINEAR; dX, dW, dbias: each may be NULL (not computed; dbias needs dW)
+ */
+typedef struct {
+    int32_t type, grad_type;    /* dn_type */
+    int32_t act;                /* dn_act other than softmax */
+    int32_t rows, n_in, n_out;
+    int64_t ldx, ldw, ldr, ldy; /* ldy: of Y and of dY */
+    float drop, grad_scale;
+    uint64_t seed, offset;
+} dn_linear_desc;
+size_t dn_linear_forward_workspace_bytes(const dn_linear_desc *d);
+size_t dn_linear_backward_workspace_bytes(const dn_linear_desc *d);
+dn_status dn_linear_forward(const dn_linear_desc *d, const void *X_dev, const void *W_dev, const void *bias_dev,
+                            const void *R_dev, void *Y_dev, void *Z_dev, void *workspace_dev, size_t workspace_bytes,
+                            void *hip_stream);
+dn_status dn_linear_backward(const dn_linear_desc *d, const void *X_dev, const void *W_dev, const void *Z_dev,
+                             const void *dY_dev, void *dX_dev, void *dW_dev, void *dbias_dev, void *workspace_dev,
+                             size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gated feed-forward block of width d and hidden width f:
+ *   G = X Wg^T + bg,  U = X Wu^T + bu,  H = act(G) * U,  Y = R + D(H Wd^T + bd)
+ *   X [rows][d], Wg and Wu [f][d], Wd [d][f], bg and bu [f], bd [d] (each may be NULL), R [rows][d] or NULL
+ *   Y [rows][d]; GU [rows][2 f] receives G and, beside it, U for the backward pass, or NULL
+ * Backward, with dZ = D(dY):  dH = dZ Wd,  dG = dH * U * act'(G),  dU = dH * act(G),  dX = dG Wg + dU Wu, and grad_scale
+ * times  dWg = dG^T X,  dWu = dU^T X,  dWd = dZ^T H,  dbg, dbu, dbd (column sums of dG, dU, dZ; each may be NULL).
+ *   H is computed again from GU.  dX may be NULL (not computed).
+ */
+typedef struct {
+    int32_t type, grad_type; /* dn_type */
+    int32_t act;             /* dn_act other than softmax */
+    int32_t rows, d, f;
+    int64_t ldx, ldr, ldy;   /* ldy: of Y and of dY */
+    float drop, grad_scale;
+    uint64_t seed, offset;
+} dn_ffn_desc;
+size_t dn_ffn_forward_workspace_bytes(const dn_ffn_desc *d);
+size_t dn_ffn_backward_workspace_bytes(const dn_ffn_desc *d);
+dn_status dn_ffn_forward(const dn_ffn_desc *d, const void *X_dev, const void *Wg_dev, const void *bg_dev, const void *Wu_dev,
+                         const void *bu_dev, const void *Wd_dev, const void *bd_dev, const void *R_dev, void *Y_dev,
+                         void *GU_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
+                          const void *GU_dev, const void *dY_dev, void *dX_dev, void *dWg_dev, void *dbg_dev, void *dWu_dev,
+                          void *dbu_dev, void *dWd_dev, void *dbd_dev, void *workspace_dev, size_t workspace_bytes,
+                          void *hip_stream);
+
+/*
+ * Between two blocks:  c = post(b),  x' = x + scale * gate * c,  n = pre(x').
+ *   x, b [rows][d]; gate [ceil(rows / rows_per_gate)][d]: row i takes row i div rows_per_gate, NULL: ones
+ *   post_w, post_b, pre_w, pre_b [d]: weights and shifts of the norms, NULL: ones and zeros (a shift: layer norm only)
+ *   x_out, n_out [rows][d]; x_out may be x or b, n_out may be b
+ * b NULL: no block; x' = x and x_out is not written.  pre DN_NORM_NONE: n_out is not written (a block is needed then).
+ * n is formed from x' before x' is rounded to `type`.
+ * Backward, from x' as the forward call stored it, dx_out = the derivative with respect to x' from elsewhere (NULL: zero) and dn:
+ *   dx = dx_out + pre'(dn),  dc = scale * gate * dx,  db = post'(dc),  dgate = scale dx * c summed over the rows of a gate,
+ *   dpost_w, dpost_b, dpre_w, dpre_b (sums over all rows; each may be NULL, as may dgate).  dx may be dx_out or dn, db may
+ *   be b.  The statistics are formed again from x' and b.
+ */
+typedef struct {
+    int32_t type, grad_type; /* dn_type */
+    int32_t rows, d;
+    int32_t post, pre;       /* dn_norm_kind */
+    int32_t rows_per_gate;   /* >= 1 */
+    float scale, eps;
+} dn_norm_desc;
+size_t dn_norm_backward_workspace_bytes(const dn_norm_desc *d);
+dn_status dn_norm_forward(const dn_norm_desc *d, const void *x_dev, const void *b_dev, const void *gate_dev,
+                          const void *post_w_dev, const void *post_b_dev, const void *pre_w_dev, const void *pre_b_dev,
+                          void *x_out_dev, void *n_out_dev, void *hip_stream);
+dn_status dn_norm_backward(const dn_norm_desc *d, const void *x_dev, const void *b_dev, const void *gate_dev,
+                           const void *post_w_dev, const void *post_b_dev, const void *pre_w_dev, const void *dx_out_dev,
+                           const void *dn_dev, void *dx_dev, void *db_dev, void *dgate_dev, void *dpost_w_dev,
+                           void *dpost_b_dev, void *dpre_w_dev, void *dpre_b_dev, void *workspace_dev,
+                           size_t workspace_bytes, void *hip_stream);
+
+/* Dropout by itself, forward and backward alike: Y = D(X), [rows][cols], rows ldx and ldy elements apart (0: cols); Y may be X. */
+dn_status dn_dropout(int32_t type, const void *X_dev, void *Y_dev, int32_t rows, int32_t cols, int64_t ldx, int64_t ldy,
+                     float drop, uint64_t seed, uint64_t offset, void *hip_stream);
 
 /*
  * Measurement hooks (the paper times its two offloaded methods with wall-clock

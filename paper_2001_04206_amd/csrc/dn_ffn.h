@@ -1,0 +1,258 @@
+// Operators of the residual feed-forward block: what their kernels share.  Internal; the entry points are in include/dn.h.
+#pragma once
+
+#include "dn_internal.h"
+
+namespace dn {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+template <class T> struct Elem;
+template <> struct Elem<float> { static constexpr int TYPE = DN_F32; };
+template <> struct Elem<f16> { static constexpr int TYPE = DN_F16; };
+template <> struct Elem<bf16> { static constexpr int TYPE = DN_BF16; };
+
+// eight elements as they lie in memory, at any alignment of theirs
+template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
+
+template <class T>
+__device__ __forceinline__ void load8(float (&v)[8], const void *p, int64_t at, int left)
+{
+    const T *q = static_cast<const T *>(p) + at;
+    if (left >= 8) {
+        const auto x = *reinterpret_cast<const typename Eight<T>::type *>(q);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < left ? (float)q[j] : 0.f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8], int left)
+{
+    T *q = static_cast<T *>(p) + at;
+    if (left >= 8) {
+        typename Eight<T>::type x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
+        *reinterpret_cast<typename Eight<T>::type *>(q) = x;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left) q[j] = (T)v[j];
+    }
+}
+
+// ---- dropout --------------------------------------------------------------------------------------------------
+// Philox 4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): ten rounds of two
+// 32 x 32 -> 64 bit products over a 128-bit counter.  One call gives the eight 16-bit numbers of eight neighbouring columns
+// of a row, which is what a thread of every kernel here has in hand: twenty products for eight numbers.  (With 32-bit
+// numbers it would be forty, and the numbers a third of a wide layer's epilogue.)
+struct Dropout {
+    uint32_t t = 0;          // numbers below t are dropped; 0: none are
+    float scale = 1.f;       // 65536 / (65536 - t)
+    uint32_t k0 = 0, k1 = 0; // seed
+    uint32_t o0 = 0, o1 = 0; // offset
+};
+
+__device__ __forceinline__ v4u philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1)
+{
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p = (uint64_t)c0 * 0xD2511F53u, q = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)q;
+        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)p;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return v4u{c0, c1, c2, c3};
+}
+
+// v[j] of row m, columns n .. n + 7 (n a multiple of 8) as dropout leaves them
+__device__ __forceinline__ void drop8(const Dropout &d, int m, int n, float (&v)[8])
+{
+    const v4u w = philox((uint32_t)n >> 3, (uint32_t)m, d.o0, d.o1, d.k0, d.k1);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t u = j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xffff;
+        v[j] = u >= d.t ? v[j] * d.scale : 0.f;
+    }
+}
+
+// ---- activations ------------------------------------------------------------------------------------------------
+// fp32 results come from the library's functions.  Results that are rounded to 16 bits come from the hardware's exp2 and
+// reciprocal (1 ulp each), and their error function from Abramowitz and Stegun 7.1.26 (|error| <= 1.5e-7): a few
+// instructions instead of some sixty, which would be a quarter of a wide layer's time.
+template <bool FAST> struct Math;
+template <> struct Math<false> {
+    static __device__ __forceinline__ float exp(float x) { return expf(x); }
+    static __device__ __forceinline__ float inv(float x) { return 1.f / x; }
+    static __device__ __forceinline__ float tanh(float x) { return tanhf(x); }
+    // the normal distribution's function and density
+    static __device__ __forceinline__ void normal(float x, float &cdf, float &pdf)
+    {
+        cdf = 0.5f * (1.f + erff(x * 0.70710678f));
+        pdf = 0.39894228f * expf(-0.5f * x * x);
+    }
+};
+template <> struct Math<true> {
+    static __device__ __forceinline__ float exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+    static __device__ __forceinline__ float inv(float x) { return __builtin_amdgcn_rcpf(x); }
+    static __device__ __forceinline__ float tanh(float x)
+    {
+        // 1 - 2 / (e^2x + 1) loses the leading bits of small results: their series instead
+        const float big = 1.f - 2.f * inv(exp(2.f * x) + 1.f), s = x * x;
+        return s < 0.01f ? x * (1.f + s * (-0.33333333f + s * 0.13333333f)) : big;
+    }
+    static __device__ __forceinline__ void normal(float x, float &cdf, float &pdf)
+    {
+        const float y = fabsf(x) * 0.70710678f, t = inv(1.f + 0.3275911f * y), e = exp(-y * y);
+        const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+        const float half = 0.5f * poly * e;   // (1 - erf y) / 2
+        cdf = x < 0.f ? half : 1.f - half;
+        pdf = 0.39894228f * e;
+    }
+};
+
+// f(z), and f'(z) with it
+template <bool FAST>
+__device__ __forceinline__ void act_both(int act, float z, float &f, float &df)
+{
+    typedef Math<FAST> K;
+    switch (act) {
+    case DN_ACT_SIGMOID:
+        f = K::inv(1.f + K::exp(-z));
+        df = f * (1.f - f);
+        break;
+    case DN_ACT_TANH:
+        f = K::tanh(z);
+        df = 1.f - f * f;
+        break;
+    case DN_ACT_RELU:   // a comparison that a NaN fails would hide it
+        f = z < 0.f ? 0.f : z;
+        df = z > 0.f ? 1.f : 0.f;
+        break;
+    case DN_ACT_SILU: {
+        const float s = K::inv(1.f + K::exp(-z));
+        const bool far = fabsf(z) > 1e4f;   // where s is 0 or 1: inf * 0
+        f = far && z < 0.f ? 0.f : z * s;
+        df = far ? s : s * (1.f + z * (1.f - s));
+        break;
+    }
+    case DN_ACT_GELU: {
+        float c, p;
+        K::normal(z, c, p);
+        f = z < -30.f ? 0.f : z * c;
+        df = fabsf(z) > 30.f ? c : c + z * p;   // inf * 0
+        break;
+    }
+    default:
+        f = z;
+        df = 1.f;
+    }
+}
+template <bool FAST>
+__device__ __forceinline__ float act_value(int act, float z)
+{
+    float f, df;
+    act_both<FAST>(act, z, f, df);
+    return f;
+}
+
+// ---- matrix products ---------------------------------------------------------------------------------------------
+// C[m][n] = sum_k A(m, k) B(n, k).  An operand is stored with k contiguous ("KC": [m][k] or [n][k]) or with its own index
+// contiguous ("MC": [k][m] or [k][n]).
+enum Product : int {
+    P_FWD = 0,    // A = X [rows][n_in] KC, B = W [n_out][n_in] KC
+    P_DELTA = 1,  // A = delta [rows][n_out] KC, B = W [n_out][n_in] MC
+    P_GRAD = 2    // A = delta [rows][n_out] MC, B = X [rows][n_in] MC
+};
+enum Epilogue : int {
+    E_LINEAR = 0,  // P_FWD: + bias, activation, dropout, residual; the net input too
+    E_GATED = 1,   // P_FWD of two matrices B: f(g) u; g and u too
+    E_DGATED = 2,  // P_DELTA: d(f(g) u) from its derivative: dG, dU, and f(g) u again
+    E_STORE = 3    // alpha times the sum, as T or as fp32
+};
+
+struct Finish {
+    void *y = nullptr;          // result [M][ldy]; E_DGATED: dG [M][ldy] with dU `half_y` columns further on
+    int64_t ldy = 0;
+    void *y2 = nullptr;         // E_LINEAR: net inputs; E_GATED: G and U; E_DGATED: f(g) u; E_STORE: rows from m_split on
+    int64_t ldy2 = 0;
+    const void *r = nullptr;    // E_LINEAR: residual; E_DGATED: G and U
+    int64_t ldr = 0;
+    const void *bias = nullptr, *bias2 = nullptr;
+    void *sums = nullptr, *sums2 = nullptr;   // P_GRAD: alpha times A's sums over k, [M] (from m_split on: sums2)
+    int64_t half = 0, half_y = 0;   // columns between G and U; between dG and dU
+    int32_t m_split = 0x7fffffff;
+    int32_t m_valid = 0x7fffffff;   // rows of either side of m_split that exist
+    int32_t act = 0;
+    int32_t f32_out = 0;        // E_STORE: results are fp32 whatever T is
+    float alpha = 1.f;
+    Dropout drop;
+};
+
+struct ProductArgs {
+    const void *a[2], *b[2];    // operands; the second ones: of the second segment of k, or (E_GATED) of the second matrix
+    int64_t lda, ldb;           // bytes between stored rows
+    int32_t M, N, K;            // K: of one segment
+    int32_t segments;           // 1 or 2
+    float *ws;                  // split > 1: partial sums [split][planes][M][N], then [split][M] of E_STORE's sums
+    int32_t split, steps;       // k steps of each part
+    int32_t tiles_m, tiles_n;
+    Finish f;
+};
+
+// How a product is run.  `ws_bytes`: workspace that it needs.
+enum ProductKernel : int { K_FEW, K_SMALL_ANY, K_SMALL, K_LARGE };
+struct ProductPlan {
+    ProductKernel kernel = K_SMALL_ANY;
+    bool direct = false;
+    int split = 1, steps = 0;
+    size_t ws_bytes = 0;
+};
+// `direct`: operand pieces of 16 bytes lie at multiples of 16 bytes and inside or outside whole
+ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, int segments, bool direct, bool sums);
+hipError_t launch_product_f32(Product p, Epilogue e, const ProductPlan &plan, ProductArgs a, hipStream_t s);
+hipError_t launch_product_f16(Product p, Epilogue e, const ProductPlan &plan, ProductArgs a, hipStream_t s);
+hipError_t launch_product_bf16(Product p, Epilogue e, const ProductPlan &plan, ProductArgs a, hipStream_t s);
+
+// ---- elementwise ------------------------------------------------------------------------------------------------
+// Y = D(X), or (act >= 0) Y = kept(X) f'(Z) without D's scale, which the products that follow multiply their sums by
+struct MaskArgs {
+    const void *x, *z;
+    void *y;
+    int64_t ldx, ldz, ldy;
+    int32_t rows, cols, act;
+    Dropout drop;
+};
+hipError_t launch_mask(int type, const MaskArgs &a, hipStream_t s);
+
+// ---- norms ------------------------------------------------------------------------------------------------------
+struct NormArgs {
+    // forward: x' = x + scale gate post(b), n = pre(x'); backward: x is x'
+    const void *x, *b, *gate, *post_w, *post_b, *pre_w, *pre_b;
+    void *x_out, *n_out;
+    const void *dx_out, *dn;
+    void *dx, *db, *dgate, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
+    float *ws;
+    int32_t rows, d, group;   // rows that share a gate
+    int32_t post, pre;        // dn_norm_kind
+    int32_t f32_out;          // parameter gradients are fp32
+    float scale, eps;
+    // backward: rows of a part, parts of a group (1 where a part is whole groups), and how many parts there are
+    int32_t part_rows, group_parts, parts;
+};
+hipError_t launch_norm_forward(int type, const NormArgs &a, hipStream_t s);
+hipError_t launch_norm_backward(int type, const NormArgs &a, hipStream_t s);
+constexpr int kNormWidth = 16384;   // largest d
+// how the backward pass is divided, and its workspace
+size_t norm_backward_plan(NormArgs &a);
+
+}  // namespace dn

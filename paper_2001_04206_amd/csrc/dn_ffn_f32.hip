@@ -1,0 +1,11 @@
+// Matrix products of the residual feed-forward block on f32 operands.
+#include "dn_ffn_launch.h"
+
+namespace dn {
+
+hipError_t launch_product_f32(Product p, Epilogue e, const ProductPlan &plan, ProductArgs a, hipStream_t s)
+{
+    return launch_product<float>(p, e, plan, a, s);
+}
+
+}  // namespace dn

@@ -1,0 +1,77 @@
+// The launches of the block's matrix products for one type of element; included by the source of each type.
+#pragma once
+
+#include "dn_ffn_few.h"
+
+namespace dn {
+namespace {
+
+template <class T, int P, int EPI, class S, bool DIRECT>
+hipError_t tiles(ProductArgs &a, bool sums, hipStream_t s)
+{
+    a.tiles_m = (a.M + S::BM - 1) / S::BM;
+    const int cols = EPI == E_GATED ? S::BN / 2 : S::BN;
+    a.tiles_n = (a.N + cols - 1) / cols;
+    const dim3 grid((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split);
+    if constexpr (P == P_GRAD) {
+        if (sums) {
+            launch_kernel(product_kernel<T, P, EPI, S, DIRECT, true>, grid, dim3(S::NW * 64), 0, s, a);
+            return hipGetLastError();
+        }
+    }
+    launch_kernel(product_kernel<T, P, EPI, S, DIRECT, false>, grid, dim3(S::NW * 64), 0, s, a);
+    return hipGetLastError();
+}
+
+template <class T, int EPI, bool DIRECT>
+hipError_t few(const ProductArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.N + 15) / 16)), block(kFewWaves * 64);
+    if (a.M <= 16) launch_kernel(few_kernel<T, EPI, 1, DIRECT>, grid, block, 0, s, a);
+    else if (a.M <= 32) launch_kernel(few_kernel<T, EPI, 2, DIRECT>, grid, block, 0, s, a);
+    else launch_kernel(few_kernel<T, EPI, 4, DIRECT>, grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+template <class T, int P, int EPI>
+hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
+{
+    const bool sums = a.f.sums != nullptr;
+    a.split = plan.split;
+    a.steps = plan.steps;
+    hipError_t e = hipErrorInvalidValue;
+    switch (plan.kernel) {
+    case K_FEW:
+        if constexpr (P == P_FWD) return plan.direct ? few<T, EPI, true>(a, s) : few<T, EPI, false>(a, s);
+        return hipErrorInvalidValue;
+    case K_SMALL_ANY: e = tiles<T, P, EPI, Small, false>(a, sums, s); break;
+    case K_SMALL: e = tiles<T, P, EPI, Small, true>(a, sums, s); break;
+    case K_LARGE: e = tiles<T, P, EPI, Large, true>(a, sums, s); break;
+    }
+    if (e != hipSuccess || a.split == 1) return e;
+    const int64_t work = (int64_t)a.M * ((a.N + 7) / 8);
+    const int64_t threads = sums && work < a.M ? a.M : work;
+    launch_kernel(join_kernel<T, EPI>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, (int)sums);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+template <class T>
+hipError_t launch_product(Product p, Epilogue e, const ProductPlan &plan, ProductArgs &a, hipStream_t s)
+{
+    switch (p) {
+    case P_FWD:
+        if (e == E_LINEAR) return run<T, P_FWD, E_LINEAR>(plan, a, s);
+        if (e == E_GATED) return run<T, P_FWD, E_GATED>(plan, a, s);
+        return hipErrorInvalidValue;
+    case P_DELTA:
+        if (e == E_DGATED) return run<T, P_DELTA, E_DGATED>(plan, a, s);
+        if (e == E_STORE) return run<T, P_DELTA, E_STORE>(plan, a, s);
+        return hipErrorInvalidValue;
+    default:
+        return e == E_STORE ? run<T, P_GRAD, E_STORE>(plan, a, s) : hipErrorInvalidValue;
+    }
+}
+
+}  // namespace dn

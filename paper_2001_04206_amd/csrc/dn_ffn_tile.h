@@ -1,0 +1,461 @@
+// Matrix products in tiles on the matrix instructions, 32-bit, f16 and bf16 operands, with the block's epilogues.
+//
+// The geometry is one in bytes: a stage holds 128 bytes of k (64 16-bit numbers, 32 fp32 ones) of every row of both tiles,
+// a lane's fragment is 16 bytes (eight k of v_mfma_f32_16x16x32, or four of v_mfma_f32_16x16x4_f32 in four instructions).
+// The matrix instruction's first operand is the N side, so that a lane holds four consecutive columns of one row of C:
+// lane = 16 h + i: D register r is column 4 h + r, row i.
+#pragma once
+
+#include "dn_ffn.h"
+
+namespace dn {
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+__device__ __forceinline__ v4f mfma(const v4u &a, const v4u &b, v4f c, bf16)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mfma(const v4u &a, const v4u &b, v4f c, f16)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mfma(const v4u &a, const v4u &b, v4f c, float)
+{
+    const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+    return c;
+}
+template <class T> __device__ __forceinline__ v4u ones()
+{
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(v4u, v4f{1.f, 1.f, 1.f, 1.f});
+    else {
+        const uint32_t one = (uint32_t)__builtin_bit_cast(uint16_t, (T)1.f);
+        return v4u{one * 0x10001u, one * 0x10001u, one * 0x10001u, one * 0x10001u};
+    }
+}
+
+// ---- epilogues -------------------------------------------------------------------------------------------------------
+
+// The epilogue of row m, columns n .. n + 7 of N (n a multiple of 8, n < N): `v` the sums, E_GATED: `w` those of the second
+// matrix.
+template <class T, int EPI>
+__device__ __forceinline__ void finish8(const Finish &e, int m, int n, int N, float (&v)[8], float (&w)[8])
+{
+    constexpr bool FAST = sizeof(T) == 2;
+    const int left = N - n;
+    if constexpr (EPI == E_LINEAR) {
+        if (e.bias) {
+            float b[8];
+            load8<T>(b, e.bias, n, left);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += b[j];
+        }
+        if (e.y2) store8<T>(e.y2, m * e.ldy2 + n, v, left);
+        if (e.act != DN_ACT_LINEAR)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = act_value<FAST>(e.act, v[j]);
+        if (e.drop.t) drop8(e.drop, m, n, v);
+        if (e.r) {
+            float r[8];
+            load8<T>(r, e.r, m * e.ldr + n, left);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += r[j];
+        }
+        store8<T>(e.y, m * e.ldy + n, v, left);
+    } else if constexpr (EPI == E_GATED) {
+        if (e.bias) {
+            float b[8];
+            load8<T>(b, e.bias, n, left);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += b[j];
+        }
+        if (e.bias2) {
+            float b[8];
+            load8<T>(b, e.bias2, n, left);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] += b[j];
+        }
+        if (e.y2) {
+            store8<T>(e.y2, m * e.ldy2 + n, v, left);
+            store8<T>(e.y2, m * e.ldy2 + n + e.half, w, left);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = act_value<FAST>(e.act, v[j]) * w[j];
+        store8<T>(e.y, m * e.ldy + n, v, left);
+    } else if constexpr (EPI == E_DGATED) {
+        float g[8], u[8];
+        load8<T>(g, e.r, m * e.ldr + n, left);
+        load8<T>(u, e.r, m * e.ldr + n + e.half, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float f, df;
+            act_both<FAST>(e.act, g[j], f, df);
+            v[j] *= e.alpha;
+            w[j] = v[j] * f;
+            v[j] *= u[j] * df;
+            u[j] *= f;
+        }
+        store8<T>(e.y, m * e.ldy + n, v, left);
+        store8<T>(e.y, m * e.ldy + n + e.half_y, w, left);
+        store8<T>(e.y2, m * e.ldy2 + n, u, left);
+    } else {
+        const int row = m < e.m_split ? m : m - e.m_split;
+        if (row >= e.m_valid) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= e.alpha;
+        void *y = m < e.m_split ? e.y : e.y2;
+        const int64_t at = row * (m < e.m_split ? e.ldy : e.ldy2) + n;
+        if (e.f32_out) store8<float>(y, at, v, left);
+        else store8<T>(y, at, v, left);
+    }
+}
+template <class T>
+__device__ __forceinline__ void finish_sum(const Finish &e, int m, float v)
+{
+    void *p = m < e.m_split ? e.sums : e.sums2;
+    const int at = m < e.m_split ? m : m - e.m_split;
+    if (at >= e.m_valid) return;
+    if (e.f32_out) static_cast<float *>(p)[at] = v * e.alpha;
+    else static_cast<T *>(p)[at] = (T)(v * e.alpha);
+}
+
+// ---- operands ----------------------------------------------------------------------------------------------------------
+
+// One operand's stage of R rows in LDS, R * 128 bytes, filled by NW waves in pieces of 1024 bytes (wave w: pieces w, w + NW, ..).
+//   KC: row r at 128 r, its 16-byte chunk c at c ^ ((r >> 1) & 7).
+//   MC: k at k R sizeof(T); 16-bit: its 32-byte units u at u ^ ((k & 3) + 4 ((k >> 3) & 1)); fp32: its 64-byte units at
+//       u ^ ((k >> 2) & 3).
+// Each exclusive-or spreads what the lanes of one read touch over all banks.
+// PAIR (KC): rows 0..15, 32..47, .. are of the first matrix, the rows between them of the second.
+template <class T, int R, int NW, bool MC, bool PAIR>
+struct Operand {
+    static constexpr int Q = R / 8 / NW;             // pieces of a wave
+    static constexpr int BK = 128 / (int)sizeof(T);  // k of a stage
+    static constexpr int RB = R * (int)sizeof(T);    // MC: bytes of a k
+    static_assert(!MC || RB >= 256, "the exclusive-or of MC needs rows of 256 bytes");
+    uint32_t off[Q];   // byte offset of the lane's chunk in the first stage of a segment
+    uint32_t kbyte;    // KC: its byte within the stage's k
+    const char *base, *next;   // first row of the tile, in this segment and the second one
+    int64_t ld;
+    int rows;          // rows of the tile that exist
+
+    // `wave` and everything but `lane` are uniform
+    __device__ __forceinline__ void init(const void *const (&p)[2], int64_t ld_, int row0, int total, int wave, int lane)
+    {
+        ld = ld_;
+        rows = min(total - row0, PAIR ? R / 2 : R);
+        const int64_t at = MC ? (int64_t)row0 * (int)sizeof(T) : row0 * ld;
+        const bool second = PAIR && ((wave >> 1) & 1);
+        base = static_cast<const char *>(second ? p[1] : p[0]) + at;
+        next = PAIR ? base : static_cast<const char *>(p[1]) + at;
+        if (MC) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int byte = (wave + q * NW) * 1024 + lane * 16, k = byte / RB;
+                int x = byte % RB;
+                x ^= sizeof(T) == 2 ? ((k & 3) + 4 * ((k >> 3) & 1)) << 5 : ((k >> 2) & 3) << 6;
+                off[q] = (uint32_t)(k * ld) + (uint32_t)x;
+            }
+            kbyte = 0;
+        } else {
+            const int r = 8 * (wave & 1) + (lane >> 3);   // within a block of 16 rows
+            kbyte = (uint32_t)(((lane & 7) ^ ((r >> 1) & 7)) * 16);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int block = (wave >> 1) + q * (NW / 2);   // of sixteen rows
+                off[q] = (uint32_t)((r + 16 * (PAIR ? block >> 1 : block)) * ld) + kbyte;
+            }
+        }
+    }
+
+    // stage `step` of this segment (K elements long) from memory straight into LDS; what lies outside the matrix becomes zero
+    // or (columns of MC beyond the tile) a number that no result depends on.  Pieces of 16 bytes lie inside or outside whole.
+    __device__ __forceinline__ void fetch(lds_char *lds, bool second, int step, int K, int wave) const
+    {
+        const int k0 = step * BK, kleft = K - k0;
+        const char *b = second ? next : base;
+        if (MC) {
+            b += (int64_t)k0 * ld;
+            const int64_t bytes = (int64_t)(min(kleft, BK) - 1) * ld + rows * (int)sizeof(T);
+            const auto res = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(b), 0, (int)bytes, 0x00020000);
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * 1024), 16, (int)off[q], 0, 0, 0);
+        } else {
+            b += (int64_t)k0 * (int)sizeof(T);
+            const int64_t bytes = (int64_t)(rows - 1) * ld + kleft * (int)sizeof(T);
+            const auto res = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(b), 0, (int)bytes, 0x00020000);
+            const uint32_t out = (int)kbyte < kleft * (int)sizeof(T) ? 0u : 0x80000000u;
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * 1024), 16, (int)(off[q] | out), 0, 0, 0);
+        }
+    }
+
+    // the same through registers, for operands at any alignment and of any length
+    __device__ __forceinline__ void load(v4u (&v)[Q], bool second, int step, int K, int wave, int lane) const
+    {
+        constexpr int E = 16 / (int)sizeof(T);
+        const int k0 = step * BK, kleft = K - k0;
+        const char *b = (second ? next : base) + (MC ? (int64_t)k0 * ld : (int64_t)k0 * (int)sizeof(T));
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            int there, line, lines;   // elements of the chunk that exist; its row, and how many there are
+            if (MC) {
+                const int k = ((wave + q * NW) * 1024 + lane * 16) / RB;
+                there = rows - (int)((off[q] - (uint32_t)(k * ld)) / sizeof(T));
+                line = k;
+                lines = kleft;
+            } else {
+                there = kleft - (int)(kbyte / sizeof(T));
+                const int r = 8 * (wave & 1) + (lane >> 3), block = (wave >> 1) + q * (NW / 2);
+                line = r + 16 * (PAIR ? block >> 1 : block);
+                lines = rows;
+            }
+            if (line >= lines) there = 0;
+            const T *p = reinterpret_cast<const T *>(b + off[q]);
+            typedef T Piece __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    
+            if (there >= E) {
+                v[q] = __builtin_bit_cast(v4u, *reinterpret_cast<const Piece *>(p));
+            } else {
+                Piece x;
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] = j < there ? p[j] : (T)0.f;
+                v[q] = __builtin_bit_cast(v4u, x);
+            }
+        }
+    }
+    static __device__ __forceinline__ void put(lds_char *lds, const v4u (&v)[Q], int wave, int lane)
+    {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            *(__attribute__((address_space(3))) v4u *)(lds + (wave + q * NW) * 1024 + lane * 16) = v[q];
+    }
+
+    // Fragments: sixteen rows from 16 block on, half kk (64 bytes of k) of the stage.  `at` from start(), block a constant
+    // below the number of blocks that the wave's rows start at a multiple of.
+    static __device__ __forceinline__ uint32_t start(int row0, int lane)
+    {
+        const int i = lane & 15, h = lane >> 4;
+        if (!MC) return (uint32_t)((row0 + i) * 128 + ((h ^ ((i >> 1) & 7)) * 16));
+        if (sizeof(T) == 2) return (uint32_t)((8 * h + (i >> 2)) * RB + (((row0 >> 4) ^ ((i >> 2) + 4 * (h & 1))) << 5) + (i & 3) * 8);
+        return (uint32_t)(4 * h * RB + (((row0 >> 4) ^ h) << 6) + i * 4);
+    }
+    static __device__ __forceinline__ v4u read(const lds_char *lds, uint32_t at, int block, int kk)
+    {
+        if (!MC) {   // chunk 4 kk + h
+            const lds_char *p = lds + ((at ^ (uint32_t)(kk * 64)) + block * 2048);
+            return *(const __attribute__((address_space(3))) v4u *)p;
+        }
+        if (sizeof(T) == 2) {
+            // ds_read_b64_tr_b16: of each sixteen lanes, lanes 4 r .. 4 r + 3 read row r of a 4 x 16 block, lane i gets column i
+            const lds_char *p = lds + ((at ^ (uint32_t)(block << 5)) + kk * 32 * RB);
+            typedef __attribute__((address_space(3))) v4s *P;
+            const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds_char *)p);
+            const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds_char *)(p + 4 * RB));
+            return __builtin_bit_cast(v4u, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        const lds_char *p = lds + ((at ^ (uint32_t)(block << 6)) + kk * 16 * RB);
+        v4u v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = *(const __attribute__((address_space(3))) uint32_t *)(p + j * RB);
+        return v;
+    }
+};
+
+// Workgroup b of n runs on XCD b mod 8: each XCD gets a run of consecutive tiles, and they go down bands of four tile rows, so
+// that the workgroups of an XCD share operands in its L2.
+__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    const int n = tiles_m * tiles_n, each = n / 8, more = n % 8, x = b % 8;
+    const int t = x * each + min(x, more) + b / 8;
+    const int band = t / (4 * tiles_n), first = band * 4, high = min(4, tiles_m - first), in = t - band * 4 * tiles_n;
+    tm = first + in % high;
+    tn = in / high;
+}
+
+// every wave's loads into LDS are there, and every wave is done with what it read
+__device__ __forceinline__ void arrived()
+{
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// WM x WN waves, each TM x TN blocks of 16 x 16
+template <int WM_, int WN_, int TM_, int TN_>
+struct Shape {
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
+};
+typedef Shape<2, 4, 8, 4> Large;   // 256 x 256, 8 waves
+typedef Shape<2, 2, 4, 4> Small;   // 128 x 128, 4 waves
+
+template <class T, int P, int EPI, class S, bool DIRECT, bool SUMS>
+__global__ __launch_bounds__(S::NW * 64, S::NW == 8 ? 2 : 2) void product_kernel(const ProductArgs a)
+{
+    constexpr bool PAIR = EPI == E_GATED;
+    typedef Operand<T, S::BM, S::NW, P == P_GRAD, false> OpA;
+    typedef Operand<T, S::BN, S::NW, P != P_FWD, PAIR> OpB;
+    constexpr int COLS = PAIR ? S::BN / 2 : S::BN;
+    __shared__ __attribute__((aligned(1024))) char stage0[(S::BM + S::BN) * 128];
+    __shared__ __attribute__((aligned(1024))) char stage1[(S::BM + S::BN) * 128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int tm, tn;
+    tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
+    const int m0 = tm * S::BM, n0 = tn * COLS;
+    const int wm = wave / S::WN, wn = wave % S::WN;
+
+    OpA oa;
+    OpB ob;
+    oa.init(a.a, a.lda, m0, a.M, wave, lane);
+    ob.init(a.b, a.ldb, n0, a.N, wave, lane);
+    const int per_seg = (a.K + OpA::BK - 1) / OpA::BK, all = per_seg * a.segments;
+    const int t0 = blockIdx.y * a.steps, t1 = min(all, t0 + a.steps);
+
+    v4f acc[S::TM][S::TN] = {};
+    v4f sum[SUMS ? S::TM : 1] = {};
+    const bool sums = SUMS && tn == 0 && wn == 0;
+    const uint32_t ra = OpA::start(wm * S::TM * 16, lane), rb = OpB::start(wn * S::TN * 16, lane);
+
+    auto fetch = [&](char *stage, int t) {
+        const bool second = t >= per_seg;
+        const int step = second ? t - per_seg : t;
+        lds_char *l = (lds_char *)stage;
+        if constexpr (DIRECT) {
+            oa.fetch(l, second, step, a.K, wave);
+            ob.fetch(l + S::BM * 128, second, step, a.K, wave);
+        } else {
+            v4u va[OpA::Q], vb[OpB::Q];
+            oa.load(va, second, step, a.K, wave, lane);
+            ob.load(vb, second, step, a.K, wave, lane);
+            OpA::put(l, va, wave, lane);
+            OpB::put(l + S::BM * 128, vb, wave, lane);
+        }
+    };
+    auto contract = [&](const char *stage) {
+        const lds_char *l = (const lds_char *)stage;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            v4u fb[S::TN], fa[S::TM];
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) fb[j] = OpB::read(l + S::BM * 128, rb, j, kk);
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i) fa[i] = OpA::read(l, ra, i, kk);
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j], T());
+            if (SUMS && sums)
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i) sum[i] = mfma(ones<T>(), fa[i], sum[i], T());
+        }
+    };
+
+    if (t0 < t1) {
+        fetch(stage0, t0);
+        arrived();
+        int t = t0;
+        for (; t + 1 < t1; t += 2) {
+            fetch(stage1, t + 1);
+            contract(stage0);
+            arrived();
+            if (t + 2 < t1) fetch(stage0, t + 2);
+            contract(stage1);
+            arrived();
+        }
+        if (t < t1) contract(stage0);
+        __syncthreads();
+    }
+
+    // Epilogue.  A wave turns its sums through its own 16 KB of LDS, sixty-four rows at a time, so that a lane gets eight
+    // neighbouring columns of a row: rows of 256 bytes, their 16-byte units u at u ^ (row mod 16).
+    const int i16 = lane & 15, h = lane >> 4;
+    const int64_t plane = (int64_t)a.M * a.N;
+    const int row0 = m0 + wm * S::TM * 16;
+    if (SUMS && sums && h == 0)
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i) {
+            const int m = row0 + i * 16 + i16;
+            if (m < a.M) {
+                if (a.split > 1) a.ws[a.split * plane + (int64_t)blockIdx.y * a.M + m] = sum[i][0];
+                else finish_sum<T>(a.f, m, sum[i][0]);
+            }
+        }
+    float *part = a.ws + blockIdx.y * plane * (PAIR ? 2 : 1);
+    char *own = (wave < S::NW / 2 ? stage0 : stage1) + wave % (S::NW / 2) * 16384;
+    constexpr int LANES = PAIR ? 4 : 8;   // of a row
+    const int c = lane % LANES, n = n0 + wn * (PAIR ? 32 : 64) + c * 8;
+    auto unit = [&](int row, int u) { return reinterpret_cast<v4f *>(own + row * 256 + ((u ^ (row & 15)) << 4)); };
+#pragma unroll
+    for (int i0 = 0; i0 < S::TM; i0 += 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)   // a pair's blocks alternate: those of the first matrix first
+                *unit(i * 16 + i16, (PAIR ? (j >> 1) + (j & 1) * 2 : j) * 4 + h) = acc[i0 + i][j];
+#pragma unroll 1
+        for (int r = lane / LANES; r < 64; r += 64 / LANES) {
+            const int m = row0 + i0 * 16 + r;
+            if (m >= a.M || n >= a.N) break;
+            float v[8], w[8];
+            const v4f x = *unit(r, 2 * c), y = *unit(r, 2 * c + 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = x[j];
+                v[4 + j] = y[j];
+            }
+            if (PAIR) {
+                const v4f p = *unit(r, 8 + 2 * c), q = *unit(r, 9 + 2 * c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j] = p[j];
+                    w[4 + j] = q[j];
+                }
+            }
+            if (a.split > 1) {
+                store8<float>(part, (int64_t)m * a.N + n, v, a.N - n);
+                if (PAIR) store8<float>(part, plane + (int64_t)m * a.N + n, w, a.N - n);
+            } else {
+                finish8<T, EPI>(a.f, m, n, a.N, v, w);
+            }
+        }
+    }
+}
+
+// The parts of a product whose k was split, added in order, and its epilogue.  A thread takes eight columns of one row.
+template <class T, int EPI>
+__global__ __launch_bounds__(256) void join_kernel(const ProductArgs a, int sums)
+{
+    constexpr int PLANES = EPI == E_GATED ? 2 : 1;
+    const int eights = (a.N + 7) / 8;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, plane = (int64_t)a.M * a.N;
+    if (at < (int64_t)a.M * eights) {
+        const int m = (int)(at / eights), n = (int)(at % eights) * 8;
+        float v[8] = {}, w[8] = {};
+        for (int s = 0; s < a.split; ++s) {
+            const float *p = a.ws + s * plane * PLANES;
+            float x[8];
+            load8<float>(x, p, (int64_t)m * a.N + n, a.N - n);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += x[j];
+            if (PLANES == 2) {
+                load8<float>(x, p + plane, (int64_t)m * a.N + n, a.N - n);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] += x[j];
+            }
+        }
+        finish8<T, EPI>(a.f, m, n, a.N, v, w);
+    }
+    if (EPI == E_STORE && sums && at < a.M) {
+        float v = 0.f;
+        for (int s = 0; s < a.split; ++s) v += a.ws[a.split * plane + (int64_t)s * a.M + at];
+        finish_sum<T>(a.f, (int)at, v);
+    }
+}
+
+}  // namespace dn

@@ -18,7 +18,10 @@ LIB_PATH = os.path.join(_HERE, "libdn.so")
 
 DN_OK, DN_ERR_INVALID_ARG, DN_ERR_SHAPE, DN_ERR_UNSUPPORTED, DN_ERR_OOM, DN_ERR_DEVICE = range(6)
 DN_ACT_LINEAR, DN_ACT_SIGMOID, DN_ACT_TANH, DN_ACT_RELU, DN_ACT_SOFTMAX = range(5)
+DN_ACT_SILU, DN_ACT_GELU = 5, 6
 DN_LOSS_MSE, DN_LOSS_CROSS_ENTROPY = 0, 1
+DN_F32, DN_F16, DN_BF16 = range(3)
+DN_NORM_NONE, DN_NORM_RMS, DN_NORM_LAYER = range(3)
 DN_K_FORWARD, DN_K_DELTA, DN_K_GRAD_UPDATE, DN_K_OUTPUT, DN_K_ONLINE = range(5)
 KERNEL_CLASS_NAMES = ["forward", "delta", "grad_update", "output", "online"]
 (DN_SCHED_NONE, DN_SCHED_LAUNCHES, DN_SCHED_PER_SAMPLE, DN_SCHED_TWO_COPY, DN_SCHED_MINIBATCH,
@@ -42,7 +45,33 @@ EXPORTS = [
     "dn_conv_backward_static", "dn_conv_backward_static_limit",
     "dn_cnn_arena_bytes", "dn_cnn_create", "dn_cnn_destroy", "dn_cnn_dense", "dn_cnn_flat_size",
     "dn_cnn_set_filters", "dn_cnn_get_filters", "dn_cnn_get_filter_grads", "dn_cnn_forward", "dn_cnn_train_epoch",
+    "dn_linear_forward_workspace_bytes", "dn_linear_backward_workspace_bytes", "dn_linear_forward", "dn_linear_backward",
+    "dn_ffn_forward_workspace_bytes", "dn_ffn_backward_workspace_bytes", "dn_ffn_forward", "dn_ffn_backward",
+    "dn_norm_backward_workspace_bytes", "dn_norm_forward", "dn_norm_backward", "dn_dropout",
 ]
+
+
+class LinearDesc(C.Structure):
+    """dn_linear_desc"""
+    _fields_ = [("type", C.c_int32), ("grad_type", C.c_int32), ("act", C.c_int32), ("rows", C.c_int32),
+                ("n_in", C.c_int32), ("n_out", C.c_int32), ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldr", C.c_int64),
+                ("ldy", C.c_int64), ("drop", C.c_float), ("grad_scale", C.c_float), ("seed", C.c_uint64),
+                ("offset", C.c_uint64)]
+
+
+class FfnDesc(C.Structure):
+    """dn_ffn_desc"""
+    _fields_ = [("type", C.c_int32), ("grad_type", C.c_int32), ("act", C.c_int32), ("rows", C.c_int32),
+                ("d", C.c_int32), ("f", C.c_int32), ("ldx", C.c_int64), ("ldr", C.c_int64), ("ldy", C.c_int64),
+                ("drop", C.c_float), ("grad_scale", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint64)]
+
+
+class NormDesc(C.Structure):
+    """dn_norm_desc"""
+    _fields_ = [("type", C.c_int32), ("grad_type", C.c_int32), ("rows", C.c_int32), ("d", C.c_int32),
+                ("post", C.c_int32), ("pre", C.c_int32), ("rows_per_gate", C.c_int32), ("scale", C.c_float),
+                ("eps", C.c_float)]
+
 
 _lib = None
 
@@ -100,6 +129,17 @@ def lib():
             f.argtypes = [vp, i32, vp, vp]
         l.dn_cnn_forward.argtypes = [vp, vp, i32, vp]
         l.dn_cnn_train_epoch.argtypes = [vp, vp, vp, i64, i32, f32, f32, C.POINTER(f32)]
+        sz, u64 = C.c_size_t, C.c_uint64
+        for f in (l.dn_linear_forward_workspace_bytes, l.dn_linear_backward_workspace_bytes, l.dn_ffn_forward_workspace_bytes,
+                  l.dn_ffn_backward_workspace_bytes, l.dn_norm_backward_workspace_bytes):
+            f.argtypes = [vp]
+        l.dn_linear_forward.argtypes = [vp] * 8 + [sz, vp]
+        l.dn_linear_backward.argtypes = [vp] * 9 + [sz, vp]
+        l.dn_ffn_forward.argtypes = [vp] * 12 + [sz, vp]
+        l.dn_ffn_backward.argtypes = [vp] * 15 + [sz, vp]
+        l.dn_norm_forward.argtypes = [vp] * 11
+        l.dn_norm_backward.argtypes = [vp] * 17 + [sz, vp]
+        l.dn_dropout.argtypes = [i32, vp, vp, i32, i32, i64, i64, f32, u64, u64, vp]
         for name in EXPORTS[2:]:
             if name.endswith("_workspace_bytes") or name.endswith("_static_limit") or name.endswith("_arena_bytes"):
                 getattr(l, name).restype = C.c_size_t
@@ -301,6 +341,216 @@ def dn_sgd_step(param, grad, velocity, lr: float, momentum: float):
                                  None if velocity is None else _dev_ptr(velocity, f32, "velocity"),
                                  int(param.numel()), float(lr), float(momentum), C.c_void_p(stream.cuda_stream)),
                "dn_sgd_step")
+
+
+# ---- the residual feed-forward block -----------------------------------------------------------------------------
+
+def _type_of(t, what: str) -> int:
+    import torch
+    kinds = {torch.float32: DN_F32, torch.float16: DN_F16, torch.bfloat16: DN_BF16}
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in kinds:
+        raise TypeError("%s must be a device tensor of float32, float16 or bfloat16" % what)
+    return kinds[t.dtype]
+
+
+def _matrix(t, like, rows: int, cols: int, what: str):
+    """(pointer, elements between rows) of a matrix of `like`'s type and device; rows may lie apart."""
+    if t is None:
+        return None, 0
+    if t.dtype != like.dtype or t.device != like.device:
+        raise TypeError("%s must be a tensor of dtype %s on %s" % (what, like.dtype, like.device))
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise TypeError("%s must have shape %s, not %s" % (what, (rows, cols), tuple(t.shape)))
+    step, one = t.stride()
+    if (one != 1 and cols > 1) or (step < cols and rows > 1):
+        raise TypeError("%s must have contiguous rows that do not overlap" % what)
+    return t.data_ptr(), step if rows > 1 else cols
+
+
+def _dense(t, like, shape, what: str, dtype=None):
+    """The pointer of a contiguous tensor of `like`'s type (or `dtype`) and device, None for None."""
+    if t is None:
+        return None
+    if t.dtype != (dtype or like.dtype) or t.device != like.device or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous tensor of dtype %s on %s" % (what, dtype or like.dtype, like.device))
+    if t.shape != shape:
+        raise TypeError("%s must have shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _grad_type(grad, like):
+    """Parameter gradients are of the tensors' own type or fp32."""
+    import torch
+    if grad is not None and grad.dtype == torch.float32:
+        return DN_F32, torch.float32
+    return _type_of(like, "X"), like.dtype
+
+
+def _workspace(need: int, workspace, like, where: str):
+    """(the tensor, its pointer, its bytes); allocated here if the caller brings none."""
+    import torch
+    if need == C.c_size_t(-1).value:
+        return None, None, 0      # the call itself says what is wrong
+    if workspace is None:
+        if need == 0:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    elif workspace.dtype != torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous uint8 tensor on %s" % (like.device,))
+    return workspace, workspace.data_ptr(), workspace.numel()
+
+
+def _on(like):
+    import torch
+    return torch.cuda.device(like.device)
+
+
+def _stream(like) -> int:
+    import torch
+    return torch.cuda.current_stream(like.device).cuda_stream
+
+
+def _two(t, what: str):
+    if t.dim() != 2:
+        raise TypeError("%s must be a matrix" % what)
+    return t.shape
+
+
+def _linear_desc(X, W, R, Y, Yname, act, drop, seed, offset, grad_type, grad_scale):
+    kind = _type_of(X, "X")
+    rows, n_in = _two(X, "X")
+    n_out = _two(W, "W")[0]
+    x, ldx = _matrix(X, X, rows, n_in, "X")
+    w, ldw = _matrix(W, X, n_out, n_in, "W")
+    r, ldr = _matrix(R, X, rows, n_out, "R")
+    y, ldy = _matrix(Y, X, rows, n_out, Yname)
+    d = LinearDesc(kind, kind if grad_type is None else grad_type, int(act), rows, n_in, n_out, ldx, ldw, ldr, ldy, float(drop),
+                   float(grad_scale), int(seed), int(offset))
+    return d, x, w, r, y, rows, n_in, n_out
+
+
+def dn_linear_forward(X, W, bias, R, Y, Z=None, act: int = DN_ACT_LINEAR, drop: float = 0.0, seed: int = 0, offset: int = 0,
+                      workspace=None):
+    """Y = R + D(f(X W^T + bias)); Z receives X W^T + bias.  bias, R and Z may be None.  Enqueued on torch's current stream, as
+    everything below; `workspace`: a uint8 tensor of dn_linear_forward_workspace_bytes bytes (allocated here if None)."""
+    l = lib()
+    d, x, w, r, y, rows, _, n_out = _linear_desc(X, W, R, Y, "Y", act, drop, seed, offset, None, 1.0)
+    b, z = _dense(bias, X, (n_out,), "bias"), _dense(Z, X, (rows, n_out), "Z")
+    with _on(X):
+        at = C.addressof(d)
+        _keep, ws, n = _workspace(l.dn_linear_forward_workspace_bytes(at), workspace, X, "dn_linear_forward")
+        _check(l.dn_linear_forward(at, x, w, b, r, y, z, ws, n, _stream(X)), "dn_linear_forward")
+
+
+def dn_linear_backward(X, W, Z, dY, dX, dW, dbias, act: int = DN_ACT_LINEAR, drop: float = 0.0, seed: int = 0, offset: int = 0,
+                       grad_scale: float = 1.0, workspace=None):
+    """delta = D(dY) f'(Z); dX = delta W, dW = grad_scale delta^T X, dbias = grad_scale times delta's column sums.  Z may be
+    None without an activation; dX, dW, dbias may be None; dW and dbias are of X's type or float32."""
+    l = lib()
+    gt, gdtype = _grad_type(dW, X)
+    d, x, w, _, y, rows, n_in, n_out = _linear_desc(X, W, None, dY, "dY", act, drop, seed, offset, gt, grad_scale)
+    z, dx = _dense(Z, X, (rows, n_out), "Z"), _dense(dX, X, (rows, n_in), "dX")
+    dw, db = _dense(dW, X, (n_out, n_in), "dW", gdtype), _dense(dbias, X, (n_out,), "dbias", gdtype)
+    with _on(X):
+        at = C.addressof(d)
+        _keep, ws, n = _workspace(l.dn_linear_backward_workspace_bytes(at), workspace, X, "dn_linear_backward")
+        _check(l.dn_linear_backward(at, x, w, z, y, dx, dw, db, ws, n, _stream(X)), "dn_linear_backward")
+
+
+def _ffn_desc(X, Wg, Wu, Wd, R, Y, Yname, act, drop, seed, offset, grad_type, grad_scale):
+    kind = _type_of(X, "X")
+    rows, d = _two(X, "X")
+    f = _two(Wg, "Wg")[0]
+    x, ldx = _matrix(X, X, rows, d, "X")
+    r, ldr = _matrix(R, X, rows, d, "R")
+    y, ldy = _matrix(Y, X, rows, d, Yname)
+    desc = FfnDesc(kind, kind if grad_type is None else grad_type, int(act), rows, d, f, ldx, ldr, ldy, float(drop),
+                   float(grad_scale), int(seed), int(offset))
+    return desc, x, r, y, _dense(Wg, X, (f, d), "Wg"), _dense(Wu, X, (f, d), "Wu"), _dense(Wd, X, (d, f), "Wd"), rows, d, f
+
+
+def dn_ffn_forward(X, Wg, bg, Wu, bu, Wd, bd, R, Y, GU=None, act: int = DN_ACT_SILU, drop: float = 0.0, seed: int = 0,
+                   offset: int = 0, workspace=None):
+    """Y = R + D((f(X Wg^T + bg) * (X Wu^T + bu)) Wd^T + bd); GU [rows][2 f] receives both net inputs.  The biases, R and GU
+    may be None."""
+    l = lib()
+    desc, x, r, y, wg, wu, wd, rows, d, f = _ffn_desc(X, Wg, Wu, Wd, R, Y, "Y", act, drop, seed, offset, None, 1.0)
+    g, u, b = _dense(bg, X, (f,), "bg"), _dense(bu, X, (f,), "bu"), _dense(bd, X, (d,), "bd")
+    gu = _dense(GU, X, (rows, 2 * f), "GU")
+    with _on(X):
+        at = C.addressof(desc)
+        _keep, ws, n = _workspace(l.dn_ffn_forward_workspace_bytes(at), workspace, X, "dn_ffn_forward")
+        _check(l.dn_ffn_forward(at, x, wg, g, wu, u, wd, b, r, y, gu, ws, n, _stream(X)), "dn_ffn_forward")
+
+
+def dn_ffn_backward(X, Wg, Wu, Wd, GU, dY, dX, dWg, dbg, dWu, dbu, dWd, dbd, act: int = DN_ACT_SILU, drop: float = 0.0,
+                    seed: int = 0, offset: int = 0, grad_scale: float = 1.0, workspace=None):
+    """The block's gradients; dX and the biases' may be None, the parameters' are all of X's type or all float32."""
+    l = lib()
+    gt, gdtype = _grad_type(dWg, X)
+    desc, x, _, y, wg, wu, wd, rows, d, f = _ffn_desc(X, Wg, Wu, Wd, None, dY, "dY", act, drop, seed, offset, gt, grad_scale)
+    gu, dx = _dense(GU, X, (rows, 2 * f), "GU"), _dense(dX, X, (rows, d), "dX")
+    dwg, dwu, dwd = (_dense(t, X, s, n, gdtype) for t, s, n in ((dWg, (f, d), "dWg"), (dWu, (f, d), "dWu"), (dWd, (d, f), "dWd")))
+    g, u, b = (_dense(t, X, (m,), n, gdtype) for t, m, n in ((dbg, f, "dbg"), (dbu, f, "dbu"), (dbd, d, "dbd")))
+    with _on(X):
+        at = C.addressof(desc)
+        _keep, ws, n = _workspace(l.dn_ffn_backward_workspace_bytes(at), workspace, X, "dn_ffn_backward")
+        _check(l.dn_ffn_backward(at, x, wg, wu, wd, gu, y, dx, dwg, g, dwu, u, dwd, b, ws, n, _stream(X)), "dn_ffn_backward")
+
+
+def _norm_desc(like, gate, post, pre, scale, eps, rows_per_gate, grad_type=None):
+    kind = _type_of(like, "x")
+    rows, d = _two(like, "x")
+    per = rows if rows_per_gate is None else int(rows_per_gate)
+    desc = NormDesc(kind, kind if grad_type is None else grad_type, rows, d, int(post), int(pre), max(per, 0), float(scale), float(eps))
+    return desc, rows, d, -(-rows // per) if per > 0 else 0
+
+
+def dn_norm_forward(x, b, gate, post_w, post_b, pre_w, pre_b, x_out, n_out, post: int = DN_NORM_RMS, pre: int = DN_NORM_RMS,
+                    scale: float = 1.0, eps: float = 1e-5, rows_per_gate: Optional[int] = None):
+    """x_out = x + scale gate post(b), n_out = pre(x_out).  b, gate, the norms' weights and shifts may be None (no block,
+    ones, zeros); gate [ceil(rows / rows_per_gate)][d] (default: one row)."""
+    l = lib()
+    desc, rows, d, groups = _norm_desc(x, gate, post, pre, scale, eps, rows_per_gate)
+    big, one = (rows, d), (d,)
+    p = [_dense(x, x, big, "x"), _dense(b, x, big, "b"), _dense(gate, x, (groups, d), "gate"), _dense(post_w, x, one, "post_w"),
+         _dense(post_b, x, one, "post_b"), _dense(pre_w, x, one, "pre_w"), _dense(pre_b, x, one, "pre_b"),
+         _dense(x_out, x, big, "x_out"), _dense(n_out, x, big, "n_out")]
+    with _on(x):
+        _check(l.dn_norm_forward(C.addressof(desc), *p, _stream(x)), "dn_norm_forward")
+
+
+def dn_norm_backward(x, b, gate, post_w, post_b, pre_w, dx_out, dn, dx, db, dgate, dpost_w, dpost_b, dpre_w, dpre_b,
+                     post: int = DN_NORM_RMS, pre: int = DN_NORM_RMS, scale: float = 1.0, eps: float = 1e-5,
+                     rows_per_gate: Optional[int] = None, workspace=None):
+    """The gradients of dn_norm_forward; x is its x_out.  dx_out may be None (zero), so may the gradients of gate, weights and
+    shifts (not computed), which are all of x's type or all float32."""
+    l = lib()
+    like = x if x is not None else dx
+    grads = [t for t in (dgate, dpost_w, dpost_b, dpre_w, dpre_b) if t is not None]
+    gt, gdtype = _grad_type(grads[0] if grads else None, like)
+    desc, rows, d, groups = _norm_desc(like, gate, post, pre, scale, eps, rows_per_gate, gt)
+    big, one = (rows, d), (d,)
+    p = [_dense(x, like, big, "x"), _dense(b, like, big, "b"), _dense(gate, like, (groups, d), "gate"),
+         _dense(post_w, like, one, "post_w"), _dense(post_b, like, one, "post_b"), _dense(pre_w, like, one, "pre_w"),
+         _dense(dx_out, like, big, "dx_out"), _dense(dn, like, big, "dn"), _dense(dx, like, big, "dx"), _dense(db, like, big, "db"),
+         _dense(dgate, like, (groups, d), "dgate", gdtype), _dense(dpost_w, like, one, "dpost_w", gdtype),
+         _dense(dpost_b, like, one, "dpost_b", gdtype), _dense(dpre_w, like, one, "dpre_w", gdtype),
+         _dense(dpre_b, like, one, "dpre_b", gdtype)]
+    with _on(like):
+        at = C.addressof(desc)
+        _keep, ws, n = _workspace(l.dn_norm_backward_workspace_bytes(at), workspace, like, "dn_norm_backward")
+        _check(l.dn_norm_backward(at, *p, ws, n, _stream(like)), "dn_norm_backward")
+
+
+def dn_dropout(X, Y, drop: float, seed: int, offset: int = 0):
+    """Y = D(X), forward and backward alike; Y may be X, rows of either may lie apart."""
+    kind = _type_of(X, "X")
+    rows, cols = _two(X, "X")
+    x, ldx = _matrix(X, X, rows, cols, "X")
+    y, ldy = _matrix(Y, X, rows, cols, "Y")
+    with _on(X):
+        _check(lib().dn_dropout(kind, x, y, rows, cols, ldx, ldy, float(drop), int(seed), int(offset), _stream(X)), "dn_dropout")
 
 
 class Net:
