@@ -18,24 +18,29 @@ template <> struct Elem<bf16> { static constexpr int TYPE = DN_BF16; };
 // eight elements as they lie in memory, at any alignment of theirs
 template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
 
-template <class T>
-__device__ __forceinline__ void load8(float (&v)[8], const void *p, int64_t at, int left)
+// elements from p[at] on; those from `left` on are zero, and not stored.  ALL: left is 8 or more.
+template <class T, bool ALL = false>
+__device__ __forceinline__ typename Eight<T>::type get8(const void *p, int64_t at, int left)
 {
     const T *q = static_cast<const T *>(p) + at;
-    if (left >= 8) {
-        const auto x = *reinterpret_cast<const typename Eight<T>::type *>(q);
+    if (ALL || left >= 8) return *reinterpret_cast<const typename Eight<T>::type *>(q);
+    typename Eight<T>::type x;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < left ? (float)q[j] : 0.f;
-    }
+    for (int j = 0; j < 8; ++j) x[j] = j < left ? q[j] : (T)0.f;
+    return x;
 }
-template <class T>
+template <class T, bool ALL = false>
+__device__ __forceinline__ void load8(float (&v)[8], const void *p, int64_t at, int left)
+{
+    const auto x = get8<T, ALL>(p, at, left);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
+}
+template <class T, bool ALL = false>
 __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8], int left)
 {
     T *q = static_cast<T *>(p) + at;
-    if (left >= 8) {
+    if (ALL || left >= 8) {
         typename Eight<T>::type x;
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
@@ -208,6 +213,8 @@ struct ProductArgs {
     int32_t tiles_m, tiles_n;
     Finish f;
 };
+
+constexpr int kSumParts = 32;   // parts of k that a launch of its own adds A's columns in
 
 // How a product is run.  `ws_bytes`: workspace that it needs.
 enum ProductKernel : int { K_FEW, K_SMALL_ANY, K_SMALL, K_LARGE };

@@ -189,8 +189,9 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
         return plan;
     }
     auto tiles = [&](int64_t edge) { return (M + edge - 1) / edge * ((N + (e == E_GATED ? edge / 2 : edge) - 1) / (e == E_GATED ? edge / 2 : edge)); };
-    if (direct && tiles(256) >= 192) {
+    if (type != DN_F32 && direct && tiles(256) >= 192) {
         plan.kernel = K_LARGE;
+        if (sums) plan.ws_bytes = (size_t)kSumParts * (size_t)M * sizeof(float);
         return plan;
     }
     plan.kernel = direct ? K_SMALL : K_SMALL_ANY;

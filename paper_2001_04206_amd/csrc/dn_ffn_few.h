@@ -69,6 +69,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProductArgs a
     // a thread: eight columns of one row, the lanes of two h
     const int t = threadIdx.x, m = t >> 1, n = n0 + 8 * (t & 1);
     if (t >= 32 * MB || m >= a.M || n >= a.N) return;
+    Beside<T, EPI> side;
+    side.template get<false>(a.f, m, n, a.N - n);
     float v[8] = {}, u[8] = {};
 #pragma unroll
     for (int s = 0; s < kFewWaves; ++s)
@@ -82,7 +84,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProductArgs a
                 u[4 * q + j] += z[j];
             }
         }
-    finish8<T, EPI>(a.f, m, n, a.N, v, u);
+    finish8<T, EPI, false>(a.f, side, m, n, a.N - n, v, u);
 }
 
 }  // namespace dn

@@ -13,7 +13,7 @@ hipError_t tiles(ProductArgs &a, bool sums, hipStream_t s)
     const int cols = EPI == E_GATED ? S::BN / 2 : S::BN;
     a.tiles_n = (a.N + cols - 1) / cols;
     const dim3 grid((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split);
-    if constexpr (P == P_GRAD) {
+    if constexpr (P == P_GRAD && S::BM == 128) {
         if (sums) {
             launch_kernel(product_kernel<T, P, EPI, S, DIRECT, true>, grid, dim3(S::NW * 64), 0, s, a);
             return hipGetLastError();
@@ -36,7 +36,7 @@ hipError_t few(const ProductArgs &a, hipStream_t s)
 template <class T, int P, int EPI>
 hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
 {
-    const bool sums = a.f.sums != nullptr;
+    const bool sums = a.f.sums || a.f.sums2;
     a.split = plan.split;
     a.steps = plan.steps;
     hipError_t e = hipErrorInvalidValue;
@@ -46,7 +46,16 @@ hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
         return hipErrorInvalidValue;
     case K_SMALL_ANY: e = tiles<T, P, EPI, Small, false>(a, sums, s); break;
     case K_SMALL: e = tiles<T, P, EPI, Small, true>(a, sums, s); break;
-    case K_LARGE: e = tiles<T, P, EPI, Large, true>(a, sums, s); break;
+    case K_LARGE:
+        if constexpr (sizeof(T) == 2) {
+            if (P == P_GRAD && sums) {
+                launch_kernel(sum_parts_kernel<T>, dim3((unsigned)((a.M + 255) / 256), kSumParts), dim3(256), 0, s, a);
+                launch_kernel(sum_join_kernel<T>, dim3((unsigned)((a.M + 255) / 256)), dim3(256), 0, s, a);
+                if ((e = hipGetLastError()) != hipSuccess) return e;
+            }
+            return tiles<T, P, EPI, Large, true>(a, sums, s);
+        }
+        return hipErrorInvalidValue;
     }
     if (e != hipSuccess || a.split == 1) return e;
     const int64_t work = (int64_t)a.M * ((a.N + 7) / 8);

@@ -30,79 +30,106 @@ __device__ __forceinline__ v4f mfma(const v4u &a, const v4u &b, v4f c, float)
     for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
     return c;
 }
-template <class T> __device__ __forceinline__ v4u ones()
+// c plus the sum of a fragment's elements
+__device__ __forceinline__ float add_all(const v4u &a, float c, bf16)
 {
-    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(v4u, v4f{1.f, 1.f, 1.f, 1.f});
-    else {
-        const uint32_t one = (uint32_t)__builtin_bit_cast(uint16_t, (T)1.f);
-        return v4u{one * 0x10001u, one * 0x10001u, one * 0x10001u, one * 0x10001u};
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t two = a[j];   // (a cast of a[j] itself reads a[0])
+        c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2b, two), v2b{(bf16)1.f, (bf16)1.f}, c, false);
     }
+    return c;
+}
+__device__ __forceinline__ float add_all(const v4u &a, float c, f16)
+{
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t two = a[j];
+        c = __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, two), v2h{(f16)1.f, (f16)1.f}, c, false);
+    }
+    return c;
+}
+__device__ __forceinline__ float add_all(const v4u &a, float c, float)
+{
+    const v4f x = __builtin_bit_cast(v4f, a);
+    return c + ((x[0] + x[1]) + (x[2] + x[3]));
 }
 
 // ---- epilogues -------------------------------------------------------------------------------------------------------
 
-// The epilogue of row m, columns n .. n + 7 of N (n a multiple of 8, n < N): `v` the sums, E_GATED: `w` those of the second
-// matrix.
+// What the epilogue of row m, columns n .. n + 7 of N (n a multiple of 8, n < N) reads: the residual; G and U.  Apart from
+// finish8 so that a thread's reads of several rows can be under way together.  ALL: all eight columns exist.
 template <class T, int EPI>
-__device__ __forceinline__ void finish8(const Finish &e, int m, int n, int N, float (&v)[8], float (&w)[8])
+struct Beside {
+    typename Eight<T>::type r, u;
+    template <bool ALL>
+    __device__ __forceinline__ void get(const Finish &e, int m, int n, int left)
+    {
+        if (EPI == E_LINEAR && e.r) r = get8<T, ALL>(e.r, m * e.ldr + n, left);
+        if (EPI == E_DGATED) {
+            r = get8<T, ALL>(e.r, m * e.ldr + n, left);
+            u = get8<T, ALL>(e.r, m * e.ldr + n + e.half, left);
+        }
+    }
+};
+
+// The epilogue: `v` the sums, E_GATED: `w` those of the second matrix.
+template <class T, int EPI, bool ALL>
+__device__ __forceinline__ void finish8(const Finish &e, const Beside<T, EPI> &side, int m, int n, int left, float (&v)[8], float (&w)[8])
 {
     constexpr bool FAST = sizeof(T) == 2;
-    const int left = N - n;
     if constexpr (EPI == E_LINEAR) {
         if (e.bias) {
             float b[8];
-            load8<T>(b, e.bias, n, left);
+            load8<T, ALL>(b, e.bias, n, left);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += b[j];
         }
-        if (e.y2) store8<T>(e.y2, m * e.ldy2 + n, v, left);
+        if (e.y2) store8<T, ALL>(e.y2, m * e.ldy2 + n, v, left);
         if (e.act != DN_ACT_LINEAR)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = act_value<FAST>(e.act, v[j]);
         if (e.drop.t) drop8(e.drop, m, n, v);
-        if (e.r) {
-            float r[8];
-            load8<T>(r, e.r, m * e.ldr + n, left);
+        if (e.r)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += r[j];
-        }
-        store8<T>(e.y, m * e.ldy + n, v, left);
+            for (int j = 0; j < 8; ++j) v[j] += (float)side.r[j];
+        store8<T, ALL>(e.y, m * e.ldy + n, v, left);
     } else if constexpr (EPI == E_GATED) {
         if (e.bias) {
             float b[8];
-            load8<T>(b, e.bias, n, left);
+            load8<T, ALL>(b, e.bias, n, left);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += b[j];
         }
         if (e.bias2) {
             float b[8];
-            load8<T>(b, e.bias2, n, left);
+            load8<T, ALL>(b, e.bias2, n, left);
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] += b[j];
         }
         if (e.y2) {
-            store8<T>(e.y2, m * e.ldy2 + n, v, left);
-            store8<T>(e.y2, m * e.ldy2 + n + e.half, w, left);
+            store8<T, ALL>(e.y2, m * e.ldy2 + n, v, left);
+            store8<T, ALL>(e.y2, m * e.ldy2 + n + e.half, w, left);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = act_value<FAST>(e.act, v[j]) * w[j];
-        store8<T>(e.y, m * e.ldy + n, v, left);
+        store8<T, ALL>(e.y, m * e.ldy + n, v, left);
     } else if constexpr (EPI == E_DGATED) {
-        float g[8], u[8];
-        load8<T>(g, e.r, m * e.ldr + n, left);
-        load8<T>(u, e.r, m * e.ldr + n + e.half, left);
+        float h[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float f, df;
-            act_both<FAST>(e.act, g[j], f, df);
+            act_both<FAST>(e.act, (float)side.r[j], f, df);
             v[j] *= e.alpha;
             w[j] = v[j] * f;
-            v[j] *= u[j] * df;
-            u[j] *= f;
+            v[j] *= (float)side.u[j] * df;
+            h[j] = (float)side.u[j] * f;
         }
-        store8<T>(e.y, m * e.ldy + n, v, left);
-        store8<T>(e.y, m * e.ldy + n + e.half_y, w, left);
-        store8<T>(e.y2, m * e.ldy2 + n, u, left);
+        store8<T, ALL>(e.y, m * e.ldy + n, v, left);
+        store8<T, ALL>(e.y, m * e.ldy + n + e.half_y, w, left);
+        store8<T, ALL>(e.y2, m * e.ldy2 + n, h, left);
     } else {
         const int row = m < e.m_split ? m : m - e.m_split;
         if (row >= e.m_valid) return;
@@ -110,8 +137,8 @@ __device__ __forceinline__ void finish8(const Finish &e, int m, int n, int N, fl
         for (int j = 0; j < 8; ++j) v[j] *= e.alpha;
         void *y = m < e.m_split ? e.y : e.y2;
         const int64_t at = row * (m < e.m_split ? e.ldy : e.ldy2) + n;
-        if (e.f32_out) store8<float>(y, at, v, left);
-        else store8<T>(y, at, v, left);
+        if (e.f32_out) store8<float, ALL>(y, at, v, left);
+        else store8<T, ALL>(y, at, v, left);
     }
 }
 template <class T>
@@ -119,7 +146,7 @@ __device__ __forceinline__ void finish_sum(const Finish &e, int m, float v)
 {
     void *p = m < e.m_split ? e.sums : e.sums2;
     const int at = m < e.m_split ? m : m - e.m_split;
-    if (at >= e.m_valid) return;
+    if (at >= e.m_valid || !p) return;
     if (e.f32_out) static_cast<float *>(p)[at] = v * e.alpha;
     else static_cast<T *>(p)[at] = (T)(v * e.alpha);
 }
@@ -128,21 +155,30 @@ __device__ __forceinline__ void finish_sum(const Finish &e, int m, float v)
 
 // One operand's stage of R rows in LDS, R * 128 bytes, filled by NW waves in pieces of 1024 bytes (wave w: pieces w, w + NW, ..).
 //   KC: row r at 128 r, its 16-byte chunk c at c ^ ((r >> 1) & 7).
-//   MC: k at k R sizeof(T); 16-bit: its 32-byte units u at u ^ ((k & 3) + 4 ((k >> 3) & 1)); fp32: its 64-byte units at
-//       u ^ ((k >> 2) & 3).
-// Each exclusive-or spreads what the lanes of one read touch over all banks.
+//   MC, fp32: k at k R 4, its 64-byte units u at u ^ ((k >> 2) & 3).
+//   MC, 16-bit, 128 rows: k at k 256, its 32-byte units u at u ^ ((k & 3) + 4 ((k >> 3) & 1)).
+//   MC, 16-bit, 256 rows (PAD): 32 bytes more after every piece, which is two k, and the units of odd k at u ^ 2.
+// Each spreads what the lanes of one read touch over all banks; the last one's reads have their blocks at constant
+// distances of two addresses, where an exclusive-or of three bits would take an address register for each of eight blocks.
 // PAIR (KC): rows 0..15, 32..47, .. are of the first matrix, the rows between them of the second.
 template <class T, int R, int NW, bool MC, bool PAIR>
 struct Operand {
+    static constexpr bool MC_ = MC;
     static constexpr int Q = R / 8 / NW;             // pieces of a wave
     static constexpr int BK = 128 / (int)sizeof(T);  // k of a stage
     static constexpr int RB = R * (int)sizeof(T);    // MC: bytes of a k
+    static constexpr bool PAD = MC && sizeof(T) == 2 && R == 256;
+    static constexpr int PIECE = PAD ? 1056 : 1024, STAGE = R / 8 * PIECE;
+    static constexpr int READS = MC ? (sizeof(T) == 2 ? 2 : 4) : 1;   // LDS instructions of a fragment
     static_assert(!MC || RB >= 256, "the exclusive-or of MC needs rows of 256 bytes");
-    uint32_t off[Q];   // byte offset of the lane's chunk in the first stage of a segment
+    static constexpr bool HOP = !MC || sizeof(T) == 2;   // the lane's chunks lie one distance apart
+    uint32_t off[HOP ? 1 : Q], hop;   // byte offsets of the lane's chunks in the first stage of a segment
     uint32_t kbyte;    // KC: its byte within the stage's k
     const char *base, *next;   // first row of the tile, in this segment and the second one
     int64_t ld;
     int rows;          // rows of the tile that exist
+
+    __device__ __forceinline__ uint32_t offset(int q) const { return HOP ? off[0] + q * hop : off[HOP ? 0 : q]; }
 
     // `wave` and everything but `lane` are uniform
     __device__ __forceinline__ void init(const void *const (&p)[2], int64_t ld_, int row0, int total, int wave, int lane)
@@ -155,46 +191,47 @@ struct Operand {
         next = PAIR ? base : static_cast<const char *>(p[1]) + at;
         if (MC) {
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
+            for (int q = 0; q < (HOP ? 1 : Q); ++q) {
                 const int byte = (wave + q * NW) * 1024 + lane * 16, k = byte / RB;
                 int x = byte % RB;
-                x ^= sizeof(T) == 2 ? ((k & 3) + 4 * ((k >> 3) & 1)) << 5 : ((k >> 2) & 3) << 6;
+                x ^= PAD ? (k & 1) << 6 : sizeof(T) == 2 ? ((k & 3) + 4 * ((k >> 3) & 1)) << 5 : ((k >> 2) & 3) << 6;
                 off[q] = (uint32_t)(k * ld) + (uint32_t)x;
             }
+            static_assert(!MC || !HOP || NW * 1024 / RB % 16 == 0, "the exclusive-or repeats after sixteen k");
+            hop = (uint32_t)(NW * 1024 / RB * ld);
             kbyte = 0;
         } else {
             const int r = 8 * (wave & 1) + (lane >> 3);   // within a block of 16 rows
             kbyte = (uint32_t)(((lane & 7) ^ ((r >> 1) & 7)) * 16);
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const int block = (wave >> 1) + q * (NW / 2);   // of sixteen rows
-                off[q] = (uint32_t)((r + 16 * (PAIR ? block >> 1 : block)) * ld) + kbyte;
-            }
+            const int block = wave >> 1;   // of sixteen rows; the lane's next chunk is NW / 2 blocks further on
+            off[0] = (uint32_t)((r + 16 * (PAIR ? block >> 1 : block)) * ld) + kbyte;
+            hop = (uint32_t)(16 * (PAIR ? NW / 4 : NW / 2) * ld);
         }
     }
 
-    // stage `step` of this segment (K elements long) from memory straight into LDS; what lies outside the matrix becomes zero
-    // or (columns of MC beyond the tile) a number that no result depends on.  Pieces of 16 bytes lie inside or outside whole.
-    __device__ __forceinline__ void fetch(lds_char *lds, bool second, int step, int K, int wave) const
+    // Stage `step` of a segment (K elements long) from memory straight into LDS (zeros if it is not `valid`).  What lies outside
+    // the matrix becomes zero or (columns of MC beyond the tile) a number that no result depends on.  Pieces of 16 bytes lie inside
+    // or outside whole.  aim() holds the arithmetic, so that it is out of the way when the loads are due.
+    struct Aim {
+        const char *from;
+        int bytes;
+        uint32_t first;   // offset of the lane's first chunk, past every resource if it is not to be read
+    };
+    __device__ __forceinline__ Aim aim(bool valid, bool second, int step, int K) const
     {
         const int k0 = step * BK, kleft = K - k0;
-        const char *b = second ? next : base;
-        if (MC) {
-            b += (int64_t)k0 * ld;
-            const int64_t bytes = (int64_t)(min(kleft, BK) - 1) * ld + rows * (int)sizeof(T);
-            const auto res = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(b), 0, (int)bytes, 0x00020000);
+        const char *b = (second ? next : base) + (MC ? (int64_t)k0 * ld : (int64_t)k0 * (int)sizeof(T));
+        const int64_t bytes = MC ? (int64_t)(min(kleft, BK) - 1) * ld + rows * (int)sizeof(T) : (int64_t)(rows - 1) * ld + kleft * (int)sizeof(T);
+        const bool in = valid && (MC || (int)kbyte < kleft * (int)sizeof(T));
+        return {b, valid ? (int)bytes : 0, in ? off[0] : 0x80000000u};
+    }
+    __device__ __forceinline__ void fetch(lds_char *lds, const Aim &at, int wave) const
+    {
+        const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at.from), 0, at.bytes, 0x00020000);
 #pragma unroll
-            for (int q = 0; q < Q; ++q)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * 1024), 16, (int)off[q], 0, 0, 0);
-        } else {
-            b += (int64_t)k0 * (int)sizeof(T);
-            const int64_t bytes = (int64_t)(rows - 1) * ld + kleft * (int)sizeof(T);
-            const auto res = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(b), 0, (int)bytes, 0x00020000);
-            const uint32_t out = (int)kbyte < kleft * (int)sizeof(T) ? 0u : 0x80000000u;
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * 1024), 16, (int)(off[q] | out), 0, 0, 0);
-        }
+        for (int q = 0; q < Q; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * PIECE), 16,
+                                                     (int)(HOP ? at.first + q * hop : offset(q)), 0, 0, 0);
     }
 
     // the same through registers, for operands at any alignment and of any length
@@ -208,7 +245,7 @@ struct Operand {
             int there, line, lines;   // elements of the chunk that exist; its row, and how many there are
             if (MC) {
                 const int k = ((wave + q * NW) * 1024 + lane * 16) / RB;
-                there = rows - (int)((off[q] - (uint32_t)(k * ld)) / sizeof(T));
+                there = rows - (int)((offset(q) - (uint32_t)(k * ld)) / sizeof(T));
                 line = k;
                 lines = kleft;
             } else {
@@ -218,7 +255,7 @@ struct Operand {
                 lines = rows;
             }
             if (line >= lines) there = 0;
-            const T *p = reinterpret_cast<const T *>(b + off[q]);
+            const T *p = reinterpret_cast<const T *>(b + offset(q));
             typedef T Piece __attribute__((ext_vector_type(E), aligned(sizeof(T))));
     
             if (there >= E) {
@@ -235,33 +272,38 @@ struct Operand {
     {
 #pragma unroll
         for (int q = 0; q < Q; ++q)
-            *(__attribute__((address_space(3))) v4u *)(lds + (wave + q * NW) * 1024 + lane * 16) = v[q];
+            *(__attribute__((address_space(3))) v4u *)(lds + (wave + q * NW) * PIECE + lane * 16) = v[q];
     }
 
     // Fragments: sixteen rows from 16 block on, half kk (64 bytes of k) of the stage.  `at` from start(), block a constant
     // below the number of blocks that the wave's rows start at a multiple of.
-    static __device__ __forceinline__ uint32_t start(int row0, int lane)
+    struct At { uint32_t x, y; };   // y: PAD, blocks whose bit 1 is set
+    static __device__ __forceinline__ At start(int row0, int lane)
     {
         const int i = lane & 15, h = lane >> 4;
-        if (!MC) return (uint32_t)((row0 + i) * 128 + ((h ^ ((i >> 1) & 7)) * 16));
-        if (sizeof(T) == 2) return (uint32_t)((8 * h + (i >> 2)) * RB + (((row0 >> 4) ^ ((i >> 2) + 4 * (h & 1))) << 5) + (i & 3) * 8);
-        return (uint32_t)(4 * h * RB + (((row0 >> 4) ^ h) << 6) + i * 4);
+        if (!MC) return {(uint32_t)((row0 + i) * 128 + ((h ^ ((i >> 1) & 7)) * 16)), 0};
+        if (PAD) {
+            const uint32_t odd = (i >> 2) & 1, x = (4 * h + (i >> 3)) * PIECE + odd * RB + row0 * 2 + (i & 3) * 8;
+            return {x + odd * 64, x - odd * 64};
+        }
+        if (sizeof(T) == 2) return {(uint32_t)((8 * h + (i >> 2)) * RB + (((row0 >> 4) ^ ((i >> 2) + 4 * (h & 1))) << 5) + (i & 3) * 8), 0};
+        return {(uint32_t)(4 * h * RB + (((row0 >> 4) ^ h) << 6) + i * 4), 0};
     }
-    static __device__ __forceinline__ v4u read(const lds_char *lds, uint32_t at, int block, int kk)
+    static __device__ __forceinline__ v4u read(const lds_char *lds, const At &at, int block, int kk)
     {
         if (!MC) {   // chunk 4 kk + h
-            const lds_char *p = lds + ((at ^ (uint32_t)(kk * 64)) + block * 2048);
+            const lds_char *p = lds + ((at.x ^ (uint32_t)(kk * 64)) + block * 2048);
             return *(const __attribute__((address_space(3))) v4u *)p;
         }
         if (sizeof(T) == 2) {
             // ds_read_b64_tr_b16: of each sixteen lanes, lanes 4 r .. 4 r + 3 read row r of a 4 x 16 block, lane i gets column i
-            const lds_char *p = lds + ((at ^ (uint32_t)(block << 5)) + kk * 32 * RB);
+            const lds_char *p = PAD ? lds + (block & 2 ? at.y : at.x) + block * 32 + kk * 16 * PIECE : lds + ((at.x ^ (uint32_t)(block << 5)) + kk * 32 * RB);
             typedef __attribute__((address_space(3))) v4s *P;
             const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds_char *)p);
-            const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds_char *)(p + 4 * RB));
+            const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds_char *)(p + (PAD ? 2 * PIECE : 4 * RB)));
             return __builtin_bit_cast(v4u, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         }
-        const lds_char *p = lds + ((at ^ (uint32_t)(block << 6)) + kk * 16 * RB);
+        const lds_char *p = lds + ((at.x ^ (uint32_t)(block << 6)) + kk * 16 * RB);
         v4u v;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = *(const __attribute__((address_space(3))) uint32_t *)(p + j * RB);
@@ -287,6 +329,44 @@ __device__ __forceinline__ void arrived()
     __syncthreads();
 }
 
+// The order of a half stage's instructions.  First half: its TM rows of TN blocks (EACH matrix instructions a block) and the
+// reads of the second half's fragments, READS_B and READS_A instructions each, those of a row of A after the row whose
+// registers they can take.
+template <int READS_B, int READS_A, int TN, int TM, int EACH>
+__device__ __forceinline__ void order_first()
+{
+    constexpr int LDS = 0x100, MATRIX = 0x008;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        __builtin_amdgcn_sched_group_barrier(LDS, READS_B, 0);
+        __builtin_amdgcn_sched_group_barrier(MATRIX, EACH, 0);
+    }
+#pragma unroll
+    for (int i = 1; i < TM; ++i) {
+        __builtin_amdgcn_sched_group_barrier(LDS, READS_A, 0);
+        __builtin_amdgcn_sched_group_barrier(MATRIX, EACH * TN, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(LDS, READS_A, 0);
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Second half, from row FROM on: the loads from memory one for every three blocks (in a burst they hold up the waves that issue
+// them: 845 us for 8192 x 8192 x 8192 with two for every two, 800 so), and from the third block on the reads.
+template <int READS_B, int READS_A, int TN, int TM, int EACH, int FROM>
+__device__ __forceinline__ void order_second()
+{
+    constexpr int LDS = 0x100, MEMORY = 0x010, MATRIX = 0x008;
+    // those of all of B and of the rows that are past, then those of two rows of A after each row
+    constexpr int N = (TM - FROM) * TN, READS = READS_B * TN + READS_A * FROM, SOME = (READS + N / 2 - 1) / (N / 2);
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+        if (g < N / 2 && g * SOME < READS) __builtin_amdgcn_sched_group_barrier(LDS, SOME, 0);
+        if (g >= N / 2 && g % TN == 0) __builtin_amdgcn_sched_group_barrier(LDS, 2 * READS_A, 0);
+        if (g % 3 == 0) __builtin_amdgcn_sched_group_barrier(MEMORY, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(MATRIX, EACH, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // WM x WN waves, each TM x TN blocks of 16 x 16
 template <int WM_, int WN_, int TM_, int TN_>
 struct Shape {
@@ -296,14 +376,15 @@ typedef Shape<2, 4, 8, 4> Large;   // 256 x 256, 8 waves
 typedef Shape<2, 2, 4, 4> Small;   // 128 x 128, 4 waves
 
 template <class T, int P, int EPI, class S, bool DIRECT, bool SUMS>
-__global__ __launch_bounds__(S::NW * 64, S::NW == 8 ? 2 : 2) void product_kernel(const ProductArgs a)
+__global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs a)
 {
     constexpr bool PAIR = EPI == E_GATED;
     typedef Operand<T, S::BM, S::NW, P == P_GRAD, false> OpA;
     typedef Operand<T, S::BN, S::NW, P != P_FWD, PAIR> OpB;
     constexpr int COLS = PAIR ? S::BN / 2 : S::BN;
-    __shared__ __attribute__((aligned(1024))) char stage0[(S::BM + S::BN) * 128];
-    __shared__ __attribute__((aligned(1024))) char stage1[(S::BM + S::BN) * 128];
+    constexpr int A_BYTES = OpA::STAGE;
+    __shared__ __attribute__((aligned(1024))) char stage0[A_BYTES + OpB::STAGE];
+    __shared__ __attribute__((aligned(1024))) char stage1[A_BYTES + OpB::STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int tm, tn;
     tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
@@ -318,55 +399,105 @@ __global__ __launch_bounds__(S::NW * 64, S::NW == 8 ? 2 : 2) void product_kernel
     const int t0 = blockIdx.y * a.steps, t1 = min(all, t0 + a.steps);
 
     v4f acc[S::TM][S::TN] = {};
-    v4f sum[SUMS ? S::TM : 1] = {};
+    float sum[SUMS ? S::TM : 1] = {};   // the lane's part of A's sums over k
     const bool sums = SUMS && tn == 0 && wn == 0;
-    const uint32_t ra = OpA::start(wm * S::TM * 16, lane), rb = OpB::start(wn * S::TN * 16, lane);
+    const typename OpA::At ra = OpA::start(wm * S::TM * 16, lane);
+    const typename OpB::At rb = OpB::start(wn * S::TN * 16, lane);
 
-    auto fetch = [&](char *stage, int t) {
+    auto through_registers = [&](char *stage, int t) {
         const bool second = t >= per_seg;
         const int step = second ? t - per_seg : t;
         lds_char *l = (lds_char *)stage;
-        if constexpr (DIRECT) {
-            oa.fetch(l, second, step, a.K, wave);
-            ob.fetch(l + S::BM * 128, second, step, a.K, wave);
-        } else {
-            v4u va[OpA::Q], vb[OpB::Q];
-            oa.load(va, second, step, a.K, wave, lane);
-            ob.load(vb, second, step, a.K, wave, lane);
-            OpA::put(l, va, wave, lane);
-            OpB::put(l + S::BM * 128, vb, wave, lane);
-        }
+        v4u va[OpA::Q], vb[OpB::Q];
+        oa.load(va, second, step, a.K, wave, lane);
+        ob.load(vb, second, step, a.K, wave, lane);
+        OpA::put(l, va, wave, lane);
+        OpB::put(l + A_BYTES, vb, wave, lane);
     };
-    auto contract = [&](const char *stage) {
+    struct Half { v4u a[S::TM], b[S::TN]; };   // a wave's fragments of half a stage
+    auto read = [&](Half &f, const char *stage, int kk) {
         const lds_char *l = (const lds_char *)stage;
+        typename OpA::At pa = ra;
+        typename OpB::At pb = rb;
+        if (OpB::MC_ && !OpB::PAD) __asm__("" : "+v"(pa.x), "+v"(pb.x));   // the blocks' addresses are formed anew: the registers are the fragments'
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            v4u fb[S::TN], fa[S::TM];
+        for (int j = 0; j < S::TN; ++j) f.b[j] = OpB::read(l + A_BYTES, pb, j, kk);
 #pragma unroll
-            for (int j = 0; j < S::TN; ++j) fb[j] = OpB::read(l + S::BM * 128, rb, j, kk);
+        for (int i = 0; i < S::TM; ++i) f.a[i] = OpA::read(l, pa, i, kk);
+    };
+    auto multiply = [&](const Half &f, int from, int to) {
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i) fa[i] = OpA::read(l, ra, i, kk);
+        for (int i = 0; i < S::TM; ++i)
+            if (i >= from && i < to) {
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::TN; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j], T());
-            if (SUMS && sums)
-#pragma unroll
-                for (int i = 0; i < S::TM; ++i) sum[i] = mfma(ones<T>(), fa[i], sum[i], T());
-        }
+                for (int j = 0; j < S::TN; ++j) acc[i][j] = mfma(f.b[j], f.a[i], acc[i][j], T());
+                if (SUMS) sum[i] = add_all(f.a[i], sum[i], T());
+            }
     };
 
-    if (t0 < t1) {
-        fetch(stage0, t0);
+    if constexpr (DIRECT) {
+        // Two stages in LDS, and in registers the fragments of the half stage at work.  Each row of blocks (TN matrix
+        // instructions) is followed by the read of its next fragment, which can go where the last one was; the other operand's
+        // fragments, which every row needs, come beforehand and into registers of their own.  The loads from memory have a whole
+        // stage's time.
+        Half f0, f1;
+        typename OpA::Aim aim_a;
+        typename OpB::Aim aim_b;
+        auto prepare = [&](int t) {
+            const bool second = t >= per_seg;
+            aim_a = oa.aim(t < t1, second, second ? t - per_seg : t, a.K);
+            aim_b = ob.aim(t < t1, second, second ? t - per_seg : t, a.K);
+        };
+        auto fetch = [&](char *stage) {
+            oa.fetch((lds_char *)stage, aim_a, wave);
+            ob.fetch((lds_char *)stage + A_BYTES, aim_b, wave);
+        };
+        constexpr int EACH = sizeof(T) == 4 ? 4 : 1, AHEAD = 2;   // matrix instructions of a block; rows before the barrier
+        auto stage = [&](char *cur, char *next, int t) {
+            prepare(t + 2);
+            read(f1, cur, 1);
+            multiply(f0, 0, S::TM);
+            order_first<OpB::READS, OpA::READS, S::TN, S::TM, EACH>();
+            multiply(f1, 0, AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+            arrived();            // `next` has come, and every wave has read all of `cur`
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(cur);
+            read(f0, next, 0);
+            multiply(f1, AHEAD, S::TM);
+            order_second<OpB::READS, OpA::READS, S::TN, S::TM, EACH, AHEAD>();
+        };
+        prepare(t0);
+        fetch(stage0);
+        prepare(t0 + 1);
+        fetch(stage1);
         arrived();
+        read(f0, stage0, 0);
+        int t = t0;
+        for (; t < t1; t += 2) {   // a stage past the last one is zeros
+            stage(stage0, stage1, t);
+            stage(stage1, stage0, t + 1);
+        }
+        arrived();
+    } else {
+        Half f;
+        auto contract = [&](const char *stage) {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                read(f, stage, kk);
+                multiply(f, 0, S::TM);
+            }
+        };
+        through_registers(stage0, t0);
+        __syncthreads();
         int t = t0;
         for (; t + 1 < t1; t += 2) {
-            fetch(stage1, t + 1);
+            through_registers(stage1, t + 1);
             contract(stage0);
-            arrived();
-            if (t + 2 < t1) fetch(stage0, t + 2);
+            __syncthreads();
+            if (t + 2 < t1) through_registers(stage0, t + 2);
             contract(stage1);
-            arrived();
+            __syncthreads();
         }
         if (t < t1) contract(stage0);
         __syncthreads();
@@ -377,20 +508,41 @@ __global__ __launch_bounds__(S::NW * 64, S::NW == 8 ? 2 : 2) void product_kernel
     const int i16 = lane & 15, h = lane >> 4;
     const int64_t plane = (int64_t)a.M * a.N;
     const int row0 = m0 + wm * S::TM * 16;
-    if (SUMS && sums && h == 0)
+    if (SUMS && sums)
 #pragma unroll
         for (int i = 0; i < S::TM; ++i) {
             const int m = row0 + i * 16 + i16;
-            if (m < a.M) {
-                if (a.split > 1) a.ws[a.split * plane + (int64_t)blockIdx.y * a.M + m] = sum[i][0];
-                else finish_sum<T>(a.f, m, sum[i][0]);
+            float v = sum[i] + __shfl_xor(sum[i], 16);
+            v += __shfl_xor(v, 32);
+            if (h == 0 && m < a.M) {
+                if (a.split > 1) a.ws[a.split * plane + (int64_t)blockIdx.y * a.M + m] = v;
+                else finish_sum<T>(a.f, m, v);
             }
         }
     float *part = a.ws + blockIdx.y * plane * (PAIR ? 2 : 1);
     char *own = (wave < S::NW / 2 ? stage0 : stage1) + wave % (S::NW / 2) * 16384;
     constexpr int LANES = PAIR ? 4 : 8;   // of a row
     const int c = lane % LANES, n = n0 + wn * (PAIR ? 32 : 64) + c * 8;
+    static_assert(S::TN == 4, "a wave's 64 columns");
     auto unit = [&](int row, int u) { return reinterpret_cast<v4f *>(own + row * 256 + ((u ^ (row & 15)) << 4)); };
+    auto sums_of = [&](int r, float (&v)[8], float (&w)[8]) {
+        const v4f x = *unit(r, 2 * c), y = *unit(r, 2 * c + 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = x[j];
+            v[4 + j] = y[j];
+        }
+        if (PAIR) {
+            const v4f p = *unit(r, 8 + 2 * c), q = *unit(r, 9 + 2 * c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[j] = p[j];
+                w[4 + j] = q[j];
+            }
+        }
+    };
+    constexpr int STEP = 64 / LANES, TOGETHER = EPI == E_GATED ? 2 : 4;   // rows apart; rows whose reads go together
+    const bool whole = m0 + S::BM <= a.M && n0 + COLS <= a.N && a.split == 1;
 #pragma unroll
     for (int i0 = 0; i0 < S::TM; i0 += 4) {
 #pragma unroll
@@ -398,33 +550,74 @@ __global__ __launch_bounds__(S::NW * 64, S::NW == 8 ? 2 : 2) void product_kernel
 #pragma unroll
             for (int j = 0; j < 4; ++j)   // a pair's blocks alternate: those of the first matrix first
                 *unit(i * 16 + i16, (PAIR ? (j >> 1) + (j & 1) * 2 : j) * 4 + h) = acc[i0 + i][j];
+        const int first = row0 + i0 * 16;
+        if (whole) {
 #pragma unroll 1
-        for (int r = lane / LANES; r < 64; r += 64 / LANES) {
-            const int m = row0 + i0 * 16 + r;
-            if (m >= a.M || n >= a.N) break;
-            float v[8], w[8];
-            const v4f x = *unit(r, 2 * c), y = *unit(r, 2 * c + 1);
+            for (int r = lane / LANES; r < 64; r += STEP * TOGETHER) {
+                Beside<T, EPI> side[TOGETHER];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = x[j];
-                v[4 + j] = y[j];
-            }
-            if (PAIR) {
-                const v4f p = *unit(r, 8 + 2 * c), q = *unit(r, 9 + 2 * c);
+                for (int q = 0; q < TOGETHER; ++q) side[q].template get<true>(a.f, first + r + q * STEP, n, 8);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    w[j] = p[j];
-                    w[4 + j] = q[j];
+                for (int q = 0; q < TOGETHER; ++q) {
+                    float v[8], w[8];
+                    sums_of(r + q * STEP, v, w);
+                    finish8<T, EPI, true>(a.f, side[q], first + r + q * STEP, n, 8, v, w);
                 }
             }
-            if (a.split > 1) {
-                store8<float>(part, (int64_t)m * a.N + n, v, a.N - n);
-                if (PAIR) store8<float>(part, plane + (int64_t)m * a.N + n, w, a.N - n);
-            } else {
-                finish8<T, EPI>(a.f, m, n, a.N, v, w);
+        } else {
+#pragma unroll 1
+            for (int r = lane / LANES; r < 64; r += STEP) {
+                const int m = first + r;
+                if (m >= a.M || n >= a.N) break;
+                float v[8], w[8];
+                sums_of(r, v, w);
+                if (a.split > 1) {
+                    store8<float>(part, (int64_t)m * a.N + n, v, a.N - n);
+                    if (PAIR) store8<float>(part, plane + (int64_t)m * a.N + n, w, a.N - n);
+                } else {
+                    Beside<T, EPI> side;
+                    side.template get<false>(a.f, m, n, a.N - n);
+                    finish8<T, EPI, false>(a.f, side, m, n, a.N - n, v, w);
+                }
             }
         }
     }
+}
+
+// A's sums over k for a product in large tiles, whose registers have no room for them: a workgroup takes 256 columns of the
+// rows of one part, eight columns a thread, and leaves the part's sums in the workspace.
+template <class T>
+__global__ __launch_bounds__(256) void sum_parts_kernel(const ProductArgs a)
+{
+    __shared__ float share[8][256];
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, m = blockIdx.x * 256 + c * 8;
+    const int each = (a.K + kSumParts - 1) / kSumParts, from = blockIdx.y * each, to = min(a.K, from + each);
+    float v[8] = {};
+    if (m < a.M)
+        for (int k = from + r; k < to; k += 8) {
+            float x[8];
+            load8<T>(x, static_cast<const char *>(a.a[0]) + k * a.lda, m, a.M - m);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += x[j];
+        }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) share[r][c * 8 + j] = v[j];
+    __syncthreads();
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= a.M) return;
+    float s = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += share[q][threadIdx.x];
+    a.ws[(int64_t)blockIdx.y * a.M + n] = s;
+}
+template <class T>
+__global__ __launch_bounds__(256) void sum_join_kernel(const ProductArgs a)
+{
+    const int m = blockIdx.x * 256 + threadIdx.x;
+    if (m >= a.M) return;
+    float v = 0.f;
+    for (int p = 0; p < kSumParts; ++p) v += a.ws[(int64_t)p * a.M + m];
+    finish_sum<T>(a.f, m, v);
 }
 
 // The parts of a product whose k was split, added in order, and its epilogue.  A thread takes eight columns of one row.
@@ -449,7 +642,9 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs a, int sums
                 for (int j = 0; j < 8; ++j) w[j] += x[j];
             }
         }
-        finish8<T, EPI>(a.f, m, n, a.N, v, w);
+        Beside<T, EPI> side;
+        side.template get<false>(a.f, m, n, a.N - n);
+        finish8<T, EPI, false>(a.f, side, m, n, a.N - n, v, w);
     }
     if (EPI == E_STORE && sums && at < a.M) {
         float v = 0.f;
