@@ -1,4 +1,5 @@
-// Dropout by itself, and the first step of a layer's backward pass: one pass over memory, eight columns a thread.
+// Dropout by itself, the first step of a layer's backward pass, and copies to 16-byte rows: one pass over memory, eight columns
+// a thread.
 //
 // The mask is never stored: its numbers are computed again wherever it is needed.  A call of the generator is twenty 32 x 32
 // bit products for eight elements.
@@ -29,7 +30,22 @@ __global__ __launch_bounds__(256) void mask_kernel(const MaskArgs a, uint32_t ei
         }
     }
     if (a.drop.t) drop8(a.drop, (int)m, n, v);
-    store8<T>(a.y, m * a.ldy + n, v, left);
+    store8<T>(a.y, m * a.ldy + n, v, left + a.zeros);
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(const PackArgs a)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= a.groups) return;
+    int k = 0;
+    while (k + 1 < a.n && at >= a.m[k + 1].first) ++k;
+    const auto &m = a.m[k];
+    const uint32_t eights = ((uint32_t)m.cols + 7) / 8;
+    const int64_t in = at - m.first;
+    const int64_t row = a.groups >> 32 ? in / eights : (uint32_t)in / eights, n = (in - row * eights) * 8;
+    const auto v = get8<T>(m.x, row * m.ldx + n, (int)(m.cols - n));
+    *reinterpret_cast<typename Eight<T>::type *>(static_cast<T *>(m.y) + (row * eights * 8 + n)) = v;
 }
 
 template <class T>
@@ -46,6 +62,15 @@ hipError_t run(const MaskArgs &a, hipStream_t s)
 hipError_t launch_mask(int type, const MaskArgs &a, hipStream_t s)
 {
     return type == DN_F32 ? run<float>(a, s) : type == DN_F16 ? run<f16>(a, s) : run<bf16>(a, s);
+}
+
+hipError_t launch_pack(int type, const PackArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.groups + 255) / 256));
+    if (type == DN_F32) launch_kernel(pack_kernel<float>, grid, dim3(256), 0, s, a);
+    else if (type == DN_F16) launch_kernel(pack_kernel<f16>, grid, dim3(256), 0, s, a);
+    else launch_kernel(pack_kernel<bf16>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace dn

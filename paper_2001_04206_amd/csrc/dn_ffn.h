@@ -194,6 +194,7 @@ struct Finish {
     int64_t ldr = 0;
     const void *bias = nullptr, *bias2 = nullptr;
     void *sums = nullptr, *sums2 = nullptr;   // P_GRAD: alpha times A's sums over k, [M] (from m_split on: sums2)
+    int32_t zeros = 0;          // E_GATED, E_DGATED: columns of zeros that follow the results' rows, to a multiple of eight
     int64_t half = 0, half_y = 0;   // columns between G and U; between dG and dU
     int32_t m_split = 0x7fffffff;
     int32_t m_valid = 0x7fffffff;   // rows of either side of m_split that exist
@@ -206,6 +207,7 @@ struct Finish {
 struct ProductArgs {
     const void *a[2], *b[2];    // operands; the second ones: of the second segment of k, or (E_GATED) of the second matrix
     int64_t lda, ldb;           // bytes between stored rows
+    int32_t a_ext, b_ext;       // elements of a stored row that may be read: the row and zeros up to a multiple of 16 bytes
     int32_t M, N, K;            // K: of one segment
     int32_t segments;           // 1 or 2
     float *ws;                  // split > 1: partial sums [split][planes][M][N], then [split][M] of E_STORE's sums
@@ -214,18 +216,17 @@ struct ProductArgs {
     Finish f;
 };
 
+constexpr int kFewRows = 64;    // most rows of the kernel that stages nothing
 constexpr int kSumParts = 32;   // parts of k that a launch of its own adds A's columns in
 
 // How a product is run.  `ws_bytes`: workspace that it needs.
-enum ProductKernel : int { K_FEW, K_SMALL_ANY, K_SMALL, K_LARGE };
+enum ProductKernel : int { K_FEW, K_SMALL, K_LARGE };
 struct ProductPlan {
-    ProductKernel kernel = K_SMALL_ANY;
-    bool direct = false;
+    ProductKernel kernel = K_SMALL;
     int split = 1, steps = 0;
     size_t ws_bytes = 0;
 };
-// `direct`: operand pieces of 16 bytes lie at multiples of 16 bytes and inside or outside whole
-ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, int segments, bool direct, bool sums);
+ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, int segments, bool sums);
 hipError_t launch_product_f32(Product p, Epilogue e, const ProductPlan &plan, ProductArgs a, hipStream_t s);
 hipError_t launch_product_f16(Product p, Epilogue e, const ProductPlan &plan, ProductArgs a, hipStream_t s);
 hipError_t launch_product_bf16(Product p, Epilogue e, const ProductPlan &plan, ProductArgs a, hipStream_t s);
@@ -237,8 +238,17 @@ struct MaskArgs {
     void *y;
     int64_t ldx, ldz, ldy;
     int32_t rows, cols, act;
+    int32_t zeros;   // columns of zeros that follow Y's rows
     Dropout drop;
 };
+
+// Matrices whose rows do not lie at multiples of 16 bytes, or end between two, copied to where they do, zeros following.
+struct PackArgs {
+    struct { const void *x; void *y; int64_t ldx; int32_t rows, cols; int64_t first; } m[4];   // first: its first group of eight
+    int32_t n;
+    int64_t groups;
+};
+hipError_t launch_pack(int type, const PackArgs &a, hipStream_t s);
 hipError_t launch_mask(int type, const MaskArgs &a, hipStream_t s);
 
 // ---- norms ------------------------------------------------------------------------------------------------------

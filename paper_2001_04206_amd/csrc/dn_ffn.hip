@@ -70,15 +70,56 @@ dn_status workspace(size_t need, const void *ws, size_t bytes)
     if (!ws || (uintptr_t)ws % 256) return DN_ERR_INVALID_ARG;
     return bytes < need ? DN_ERR_SHAPE : DN_OK;
 }
+// Operands of tiles: those whose rows are not in sixteen-byte pieces are copied to the workspace, from `at` on.
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+size_t packed_bytes(int type, int64_t rows, int64_t cols) { return up256((size_t)rows * (size_t)(up8(cols) * size_of(type))); }
+struct Packer {
+    int type;
+    char *at;
+    PackArgs a{};
+    struct Rows {
+        const void *p;
+        int64_t ld;     // bytes
+        int32_t ext;    // elements of a row that may be read
+    };
+    Rows take(const void *p, int64_t ld, int64_t rows, int64_t cols, bool must = false)
+    {
+        if (!must && pieces(type, p, ld, cols)) return {p, ld * size_of(type), (int32_t)cols};
+        auto &m = a.m[a.n++];
+        m.x = p;
+        m.y = at;
+        m.ldx = ld;
+        m.rows = (int32_t)rows;
+        m.cols = (int32_t)cols;
+        m.first = a.groups;
+        a.groups += rows * (up8(cols) / 8);
+        at += packed_bytes(type, rows, cols);
+        return {m.y, up8(cols) * size_of(type), (int32_t)up8(cols)};
+    }
+    hipError_t run(hipStream_t s) const { return a.n ? launch_pack(type, a, s) : hipSuccess; }
+};
+void operand_a(ProductArgs &a, const Packer::Rows &r)
+{
+    a.a[0] = a.a[1] = r.p;
+    a.lda = r.ld;
+    a.a_ext = r.ext;
+}
+void operand_b(ProductArgs &a, const Packer::Rows &r)
+{
+    a.b[0] = a.b[1] = r.p;
+    a.ldb = r.ld;
+    a.b_ext = r.ext;
+}
+
 dn_status device(hipError_t e) { return e == hipSuccess ? DN_OK : DN_ERR_DEVICE; }
 
 // ---- dense layer -------------------------------------------------------------------------------------------------
 struct Linear {
     dn_linear_desc d;
     Dropout drop;
-    bool plain;          // delta is dY
-    int64_t ldd;         // between rows of delta
-    size_t delta = 0, part = 0, bytes = 0;   // backward workspace: delta, parts of a product
+    ProductPlan fwd, dx, dw;
+    size_t fwd_part = 0, fwd_bytes = 0;                  // workspace: parts of a product, packed operands
+    size_t delta = 0, bwd_part = 0, bwd_bytes = 0;       // delta, parts, packed operands
 };
 
 dn_status linear_of(const dn_linear_desc *d, Linear &l)
@@ -91,25 +132,16 @@ dn_status linear_of(const dn_linear_desc *d, Linear &l)
     if ((s = row_length(d->type, l.d.ldx, d->n_in)) != DN_OK || (s = row_length(d->type, l.d.ldw, d->n_in)) != DN_OK ||
         (s = row_length(d->type, l.d.ldr, d->n_out)) != DN_OK || (s = row_length(d->type, l.d.ldy, d->n_out)) != DN_OK)
         return s;
-    l.plain = d->act == DN_ACT_LINEAR && l.drop.t == 0;
-    l.ldd = l.plain ? l.d.ldy : ((int64_t)d->n_out + 7) / 8 * 8;
-    if (!l.plain) l.delta = up256((size_t)d->rows * (size_t)l.ldd * (size_t)size_of(d->type));
-    // parts: of whichever operands, at whichever alignment
-    for (int direct = 0; direct < 2; ++direct) {
-        const size_t x = plan_product(d->type, P_DELTA, E_STORE, d->rows, d->n_in, d->n_out, 1, direct, false).ws_bytes;
-        const size_t w = plan_product(d->type, P_GRAD, E_STORE, d->n_out, d->n_in, d->rows, 1, direct, true).ws_bytes;
-        l.part = l.part > x ? l.part : x;
-        l.part = l.part > w ? l.part : w;
-    }
-    l.bytes = l.delta + up256(l.part);
+    const size_t packed = packed_bytes(d->type, d->rows, d->n_in) + packed_bytes(d->type, d->n_out, d->n_in);
+    l.fwd = plan_product(d->type, P_FWD, E_LINEAR, d->rows, d->n_out, d->n_in, 1, false);
+    l.fwd_part = up256(l.fwd.ws_bytes);
+    l.fwd_bytes = l.fwd.kernel == K_FEW ? 0 : l.fwd_part + packed;
+    l.dx = plan_product(d->type, P_DELTA, E_STORE, d->rows, d->n_in, d->n_out, 1, false);
+    l.dw = plan_product(d->type, P_GRAD, E_STORE, d->n_out, d->n_in, d->rows, 1, true);
+    l.delta = packed_bytes(d->type, d->rows, d->n_out);
+    l.bwd_part = up256(l.dx.ws_bytes > l.dw.ws_bytes ? l.dx.ws_bytes : l.dw.ws_bytes);
+    l.bwd_bytes = l.delta + l.bwd_part + packed;
     return DN_OK;
-}
-size_t linear_forward_bytes(const Linear &l)
-{
-    const dn_linear_desc &d = l.d;
-    const size_t a = plan_product(d.type, P_FWD, E_LINEAR, d.rows, d.n_out, d.n_in, 1, false, false).ws_bytes;
-    const size_t b = plan_product(d.type, P_FWD, E_LINEAR, d.rows, d.n_out, d.n_in, 1, true, false).ws_bytes;
-    return up256(a > b ? a : b);
 }
 
 // ---- gated block ---------------------------------------------------------------------------------------------------
@@ -117,8 +149,9 @@ struct Gated {
     dn_ffn_desc d;
     Dropout drop;
     int64_t ldh;         // between rows of H; dU starts so many columns after dG
-    size_t h = 0, fwd_bytes = 0;
-    size_t dgu = 0, dz = 0, part = 0, bwd_bytes = 0;
+    ProductPlan up, down, dh, dx, dwgu, dwd;
+    size_t h = 0, fwd_part = 0, fwd_bytes = 0;                       // workspace: H, parts of a product, packed operands
+    size_t dgu = 0, dz = 0, bwd_part = 0, bwd_bytes = 0;             // H, dG and dU, dZ, parts, packed operands
 };
 
 dn_status gated_of(const dn_ffn_desc *d, Gated &g)
@@ -132,28 +165,23 @@ dn_status gated_of(const dn_ffn_desc *d, Gated &g)
         (s = row_length(d->type, g.d.ldy, d->d)) != DN_OK)
         return s;
     const int64_t e = size_of(d->type);
-    g.ldh = ((int64_t)d->f + 15) / 16 * 16;
+    g.ldh = up8(d->f);
     if (2 * g.ldh * e > kRowBytes) return DN_ERR_SHAPE;
     g.h = up256((size_t)d->rows * (size_t)(g.ldh * e));
-    size_t part = 0;
-    auto take = [&](Product p, Epilogue ep, int M, int N, int K, int segments, bool sums) {
-        for (int direct = 0; direct < 2; ++direct) {
-            const size_t n = plan_product(d->type, p, ep, M, N, K, segments, direct, sums).ws_bytes;
-            part = part > n ? part : n;
-        }
-    };
-    take(P_FWD, E_GATED, d->rows, d->f, d->d, 1, false);
-    take(P_FWD, E_LINEAR, d->rows, d->d, d->f, 1, false);
-    g.fwd_bytes = g.h + up256(part);
-    part = 0;
-    take(P_DELTA, E_DGATED, d->rows, d->f, d->d, 1, false);
-    take(P_DELTA, E_STORE, d->rows, d->d, d->f, 2, false);
-    take(P_GRAD, E_STORE, (int)(2 * g.ldh), d->d, d->rows, 1, true);
-    take(P_GRAD, E_STORE, d->d, d->f, d->rows, 1, true);
-    g.part = up256(part);
+    const size_t packed = packed_bytes(d->type, d->rows, d->d) + 2 * packed_bytes(d->type, d->f, d->d) + packed_bytes(d->type, d->d, d->f);
+    g.up = plan_product(d->type, P_FWD, E_GATED, d->rows, d->f, d->d, 1, false);
+    g.down = plan_product(d->type, P_FWD, E_LINEAR, d->rows, d->d, d->f, 1, false);
+    g.fwd_part = up256(g.up.ws_bytes > g.down.ws_bytes ? g.up.ws_bytes : g.down.ws_bytes);
+    g.fwd_bytes = g.h + (g.up.kernel == K_FEW ? 0 : g.fwd_part + packed);
+    g.dh = plan_product(d->type, P_DELTA, E_DGATED, d->rows, d->f, d->d, 1, false);
+    g.dx = plan_product(d->type, P_DELTA, E_STORE, d->rows, d->d, d->f, 2, false);
+    g.dwgu = plan_product(d->type, P_GRAD, E_STORE, (int)(2 * g.ldh), d->d, d->rows, 1, true);
+    g.dwd = plan_product(d->type, P_GRAD, E_STORE, d->d, d->f, d->rows, 1, true);
+    for (const ProductPlan *p : {&g.dh, &g.dx, &g.dwgu, &g.dwd}) g.bwd_part = g.bwd_part > p->ws_bytes ? g.bwd_part : p->ws_bytes;
+    g.bwd_part = up256(g.bwd_part);
     g.dgu = 2 * g.h;
-    g.dz = g.drop.t ? up256((size_t)d->rows * (size_t)(((int64_t)d->d + 7) / 8 * 8 * e)) : 0;
-    g.bwd_bytes = g.h + g.dgu + g.dz + g.part;
+    g.dz = packed_bytes(d->type, d->rows, d->d);
+    g.bwd_bytes = g.h + g.dgu + g.dz + g.bwd_part + packed;
     return DN_OK;
 }
 
@@ -178,32 +206,32 @@ dn_status norm_of(const dn_norm_desc *d, NormArgs &a)
 
 }  // namespace
 
-ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, int segments, bool direct, bool sums)
+ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, int segments, bool sums)
 {
     ProductPlan plan;
-    plan.direct = direct;
     const int bk = type == DN_F32 ? 32 : 64, steps = (K + bk - 1) / bk * segments;
     plan.steps = steps;
-    if (p == P_FWD && M <= 64) {
+    if (p == P_FWD && M <= kFewRows) {
         plan.kernel = K_FEW;
         return plan;
     }
-    auto tiles = [&](int64_t edge) { return (M + edge - 1) / edge * ((N + (e == E_GATED ? edge / 2 : edge) - 1) / (e == E_GATED ? edge / 2 : edge)); };
-    if (type != DN_F32 && direct && tiles(256) >= 192) {
+    const int planes = e == E_GATED ? 2 : 1;
+    auto tiles = [&](int64_t edge) { return (M + edge - 1) / edge * ((N + edge / planes - 1) / (edge / planes)); };
+    if (type != DN_F32 && tiles(256) >= 192) {
         plan.kernel = K_LARGE;
         if (sums) plan.ws_bytes = (size_t)kSumParts * (size_t)M * sizeof(float);
         return plan;
     }
-    plan.kernel = direct ? K_SMALL : K_SMALL_ANY;
-    // two workgroups of 128 x 128 fit a compute unit: split k until there are that many, at four steps at least
+    // Two workgroups of 128 x 128 fit a compute unit.  With fewer tiles than that k is split, at four steps a part at least,
+    // so that the last round of workgroups is as full as may be.
     const int64_t t = tiles(128);
-    int64_t split = (512 + t / 2) / t;
+    int64_t split = 512 / t;
     if (split > steps / 4) split = steps / 4;
     if (split > 1) {
         plan.steps = (int)((steps + split - 1) / split);
         plan.split = (steps + plan.steps - 1) / plan.steps;
     }
-    if (plan.split > 1) plan.ws_bytes = (size_t)plan.split * ((size_t)M * (size_t)N * (e == E_GATED ? 2 : 1) + (sums ? (size_t)M : 0)) * sizeof(float);
+    if (plan.split > 1) plan.ws_bytes = (size_t)plan.split * ((size_t)M * (size_t)N * planes + (sums ? (size_t)M : 0)) * sizeof(float);
     return plan;
 }
 
@@ -216,13 +244,13 @@ extern "C" {
 size_t dn_linear_forward_workspace_bytes(const dn_linear_desc *d)
 {
     Linear l;
-    return linear_of(d, l) == DN_OK ? linear_forward_bytes(l) : kBad;
+    return linear_of(d, l) == DN_OK ? l.fwd_bytes : kBad;
 }
 
 size_t dn_linear_backward_workspace_bytes(const dn_linear_desc *d)
 {
     Linear l;
-    return linear_of(d, l) == DN_OK ? l.bytes : kBad;
+    return linear_of(d, l) == DN_OK ? l.bwd_bytes : kBad;
 }
 
 dn_status dn_linear_forward(const dn_linear_desc *d, const void *X_dev, const void *W_dev, const void *bias_dev,
@@ -233,16 +261,23 @@ dn_status dn_linear_forward(const dn_linear_desc *d, const void *X_dev, const vo
     dn_status s = linear_of(d, l);
     if (s != DN_OK) return s;
     if (!X_dev || !W_dev || !Y_dev || !multiples(d->type, X_dev, W_dev, bias_dev, R_dev, Y_dev, Z_dev)) return DN_ERR_INVALID_ARG;
-    const int64_t e = size_of(d->type);
+    if ((s = workspace(l.fwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
+    const hipStream_t stream = (hipStream_t)hip_stream;
     ProductArgs a{};
-    a.a[0] = a.a[1] = X_dev;
-    a.b[0] = a.b[1] = W_dev;
-    a.lda = l.d.ldx * e;
-    a.ldb = l.d.ldw * e;
     a.M = d->rows;
     a.N = d->n_out;
     a.K = d->n_in;
     a.segments = 1;
+    a.ws = static_cast<float *>(workspace_dev);
+    if (l.fwd.kernel == K_FEW) {
+        operand_a(a, {X_dev, l.d.ldx * size_of(d->type), d->n_in});
+        operand_b(a, {W_dev, l.d.ldw * size_of(d->type), d->n_in});
+    } else {
+        Packer pack{d->type, static_cast<char *>(workspace_dev) + l.fwd_part};
+        operand_a(a, pack.take(X_dev, l.d.ldx, d->rows, d->n_in));
+        operand_b(a, pack.take(W_dev, l.d.ldw, d->n_out, d->n_in));
+        if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    }
     a.f.y = Y_dev;
     a.f.ldy = l.d.ldy;
     a.f.y2 = Z_dev;
@@ -252,11 +287,7 @@ dn_status dn_linear_forward(const dn_linear_desc *d, const void *X_dev, const vo
     a.f.bias = bias_dev;
     a.f.act = d->act;
     a.f.drop = l.drop;
-    const bool direct = pieces(d->type, X_dev, l.d.ldx, d->n_in) && pieces(d->type, W_dev, l.d.ldw, d->n_in);
-    const ProductPlan plan = plan_product(d->type, P_FWD, E_LINEAR, a.M, a.N, a.K, 1, direct, false);
-    if ((s = workspace(plan.ws_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
-    a.ws = static_cast<float *>(workspace_dev);
-    return device(launch_product(d->type, P_FWD, E_LINEAR, plan, a, (hipStream_t)hip_stream));
+    return device(launch_product(d->type, P_FWD, E_LINEAR, l.fwd, a, stream));
 }
 
 dn_status dn_linear_backward(const dn_linear_desc *d, const void *X_dev, const void *W_dev, const void *Z_dev,
@@ -268,63 +299,57 @@ dn_status dn_linear_backward(const dn_linear_desc *d, const void *X_dev, const v
     if (s != DN_OK) return s;
     if (!X_dev || !W_dev || !dY_dev || (!Z_dev && d->act != DN_ACT_LINEAR) || (dbias_dev && !dW_dev)) return DN_ERR_INVALID_ARG;
     if (!multiples(d->type, X_dev, W_dev, Z_dev, dY_dev, dX_dev) || !multiples(d->grad_type, dW_dev, dbias_dev)) return DN_ERR_INVALID_ARG;
-    if ((s = workspace(l.bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
+    if ((s = workspace(l.bwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const int64_t e = size_of(d->type);
-    const void *delta = dY_dev;
-    if (!l.plain) {
+    char *ws = static_cast<char *>(workspace_dev);
+    // delta, without dropout's scale, by which the products' sums are multiplied; dY itself where it is that and lies well
+    Packer::Rows delta{dY_dev, l.d.ldy * e, d->n_out};
+    if (d->act != DN_ACT_LINEAR || l.drop.t || !pieces(d->type, dY_dev, l.d.ldy, d->n_out)) {
+        const int64_t ld = up8(d->n_out);
         MaskArgs m{};
         m.x = dY_dev;
         m.z = Z_dev;
-        m.y = workspace_dev;
+        m.y = ws;
         m.ldx = l.d.ldy;
         m.ldz = d->n_out;
-        m.ldy = l.ldd;
+        m.ldy = ld;
         m.rows = d->rows;
         m.cols = d->n_out;
+        m.zeros = (int)(ld - d->n_out);
         m.act = d->act;
         m.drop = l.drop;
-        m.drop.scale = 1.f;   // the products' sums are multiplied by it
+        m.drop.scale = 1.f;
         if (launch_mask(d->type, m, stream) != hipSuccess) return DN_ERR_DEVICE;
-        delta = workspace_dev;
+        delta = {ws, ld * e, (int32_t)ld};
     }
-    float *part = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + l.delta);
-    const bool direct_x = pieces(d->type, X_dev, l.d.ldx, d->n_in), direct_d = pieces(d->type, delta, l.ldd, d->n_out);
+    Packer pack{d->type, ws + l.delta + l.bwd_part};
+    const Packer::Rows X = dW_dev ? pack.take(X_dev, l.d.ldx, d->rows, d->n_in) : Packer::Rows{};
+    const Packer::Rows W = dX_dev ? pack.take(W_dev, l.d.ldw, d->n_out, d->n_in) : Packer::Rows{};
+    if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    ProductArgs a{};
+    a.segments = 1;
+    a.ws = reinterpret_cast<float *>(ws + l.delta);
+    operand_a(a, delta);
+    a.N = d->n_in;
+    a.f.ldy = d->n_in;
     if (dX_dev) {
-        ProductArgs a{};
-        a.a[0] = a.a[1] = delta;
-        a.b[0] = a.b[1] = W_dev;
-        a.lda = l.ldd * e;
-        a.ldb = l.d.ldw * e;
+        operand_b(a, W);
         a.M = d->rows;
-        a.N = d->n_in;
         a.K = d->n_out;
-        a.segments = 1;
-        a.ws = part;
         a.f.y = dX_dev;
-        a.f.ldy = d->n_in;
         a.f.alpha = l.drop.scale;
-        const ProductPlan plan = plan_product(d->type, P_DELTA, E_STORE, a.M, a.N, a.K, 1, direct_d && pieces(d->type, W_dev, l.d.ldw, d->n_in), false);
-        if (launch_product(d->type, P_DELTA, E_STORE, plan, a, stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_product(d->type, P_DELTA, E_STORE, l.dx, a, stream) != hipSuccess) return DN_ERR_DEVICE;
     }
     if (dW_dev) {
-        ProductArgs a{};
-        a.a[0] = a.a[1] = delta;
-        a.b[0] = a.b[1] = X_dev;
-        a.lda = l.ldd * e;
-        a.ldb = l.d.ldx * e;
+        operand_b(a, X);
         a.M = d->n_out;
-        a.N = d->n_in;
         a.K = d->rows;
-        a.segments = 1;
-        a.ws = part;
         a.f.y = dW_dev;
-        a.f.ldy = d->n_in;
         a.f.sums = dbias_dev;
         a.f.f32_out = d->grad_type == DN_F32;
         a.f.alpha = l.drop.scale * d->grad_scale;
-        const ProductPlan plan = plan_product(d->type, P_GRAD, E_STORE, a.M, a.N, a.K, 1, direct_d && direct_x, dbias_dev != nullptr);
-        if (launch_product(d->type, P_GRAD, E_STORE, plan, a, stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_product(d->type, P_GRAD, E_STORE, l.dw, a, stream) != hipSuccess) return DN_ERR_DEVICE;
     }
     return DN_OK;
 }
@@ -353,47 +378,50 @@ dn_status dn_ffn_forward(const dn_ffn_desc *d, const void *X_dev, const void *Wg
     if ((s = workspace(g.fwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const int64_t e = size_of(d->type);
-    float *part = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + g.h);
-    ProductArgs a{};
-    a.a[0] = a.a[1] = X_dev;
-    a.b[0] = Wg_dev;
-    a.b[1] = Wu_dev;
-    a.lda = g.d.ldx * e;
-    a.ldb = d->d * e;
+    char *H = static_cast<char *>(workspace_dev);
+    ProductArgs a{}, b{};
+    if (g.up.kernel == K_FEW) {
+        operand_a(a, {X_dev, g.d.ldx * e, d->d});
+        operand_b(a, {Wg_dev, d->d * e, d->d});
+        a.b[1] = Wu_dev;
+        operand_b(b, {Wd_dev, d->f * e, d->f});
+    } else {
+        Packer pack{d->type, H + g.h + g.fwd_part};
+        operand_a(a, pack.take(X_dev, g.d.ldx, d->rows, d->d));
+        const bool both = !pieces(d->type, Wg_dev, d->d, d->d) || !pieces(d->type, Wu_dev, d->d, d->d);   // they share a stride
+        operand_b(a, pack.take(Wg_dev, d->d, d->f, d->d, both));
+        a.b[1] = pack.take(Wu_dev, d->d, d->f, d->d, both).p;
+        operand_b(b, pack.take(Wd_dev, d->f, d->d, d->f));
+        if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    }
     a.M = d->rows;
     a.N = d->f;
     a.K = d->d;
     a.segments = 1;
-    a.ws = part;
-    a.f.y = workspace_dev;
+    a.ws = reinterpret_cast<float *>(H + g.h);
+    a.f.y = H;
     a.f.ldy = g.ldh;
+    a.f.zeros = (int)(g.ldh - d->f);
     a.f.y2 = GU_dev;
     a.f.ldy2 = 2 * (int64_t)d->f;
     a.f.half = d->f;
     a.f.bias = bg_dev;
     a.f.bias2 = bu_dev;
     a.f.act = d->act;
-    const bool direct = pieces(d->type, X_dev, g.d.ldx, d->d) && pieces(d->type, Wg_dev, d->d, d->d) && pieces(d->type, Wu_dev, d->d, d->d);
-    ProductPlan plan = plan_product(d->type, P_FWD, E_GATED, a.M, a.N, a.K, 1, direct, false);
-    if (launch_product(d->type, P_FWD, E_GATED, plan, a, stream) != hipSuccess) return DN_ERR_DEVICE;
-    ProductArgs b{};
-    b.a[0] = b.a[1] = workspace_dev;
-    b.b[0] = b.b[1] = Wd_dev;
-    b.lda = g.ldh * e;
-    b.ldb = d->f * e;
+    if (launch_product(d->type, P_FWD, E_GATED, g.up, a, stream) != hipSuccess) return DN_ERR_DEVICE;
+    operand_a(b, {H, g.ldh * e, (int32_t)g.ldh});
     b.M = d->rows;
     b.N = d->d;
     b.K = d->f;
     b.segments = 1;
-    b.ws = part;
+    b.ws = a.ws;
     b.f.y = Y_dev;
     b.f.ldy = g.d.ldy;
     b.f.r = R_dev;
     b.f.ldr = g.d.ldr;
     b.f.bias = bd_dev;
     b.f.drop = g.drop;
-    plan = plan_product(d->type, P_FWD, E_LINEAR, b.M, b.N, b.K, 1, pieces(d->type, Wd_dev, d->f, d->f), false);
-    return device(launch_product(d->type, P_FWD, E_LINEAR, plan, b, stream));
+    return device(launch_product(d->type, P_FWD, E_LINEAR, g.down, b, stream));
 }
 
 dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
@@ -413,34 +441,37 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
     const int64_t e = size_of(d->type), f = d->f;
     char *ws = static_cast<char *>(workspace_dev);
     char *H = ws, *dG = H + g.h, *dU = dG + g.ldh * e;
-    float *part = reinterpret_cast<float *>(ws + g.h + g.dgu + g.dz);
-    const bool f32_out = d->grad_type == DN_F32;
-
-    // dZ without dropout's scale, by which the sums of the two products that read it are multiplied
-    const void *dZ = dY_dev;
-    int64_t ldz = g.d.ldy;
-    if (g.drop.t) {
+    // dZ without dropout's scale, by which the sums of the two products that read it are multiplied; dY itself where it is that
+    // and lies well
+    Packer::Rows dZ{dY_dev, g.d.ldy * e, d->d};
+    if (g.drop.t || !pieces(d->type, dY_dev, g.d.ldy, d->d)) {
+        const int64_t ld = up8(d->d);
         MaskArgs m{};
         m.x = dY_dev;
         m.y = ws + g.h + g.dgu;
         m.ldx = g.d.ldy;
-        m.ldy = ((int64_t)d->d + 7) / 8 * 8;
+        m.ldy = ld;
         m.rows = d->rows;
         m.cols = d->d;
+        m.zeros = (int)(ld - d->d);
         m.act = -1;
         m.drop = g.drop;
         m.drop.scale = 1.f;
         if (launch_mask(d->type, m, stream) != hipSuccess) return DN_ERR_DEVICE;
-        dZ = m.y;
-        ldz = m.ldy;
+        dZ = {m.y, ld * e, (int32_t)ld};
     }
-    const bool direct_z = pieces(d->type, dZ, ldz, d->d), direct_f = f * e % 16 == 0;
+    Packer pack{d->type, ws + g.h + g.dgu + g.dz + g.bwd_part};
+    const Packer::Rows X = pack.take(X_dev, g.d.ldx, d->rows, d->d), Wd = pack.take(Wd_dev, f, d->d, f);
+    const bool both = !pieces(d->type, Wg_dev, d->d, d->d) || !pieces(d->type, Wu_dev, d->d, d->d);   // they share a stride
+    const Packer::Rows Wg = dX_dev ? pack.take(Wg_dev, d->d, f, d->d, both) : Packer::Rows{};
+    const Packer::Rows Wu = dX_dev ? pack.take(Wu_dev, d->d, f, d->d, both) : Packer::Rows{};
+    if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    float *part = reinterpret_cast<float *>(ws + g.h + g.dgu + g.dz);
+    const bool f32_out = d->grad_type == DN_F32;
     {   // dH, and from it dG, dU and H
         ProductArgs a{};
-        a.a[0] = a.a[1] = dZ;
-        a.b[0] = a.b[1] = Wd_dev;
-        a.lda = ldz * e;
-        a.ldb = f * e;
+        operand_a(a, dZ);
+        operand_b(a, Wd);
         a.M = d->rows;
         a.N = d->f;
         a.K = d->d;
@@ -449,6 +480,7 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
         a.f.y = dG;
         a.f.ldy = 2 * g.ldh;
         a.f.half_y = g.ldh;
+        a.f.zeros = (int)(g.ldh - f);
         a.f.y2 = H;
         a.f.ldy2 = g.ldh;
         a.f.r = GU_dev;
@@ -456,17 +488,14 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
         a.f.half = f;
         a.f.act = d->act;
         a.f.alpha = g.drop.scale;
-        const ProductPlan plan = plan_product(d->type, P_DELTA, E_DGATED, a.M, a.N, a.K, 1, direct_z && pieces(d->type, Wd_dev, f, f), false);
-        if (launch_product(d->type, P_DELTA, E_DGATED, plan, a, stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_product(d->type, P_DELTA, E_DGATED, g.dh, a, stream) != hipSuccess) return DN_ERR_DEVICE;
     }
     if (dX_dev) {
         ProductArgs a{};
-        a.a[0] = dG;
+        operand_a(a, {dG, 2 * g.ldh * e, (int32_t)g.ldh});
         a.a[1] = dU;
-        a.b[0] = Wg_dev;
-        a.b[1] = Wu_dev;
-        a.lda = 2 * g.ldh * e;
-        a.ldb = d->d * e;
+        operand_b(a, Wg);
+        a.b[1] = Wu.p;
         a.M = d->rows;
         a.N = d->d;
         a.K = d->f;
@@ -474,16 +503,12 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
         a.ws = part;
         a.f.y = dX_dev;
         a.f.ldy = d->d;
-        const bool direct = direct_f && pieces(d->type, Wg_dev, d->d, d->d) && pieces(d->type, Wu_dev, d->d, d->d);
-        const ProductPlan plan = plan_product(d->type, P_DELTA, E_STORE, a.M, a.N, a.K, 2, direct, false);
-        if (launch_product(d->type, P_DELTA, E_STORE, plan, a, stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_product(d->type, P_DELTA, E_STORE, g.dx, a, stream) != hipSuccess) return DN_ERR_DEVICE;
     }
-    {   // dWg and dWu: the columns of dG, those up to ldh that no column of G has, and the columns of dU
+    {   // dWg and dWu: the columns of dG (and of the zeros up to ldh), then those of dU
         ProductArgs a{};
-        a.a[0] = a.a[1] = dG;
-        a.b[0] = a.b[1] = X_dev;
-        a.lda = 2 * g.ldh * e;
-        a.ldb = g.d.ldx * e;
+        operand_a(a, {dG, 2 * g.ldh * e, (int32_t)(2 * g.ldh)});
+        operand_b(a, X);
         a.M = (int)(2 * g.ldh);
         a.N = d->d;
         a.K = d->rows;
@@ -499,14 +524,11 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
         a.f.m_valid = d->f;
         a.f.f32_out = f32_out;
         a.f.alpha = d->grad_scale;
-        const ProductPlan plan = plan_product(d->type, P_GRAD, E_STORE, a.M, a.N, a.K, 1, pieces(d->type, X_dev, g.d.ldx, d->d), dbg_dev || dbu_dev);
-        if (launch_product(d->type, P_GRAD, E_STORE, plan, a, stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_product(d->type, P_GRAD, E_STORE, g.dwgu, a, stream) != hipSuccess) return DN_ERR_DEVICE;
     }
     ProductArgs a{};
-    a.a[0] = a.a[1] = dZ;
-    a.b[0] = a.b[1] = H;
-    a.lda = ldz * e;
-    a.ldb = g.ldh * e;
+    operand_a(a, dZ);
+    operand_b(a, {H, g.ldh * e, (int32_t)g.ldh});
     a.M = d->d;
     a.N = d->f;
     a.K = d->rows;
@@ -517,8 +539,7 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
     a.f.sums = dbd_dev;
     a.f.f32_out = f32_out;
     a.f.alpha = g.drop.scale * d->grad_scale;
-    const ProductPlan plan = plan_product(d->type, P_GRAD, E_STORE, a.M, a.N, a.K, 1, direct_z && direct_f, dbd_dev != nullptr);
-    return device(launch_product(d->type, P_GRAD, E_STORE, plan, a, stream));
+    return device(launch_product(d->type, P_GRAD, E_STORE, g.dwd, a, stream));
 }
 
 size_t dn_norm_backward_workspace_bytes(const dn_norm_desc *d)

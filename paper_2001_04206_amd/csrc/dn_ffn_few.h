@@ -7,17 +7,16 @@
 
 namespace dn {
 
-constexpr int kFewRows = 64;
 constexpr int kFewWaves = 8;
 
 // sixteen bytes of a row of which `left` elements exist from here on
-template <class T, bool DIRECT>
+template <class T, bool WHOLE>
 __device__ __forceinline__ v4u chunk(const T *p, int left)
 {
     constexpr int E = 16 / (int)sizeof(T);
-    typedef T Piece __attribute__((ext_vector_type(E), aligned(DIRECT ? 16 : sizeof(T))));
+    typedef T Piece __attribute__((ext_vector_type(E), aligned(WHOLE ? 16 : sizeof(T))));
     if (left >= E) return __builtin_bit_cast(v4u, *reinterpret_cast<const Piece *>(p));
-    if (DIRECT || left <= 0) return v4u{};
+    if (WHOLE || left <= 0) return v4u{};
     Piece x;
 #pragma unroll
     for (int j = 0; j < E; ++j) x[j] = j < left ? p[j] : (T)0.f;
@@ -25,7 +24,7 @@ __device__ __forceinline__ v4u chunk(const T *p, int left)
 }
 
 // MB: blocks of sixteen rows.  The matrix instructions work on sixteen rows at least; rows that do not exist repeat the last.
-template <class T, int EPI, int MB, bool DIRECT>
+template <class T, int EPI, int MB, bool WHOLE>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProductArgs a)
 {
     constexpr int PLANES = EPI == E_GATED ? 2 : 1, E = 16 / (int)sizeof(T), BK = 128 / (int)sizeof(T), AHEAD = MB == 1 ? 4 : 2;
@@ -48,9 +47,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProductArgs a
             for (int c = 0; c < 2; ++c) {
                 const int k = k0 + s * kFewWaves * BK + c * (BK / 2), left = a.K - k - h * E;
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) fw[s][c][p] = chunk<T, DIRECT>(w[p] + k, left);
+                for (int p = 0; p < PLANES; ++p) fw[s][c][p] = chunk<T, WHOLE>(w[p] + k, left);
 #pragma unroll
-                for (int b = 0; b < MB; ++b) fx[s][c][b] = chunk<T, DIRECT>(x[b] + k, left);
+                for (int b = 0; b < MB; ++b) fx[s][c][b] = chunk<T, WHOLE>(x[b] + k, left);
             }
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s)

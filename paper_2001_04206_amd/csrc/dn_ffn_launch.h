@@ -6,7 +6,7 @@
 namespace dn {
 namespace {
 
-template <class T, int P, int EPI, class S, bool DIRECT>
+template <class T, int P, int EPI, class S>
 hipError_t tiles(ProductArgs &a, bool sums, hipStream_t s)
 {
     a.tiles_m = (a.M + S::BM - 1) / S::BM;
@@ -15,22 +15,30 @@ hipError_t tiles(ProductArgs &a, bool sums, hipStream_t s)
     const dim3 grid((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split);
     if constexpr (P == P_GRAD && S::BM == 128) {
         if (sums) {
-            launch_kernel(product_kernel<T, P, EPI, S, DIRECT, true>, grid, dim3(S::NW * 64), 0, s, a);
+            launch_kernel(product_kernel<T, P, EPI, S, true>, grid, dim3(S::NW * 64), 0, s, a);
             return hipGetLastError();
         }
     }
-    launch_kernel(product_kernel<T, P, EPI, S, DIRECT, false>, grid, dim3(S::NW * 64), 0, s, a);
+    launch_kernel(product_kernel<T, P, EPI, S, false>, grid, dim3(S::NW * 64), 0, s, a);
     return hipGetLastError();
 }
 
-template <class T, int EPI, bool DIRECT>
-hipError_t few(const ProductArgs &a, hipStream_t s)
+template <class T, int EPI, bool WHOLE>
+hipError_t few_of(const ProductArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.N + 15) / 16)), block(kFewWaves * 64);
-    if (a.M <= 16) launch_kernel(few_kernel<T, EPI, 1, DIRECT>, grid, block, 0, s, a);
-    else if (a.M <= 32) launch_kernel(few_kernel<T, EPI, 2, DIRECT>, grid, block, 0, s, a);
-    else launch_kernel(few_kernel<T, EPI, 4, DIRECT>, grid, block, 0, s, a);
+    if (a.M <= 16) launch_kernel(few_kernel<T, EPI, 1, WHOLE>, grid, block, 0, s, a);
+    else if (a.M <= 32) launch_kernel(few_kernel<T, EPI, 2, WHOLE>, grid, block, 0, s, a);
+    else launch_kernel(few_kernel<T, EPI, 4, WHOLE>, grid, block, 0, s, a);
     return hipGetLastError();
+}
+
+template <class T, int EPI>
+hipError_t few(const ProductArgs &a, hipStream_t s)
+{
+    // whether all rows lie at multiples of 16 bytes and end at some
+    uintptr_t all = (uintptr_t)a.a[0] | (uintptr_t)a.b[0] | (uintptr_t)a.b[1] | (uintptr_t)a.lda | (uintptr_t)a.ldb | (uintptr_t)a.K * sizeof(T);
+    return all % 16 == 0 ? few_of<T, EPI, true>(a, s) : few_of<T, EPI, false>(a, s);
 }
 
 template <class T, int P, int EPI>
@@ -42,10 +50,9 @@ hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
     hipError_t e = hipErrorInvalidValue;
     switch (plan.kernel) {
     case K_FEW:
-        if constexpr (P == P_FWD) return plan.direct ? few<T, EPI, true>(a, s) : few<T, EPI, false>(a, s);
+        if constexpr (P == P_FWD) return few<T, EPI>(a, s);
         return hipErrorInvalidValue;
-    case K_SMALL_ANY: e = tiles<T, P, EPI, Small, false>(a, sums, s); break;
-    case K_SMALL: e = tiles<T, P, EPI, Small, true>(a, sums, s); break;
+    case K_SMALL: e = tiles<T, P, EPI, Small>(a, sums, s); break;
     case K_LARGE:
         if constexpr (sizeof(T) == 2) {
             if (P == P_GRAD && sums) {
@@ -53,7 +60,7 @@ hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
                 launch_kernel(sum_join_kernel<T>, dim3((unsigned)((a.M + 255) / 256)), dim3(256), 0, s, a);
                 if ((e = hipGetLastError()) != hipSuccess) return e;
             }
-            return tiles<T, P, EPI, Large, true>(a, sums, s);
+            return tiles<T, P, EPI, Large>(a, sums, s);
         }
         return hipErrorInvalidValue;
     }

@@ -114,8 +114,8 @@ __device__ __forceinline__ void finish8(const Finish &e, const Beside<T, EPI> &s
             store8<T, ALL>(e.y2, m * e.ldy2 + n + e.half, w, left);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = act_value<FAST>(e.act, v[j]) * w[j];
-        store8<T, ALL>(e.y, m * e.ldy + n, v, left);
+        for (int j = 0; j < 8; ++j) v[j] = !ALL && j >= left ? 0.f : act_value<FAST>(e.act, v[j]) * w[j];
+        store8<T, ALL>(e.y, m * e.ldy + n, v, left + e.zeros);
     } else if constexpr (EPI == E_DGATED) {
         float h[8];
 #pragma unroll
@@ -126,10 +126,11 @@ __device__ __forceinline__ void finish8(const Finish &e, const Beside<T, EPI> &s
             w[j] = v[j] * f;
             v[j] *= (float)side.u[j] * df;
             h[j] = (float)side.u[j] * f;
+            if (!ALL && j >= left) v[j] = w[j] = h[j] = 0.f;
         }
-        store8<T, ALL>(e.y, m * e.ldy + n, v, left);
-        store8<T, ALL>(e.y, m * e.ldy + n + e.half_y, w, left);
-        store8<T, ALL>(e.y2, m * e.ldy2 + n, h, left);
+        store8<T, ALL>(e.y, m * e.ldy + n, v, left + e.zeros);
+        store8<T, ALL>(e.y, m * e.ldy + n + e.half_y, w, left + e.zeros);
+        store8<T, ALL>(e.y2, m * e.ldy2 + n, h, left + e.zeros);
     } else {
         const int row = m < e.m_split ? m : m - e.m_split;
         if (row >= e.m_valid) return;
@@ -234,47 +235,6 @@ struct Operand {
                                                      (int)(HOP ? at.first + q * hop : offset(q)), 0, 0, 0);
     }
 
-    // the same through registers, for operands at any alignment and of any length
-    __device__ __forceinline__ void load(v4u (&v)[Q], bool second, int step, int K, int wave, int lane) const
-    {
-        constexpr int E = 16 / (int)sizeof(T);
-        const int k0 = step * BK, kleft = K - k0;
-        const char *b = (second ? next : base) + (MC ? (int64_t)k0 * ld : (int64_t)k0 * (int)sizeof(T));
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            int there, line, lines;   // elements of the chunk that exist; its row, and how many there are
-            if (MC) {
-                const int k = ((wave + q * NW) * 1024 + lane * 16) / RB;
-                there = rows - (int)((offset(q) - (uint32_t)(k * ld)) / sizeof(T));
-                line = k;
-                lines = kleft;
-            } else {
-                there = kleft - (int)(kbyte / sizeof(T));
-                const int r = 8 * (wave & 1) + (lane >> 3), block = (wave >> 1) + q * (NW / 2);
-                line = r + 16 * (PAIR ? block >> 1 : block);
-                lines = rows;
-            }
-            if (line >= lines) there = 0;
-            const T *p = reinterpret_cast<const T *>(b + offset(q));
-            typedef T Piece __attribute__((ext_vector_type(E), aligned(sizeof(T))));
-    
-            if (there >= E) {
-                v[q] = __builtin_bit_cast(v4u, *reinterpret_cast<const Piece *>(p));
-            } else {
-                Piece x;
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = j < there ? p[j] : (T)0.f;
-                v[q] = __builtin_bit_cast(v4u, x);
-            }
-        }
-    }
-    static __device__ __forceinline__ void put(lds_char *lds, const v4u (&v)[Q], int wave, int lane)
-    {
-#pragma unroll
-        for (int q = 0; q < Q; ++q)
-            *(__attribute__((address_space(3))) v4u *)(lds + (wave + q * NW) * PIECE + lane * 16) = v[q];
-    }
-
     // Fragments: sixteen rows from 16 block on, half kk (64 bytes of k) of the stage.  `at` from start(), block a constant
     // below the number of blocks that the wave's rows start at a multiple of.
     struct At { uint32_t x, y; };   // y: PAD, blocks whose bit 1 is set
@@ -349,19 +309,22 @@ __device__ __forceinline__ void order_first()
     __builtin_amdgcn_sched_group_barrier(LDS, READS_A, 0);
     __builtin_amdgcn_sched_barrier(0);
 }
-// Second half, from row FROM on: the loads from memory one for every three blocks (in a burst they hold up the waves that issue
-// them: 845 us for 8192 x 8192 x 8192 with two for every two, 800 so), and from the third block on the reads.
-template <int READS_B, int READS_A, int TN, int TM, int EACH, int FROM>
+// Second half, from row FROM on: the reads of the next stage's first fragments likewise, and the LOADS from memory evenly, one for
+// every three blocks of a large tile.  (In a burst they hold up the waves that issue them: two for every two blocks made 8192 x
+// 8192 x 8192 take 845 us instead of 800.  Without any loads the loop's matrix instructions are busy 95 % of its time, with them
+// 73 %.)
+template <int READS_B, int READS_A, int LOADS, int TN, int TM, int EACH, int FROM>
 __device__ __forceinline__ void order_second()
 {
     constexpr int LDS = 0x100, MEMORY = 0x010, MATRIX = 0x008;
     // those of all of B and of the rows that are past, then those of two rows of A after each row
     constexpr int N = (TM - FROM) * TN, READS = READS_B * TN + READS_A * FROM, SOME = (READS + N / 2 - 1) / (N / 2);
+    constexpr int THIRDS = (N + 2) / 3, TOGETHER = (LOADS + THIRDS - 1) / THIRDS;
 #pragma unroll
     for (int g = 0; g < N; ++g) {
         if (g < N / 2 && g * SOME < READS) __builtin_amdgcn_sched_group_barrier(LDS, SOME, 0);
         if (g >= N / 2 && g % TN == 0) __builtin_amdgcn_sched_group_barrier(LDS, 2 * READS_A, 0);
-        if (g % 3 == 0) __builtin_amdgcn_sched_group_barrier(MEMORY, 1, 0);
+        if (g % 3 == 0) __builtin_amdgcn_sched_group_barrier(MEMORY, TOGETHER, 0);
         __builtin_amdgcn_sched_group_barrier(MATRIX, EACH, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -375,7 +338,7 @@ struct Shape {
 typedef Shape<2, 4, 8, 4> Large;   // 256 x 256, 8 waves
 typedef Shape<2, 2, 4, 4> Small;   // 128 x 128, 4 waves
 
-template <class T, int P, int EPI, class S, bool DIRECT, bool SUMS>
+template <class T, int P, int EPI, class S, bool SUMS>
 __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs a)
 {
     constexpr bool PAIR = EPI == E_GATED;
@@ -393,8 +356,8 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
 
     OpA oa;
     OpB ob;
-    oa.init(a.a, a.lda, m0, a.M, wave, lane);
-    ob.init(a.b, a.ldb, n0, a.N, wave, lane);
+    oa.init(a.a, a.lda, m0, OpA::MC_ ? a.a_ext : a.M, wave, lane);
+    ob.init(a.b, a.ldb, n0, OpB::MC_ ? a.b_ext : a.N, wave, lane);
     const int per_seg = (a.K + OpA::BK - 1) / OpA::BK, all = per_seg * a.segments;
     const int t0 = blockIdx.y * a.steps, t1 = min(all, t0 + a.steps);
 
@@ -404,16 +367,6 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     const typename OpA::At ra = OpA::start(wm * S::TM * 16, lane);
     const typename OpB::At rb = OpB::start(wn * S::TN * 16, lane);
 
-    auto through_registers = [&](char *stage, int t) {
-        const bool second = t >= per_seg;
-        const int step = second ? t - per_seg : t;
-        lds_char *l = (lds_char *)stage;
-        v4u va[OpA::Q], vb[OpB::Q];
-        oa.load(va, second, step, a.K, wave, lane);
-        ob.load(vb, second, step, a.K, wave, lane);
-        OpA::put(l, va, wave, lane);
-        OpB::put(l + A_BYTES, vb, wave, lane);
-    };
     struct Half { v4u a[S::TM], b[S::TN]; };   // a wave's fragments of half a stage
     auto read = [&](Half &f, const char *stage, int kk) {
         const lds_char *l = (const lds_char *)stage;
@@ -435,73 +388,49 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             }
     };
 
-    if constexpr (DIRECT) {
-        // Two stages in LDS, and in registers the fragments of the half stage at work.  Each row of blocks (TN matrix
-        // instructions) is followed by the read of its next fragment, which can go where the last one was; the other operand's
-        // fragments, which every row needs, come beforehand and into registers of their own.  The loads from memory have a whole
-        // stage's time.
-        Half f0, f1;
-        typename OpA::Aim aim_a;
-        typename OpB::Aim aim_b;
-        auto prepare = [&](int t) {
-            const bool second = t >= per_seg;
-            aim_a = oa.aim(t < t1, second, second ? t - per_seg : t, a.K);
-            aim_b = ob.aim(t < t1, second, second ? t - per_seg : t, a.K);
-        };
-        auto fetch = [&](char *stage) {
-            oa.fetch((lds_char *)stage, aim_a, wave);
-            ob.fetch((lds_char *)stage + A_BYTES, aim_b, wave);
-        };
-        constexpr int EACH = sizeof(T) == 4 ? 4 : 1, AHEAD = 2;   // matrix instructions of a block; rows before the barrier
-        auto stage = [&](char *cur, char *next, int t) {
-            prepare(t + 2);
-            read(f1, cur, 1);
-            multiply(f0, 0, S::TM);
-            order_first<OpB::READS, OpA::READS, S::TN, S::TM, EACH>();
-            multiply(f1, 0, AHEAD);
-            __builtin_amdgcn_sched_barrier(0);
-            arrived();            // `next` has come, and every wave has read all of `cur`
-            __builtin_amdgcn_sched_barrier(0);
-            fetch(cur);
-            read(f0, next, 0);
-            multiply(f1, AHEAD, S::TM);
-            order_second<OpB::READS, OpA::READS, S::TN, S::TM, EACH, AHEAD>();
-        };
-        prepare(t0);
-        fetch(stage0);
-        prepare(t0 + 1);
-        fetch(stage1);
-        arrived();
-        read(f0, stage0, 0);
-        int t = t0;
-        for (; t < t1; t += 2) {   // a stage past the last one is zeros
-            stage(stage0, stage1, t);
-            stage(stage1, stage0, t + 1);
-        }
-        arrived();
-    } else {
-        Half f;
-        auto contract = [&](const char *stage) {
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                read(f, stage, kk);
-                multiply(f, 0, S::TM);
-            }
-        };
-        through_registers(stage0, t0);
-        __syncthreads();
-        int t = t0;
-        for (; t + 1 < t1; t += 2) {
-            through_registers(stage1, t + 1);
-            contract(stage0);
-            __syncthreads();
-            if (t + 2 < t1) through_registers(stage0, t + 2);
-            contract(stage1);
-            __syncthreads();
-        }
-        if (t < t1) contract(stage0);
-        __syncthreads();
+    // Two stages in LDS, and in registers the fragments of the half stage at work.  Each row of blocks (TN matrix
+    // instructions) is followed by the read of its next fragment, which can go where the last one was; the other operand's
+    // fragments, which every row needs, come beforehand and into registers of their own.  The loads from memory have a whole
+    // stage's time.
+    Half f0, f1;
+    typename OpA::Aim aim_a;
+    typename OpB::Aim aim_b;
+    auto prepare = [&](int t) {
+        const bool second = t >= per_seg;
+        aim_a = oa.aim(t < t1, second, second ? t - per_seg : t, OpA::MC_ ? a.K : a.a_ext);
+        aim_b = ob.aim(t < t1, second, second ? t - per_seg : t, OpB::MC_ ? a.K : a.b_ext);
+    };
+    auto fetch = [&](char *stage) {
+        oa.fetch((lds_char *)stage, aim_a, wave);
+        ob.fetch((lds_char *)stage + A_BYTES, aim_b, wave);
+    };
+    constexpr int EACH = sizeof(T) == 4 ? 4 : 1, AHEAD = 2;   // matrix instructions of a block; rows before the barrier
+    auto stage = [&](char *cur, char *next, int t) {
+        prepare(t + 2);
+        read(f1, cur, 1);
+        multiply(f0, 0, S::TM);
+        order_first<OpB::READS, OpA::READS, S::TN, S::TM, EACH>();
+        multiply(f1, 0, AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+        arrived();            // `next` has come, and every wave has read all of `cur`
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(cur);
+        read(f0, next, 0);
+        multiply(f1, AHEAD, S::TM);
+        order_second<OpB::READS, OpA::READS, OpA::Q + OpB::Q, S::TN, S::TM, EACH, AHEAD>();
+    };
+    prepare(t0);
+    fetch(stage0);
+    prepare(t0 + 1);
+    fetch(stage1);
+    arrived();
+    read(f0, stage0, 0);
+    int t = t0;
+    for (; t < t1; t += 2) {   // a stage past the last one is zeros
+        stage(stage0, stage1, t);
+        stage(stage1, stage0, t + 1);
     }
+    arrived();
 
     // Epilogue.  A wave turns its sums through its own 16 KB of LDS, sixty-four rows at a time, so that a lane gets eight
     // neighbouring columns of a row: rows of 256 bytes, their 16-byte units u at u ^ (row mod 16).

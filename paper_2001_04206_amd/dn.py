@@ -345,21 +345,26 @@ def dn_sgd_step(param, grad, velocity, lr: float, momentum: float):
 
 # ---- the residual feed-forward block -----------------------------------------------------------------------------
 
+_TYPES = {}
+
+
 def _type_of(t, what: str) -> int:
-    import torch
-    kinds = {torch.float32: DN_F32, torch.float16: DN_F16, torch.bfloat16: DN_BF16}
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in kinds:
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: DN_F32, torch.float16: DN_F16, torch.bfloat16: DN_BF16})
+    kind = _TYPES.get(getattr(t, "dtype", None))
+    if kind is None or not t.is_cuda:
         raise TypeError("%s must be a device tensor of float32, float16 or bfloat16" % what)
-    return kinds[t.dtype]
+    return kind
 
 
 def _matrix(t, like, rows: int, cols: int, what: str):
     """(pointer, elements between rows) of a matrix of `like`'s type and device; rows may lie apart."""
     if t is None:
         return None, 0
-    if t.dtype != like.dtype or t.device != like.device:
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise TypeError("%s must be a tensor of dtype %s on %s" % (what, like.dtype, like.device))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise TypeError("%s must have shape %s, not %s" % (what, (rows, cols), tuple(t.shape)))
     step, one = t.stride()
     if (one != 1 and cols > 1) or (step < cols and rows > 1):
@@ -371,7 +376,7 @@ def _dense(t, like, shape, what: str, dtype=None):
     """The pointer of a contiguous tensor of `like`'s type (or `dtype`) and device, None for None."""
     if t is None:
         return None
-    if t.dtype != (dtype or like.dtype) or t.device != like.device or not t.is_contiguous():
+    if t.dtype is not (dtype or like.dtype) or t.get_device() != like.get_device() or not t.is_contiguous():
         raise TypeError("%s must be a contiguous tensor of dtype %s on %s" % (what, dtype or like.dtype, like.device))
     if t.shape != shape:
         raise TypeError("%s must have shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
@@ -380,34 +385,50 @@ def _dense(t, like, shape, what: str, dtype=None):
 
 def _grad_type(grad, like):
     """Parameter gradients are of the tensors' own type or fp32."""
-    import torch
-    if grad is not None and grad.dtype == torch.float32:
-        return DN_F32, torch.float32
-    return _type_of(like, "X"), like.dtype
+    kind = _type_of(like, "X")
+    if grad is not None and _TYPES.get(grad.dtype) == DN_F32:
+        return DN_F32, grad.dtype
+    return kind, like.dtype
 
 
 def _workspace(need: int, workspace, like, where: str):
     """(the tensor, its pointer, its bytes); allocated here if the caller brings none."""
-    import torch
-    if need == C.c_size_t(-1).value:
+    if need == 0 and workspace is None:
+        return None, None, 0
+    if need == _REFUSED:
         return None, None, 0      # the call itself says what is wrong
+    import torch
     if workspace is None:
-        if need == 0:
-            return None, None, 0
         workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
     elif workspace.dtype != torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous uint8 tensor on %s" % (like.device,))
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
+_REFUSED = C.c_size_t(-1).value
+
+
+class _Here:
+    """In place of torch.cuda.device where the tensors' device is the current one."""
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        return False
+
+
+_HERE_ALREADY = _Here()
+
+
 def _on(like):
     import torch
-    return torch.cuda.device(like.device)
+    return _HERE_ALREADY if torch.cuda.current_device() == like.get_device() else torch.cuda.device(like.device)
 
 
 def _stream(like) -> int:
     import torch
-    return torch.cuda.current_stream(like.device).cuda_stream
+    return torch.cuda.current_stream(like.get_device()).cuda_stream
 
 
 def _two(t, what: str):
