@@ -215,23 +215,33 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
         plan.kernel = K_FEW;
         return plan;
     }
+    // Tiles of 256 x 256 or (always for fp32, where the instruction is the bound either way) of 128 x 128, and k in how many parts:
+    // whichever is expected to take less.  Microseconds a stage, a round of workgroups and bytes of parts, as measured: a stage of
+    // a large tile takes 1.5 us whether the chip is full or not, one of two small tiles on each compute unit 1.35 (fp32: 3.6), so
+    // that 2048 x 4096 x 1024 takes less on the 128 large tiles that it has than on 512 small ones, which fill the chip.
     const int planes = e == E_GATED ? 2 : 1;
-    auto tiles = [&](int64_t edge) { return (M + edge - 1) / edge * ((N + edge / planes - 1) / (edge / planes)); };
-    if (type != DN_F32 && tiles(256) >= 192) {
-        plan.kernel = K_LARGE;
-        if (sums) plan.ws_bytes = (size_t)kSumParts * (size_t)M * sizeof(float);
-        return plan;
+    double best = 1e300;
+    for (int large = type == DN_F32 ? 0 : 1; large >= 0; --large) {
+        const int64_t edge = large ? 256 : 128, cols = edge / planes, t = (M + edge - 1) / edge * ((N + cols - 1) / cols);
+        const int64_t room = large ? 256 : 512;
+        for (int split = 1; split <= 32 && split * 4 <= steps + 3; ++split) {
+            int each = (steps + split - 1) / split;
+            if (large) each = (each + 1) / 2 * 2;
+            const int parts = (steps + each - 1) / each;
+            const double rounds = (double)((t * parts + room - 1) / room);
+            double us = rounds * (each * (large ? 1.5 : type == DN_F32 ? 3.6 : 1.35) + (large ? 8 : 6));
+            if (parts > 1) us += 3 + 8e-6 * parts * planes * M * N / 4.5;
+            if (us < best) {
+                best = us;
+                plan.kernel = large ? K_LARGE : K_SMALL;
+                plan.split = parts;
+                plan.steps = each;
+            }
+        }
     }
-    // Two workgroups of 128 x 128 fit a compute unit.  With fewer tiles than that k is split, at four steps a part at least,
-    // so that the last round of workgroups is as full as may be.
-    const int64_t t = tiles(128);
-    int64_t split = 512 / t;
-    if (split > steps / 4) split = steps / 4;
-    if (split > 1) {
-        plan.steps = (int)((steps + split - 1) / split);
-        plan.split = (steps + plan.steps - 1) / plan.steps;
-    }
-    if (plan.split > 1) plan.ws_bytes = (size_t)plan.split * ((size_t)M * (size_t)N * planes + (sums ? (size_t)M : 0)) * sizeof(float);
+    if (plan.split > 1) plan.ws_bytes = (size_t)plan.split * (size_t)M * (size_t)N * planes * sizeof(float);
+    if (sums && plan.kernel == K_LARGE) plan.ws_bytes += (size_t)kSumParts * (size_t)M * sizeof(float);
+    else if (sums && plan.split > 1) plan.ws_bytes += (size_t)plan.split * (size_t)M * sizeof(float);
     return plan;
 }
 

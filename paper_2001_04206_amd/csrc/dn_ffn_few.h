@@ -1,5 +1,5 @@
 // Matrix products of few rows (at most 64): single tokens and short prompts.  All there is to do is to read the weights
-// once, so nothing is staged: a workgroup takes sixteen columns (rows of W), its waves every NW-th piece of 128 bytes of k,
+// once, so nothing is staged: a workgroup takes sixteen columns (rows of W), its waves every eighth piece of 128 bytes of k,
 // fragments come from memory in the lanes that multiply them, and the waves' sums meet in LDS.
 #pragma once
 
@@ -7,7 +7,6 @@
 
 namespace dn {
 
-constexpr int kFewWaves = 8;
 
 // sixteen bytes of a row of which `left` elements exist from here on
 template <class T, bool WHOLE>
@@ -23,6 +22,7 @@ __device__ __forceinline__ v4u chunk(const T *p, int left)
     return __builtin_bit_cast(v4u, x);
 }
 
+constexpr int kFewWaves = 8;
 // MB: blocks of sixteen rows.  The matrix instructions work on sixteen rows at least; rows that do not exist repeat the last.
 template <class T, int EPI, int MB, bool WHOLE>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProductArgs a)
@@ -56,9 +56,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProductArgs a
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p)
-#pragma unroll
-                    for (int b = 0; b < MB; ++b) acc[p][b] = mfma(fw[s][c][p], fx[s][c][b], acc[p][b], T());
+                for (int p = 0; p < PLANES; ++p) mfma_row<T, true>(fx[s][c], fw[s][c][p], acc[p]);
     }
 #pragma unroll
     for (int p = 0; p < PLANES; ++p)
@@ -84,6 +82,90 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProductArgs a
             }
         }
     finish8<T, EPI, false>(a.f, side, m, n, a.N - n, v, u);
+}
+
+// Up to four rows: single tokens.  Vector instructions suffice, so a wave reads whole rows of W, a kilobyte at a time, and every
+// line of memory is asked for once: four waves of two rows, eight columns a workgroup.  (The matrix instructions' layout asks for
+// sixteen rows, 64 bytes of each, in one load.)
+__device__ __forceinline__ float dot(const v4u &a, const v4u &b, float c, bf16)
+{
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t x = a[j], y = b[j];
+        c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2b, x), __builtin_bit_cast(v2b, y), c, false);
+    }
+    return c;
+}
+__device__ __forceinline__ float dot(const v4u &a, const v4u &b, float c, f16)
+{
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t x = a[j], y = b[j];
+        c = __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, x), __builtin_bit_cast(v2h, y), c, false);
+    }
+    return c;
+}
+__device__ __forceinline__ float dot(const v4u &a, const v4u &b, float c, float)
+{
+    const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = fmaf(x[j], y[j], c);
+    return c;
+}
+
+template <class T, int EPI, int M, bool WHOLE>
+__global__ __launch_bounds__(256) void token_kernel(const ProductArgs a)
+{
+    constexpr int PLANES = EPI == E_GATED ? 2 : 1, E = 16 / (int)sizeof(T), ROWS = 2 * PLANES, AHEAD = ROWS + M <= 4 ? 8 : 4;
+    __shared__ float share[PLANES][M][8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.x * 8;
+    const T *w[ROWS], *x[M];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+        w[r] = reinterpret_cast<const T *>(static_cast<const char *>(a.b[r / 2]) + min(n0 + wave * 2 + r % 2, a.N - 1) * a.ldb) + lane * E;
+#pragma unroll
+    for (int m = 0; m < M; ++m) x[m] = reinterpret_cast<const T *>(static_cast<const char *>(a.a[0]) + min(m, a.M - 1) * a.lda) + lane * E;
+    float acc[ROWS][M] = {};
+    for (int k0 = 0; k0 < a.K; k0 += 64 * E * AHEAD) {
+        v4u fw[AHEAD][ROWS], fx[AHEAD][M];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) {
+            const int k = k0 + s * 64 * E, left = a.K - k - lane * E;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) fw[s][r] = chunk<T, WHOLE>(w[r] + k, left);
+#pragma unroll
+            for (int m = 0; m < M; ++m) fx[s][m] = chunk<T, WHOLE>(x[m] + k, left);
+        }
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int m = 0; m < M; ++m) acc[r][m] = dot(fw[s][r], fx[s][m], acc[r][m], T());
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            float v = acc[r][m];
+#pragma unroll
+            for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+            if (lane == 0) share[r / 2][m][wave * 2 + r % 2] = v;
+        }
+    __syncthreads();
+    const int m = threadIdx.x;
+    if (m >= a.M || m >= M) return;
+    float v[8], u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[j] = share[0][m][j];
+        u[j] = share[PLANES - 1][m][j];
+    }
+    Beside<T, EPI> side;
+    side.template get<false>(a.f, m, n0, a.N - n0);
+    finish8<T, EPI, false>(a.f, side, m, n0, a.N - n0, v, u);
 }
 
 }  // namespace dn

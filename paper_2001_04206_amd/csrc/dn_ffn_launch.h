@@ -26,7 +26,14 @@ hipError_t tiles(ProductArgs &a, bool sums, hipStream_t s)
 template <class T, int EPI, bool WHOLE>
 hipError_t few_of(const ProductArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.N + 15) / 16)), block(kFewWaves * 64);
+    if (a.M <= 4) {
+        const dim3 grid((unsigned)((a.N + 7) / 8)), block(256);
+        if (a.M == 1) launch_kernel(token_kernel<T, EPI, 1, WHOLE>, grid, block, 0, s, a);
+        else if (a.M == 2) launch_kernel(token_kernel<T, EPI, 2, WHOLE>, grid, block, 0, s, a);
+        else launch_kernel(token_kernel<T, EPI, 4, WHOLE>, grid, block, 0, s, a);
+        return hipGetLastError();
+    }
+    const dim3 grid((unsigned)((a.N + 15) / 16)), block(512);
     if (a.M <= 16) launch_kernel(few_kernel<T, EPI, 1, WHOLE>, grid, block, 0, s, a);
     else if (a.M <= 32) launch_kernel(few_kernel<T, EPI, 2, WHOLE>, grid, block, 0, s, a);
     else launch_kernel(few_kernel<T, EPI, 4, WHOLE>, grid, block, 0, s, a);
@@ -44,7 +51,7 @@ hipError_t few(const ProductArgs &a, hipStream_t s)
 template <class T, int P, int EPI>
 hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
 {
-    const bool sums = a.f.sums || a.f.sums2;
+    bool sums = a.f.sums || a.f.sums2;
     a.split = plan.split;
     a.steps = plan.steps;
     hipError_t e = hipErrorInvalidValue;
@@ -56,13 +63,16 @@ hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
     case K_LARGE:
         if constexpr (sizeof(T) == 2) {
             if (P == P_GRAD && sums) {
-                launch_kernel(sum_parts_kernel<T>, dim3((unsigned)((a.M + 255) / 256), kSumParts), dim3(256), 0, s, a);
-                launch_kernel(sum_join_kernel<T>, dim3((unsigned)((a.M + 255) / 256)), dim3(256), 0, s, a);
+                ProductArgs b = a;
+                if (a.split > 1) b.ws += (int64_t)a.split * a.M * a.N;
+                launch_kernel(sum_parts_kernel<T>, dim3((unsigned)((a.M + 255) / 256), kSumParts), dim3(256), 0, s, b);
+                launch_kernel(sum_join_kernel<T>, dim3((unsigned)((a.M + 255) / 256)), dim3(256), 0, s, b);
                 if ((e = hipGetLastError()) != hipSuccess) return e;
+                sums = false;
             }
-            return tiles<T, P, EPI, Large>(a, sums, s);
+            e = tiles<T, P, EPI, Large>(a, false, s);
         }
-        return hipErrorInvalidValue;
+        break;
     }
     if (e != hipSuccess || a.split == 1) return e;
     const int64_t work = (int64_t)a.M * ((a.N + 7) / 8);

@@ -23,12 +23,24 @@ __device__ __forceinline__ v4f mfma(const v4u &a, const v4u &b, v4f c, f16)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ v4f mfma(const v4u &a, const v4u &b, v4f c, float)
+// a row of N blocks: their products with one fragment.  fp32's four instructions a block go round the blocks: one that adds to
+// the sums of the one before would wait for it.  SECOND: the blocks' fragments are the second operand.
+template <class T, bool SECOND, int N>
+__device__ __forceinline__ void mfma_row(const v4u (&b)[N], const v4u &a, v4f (&c)[N])
 {
-    const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
+    if constexpr (sizeof(T) == 4) {
+        const v4f y = __builtin_bit_cast(v4f, a);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
-    return c;
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const v4f x = __builtin_bit_cast(v4f, b[j]);
+                c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(SECOND ? y[q] : x[q], SECOND ? x[q] : y[q], c[j], 0, 0, 0);
+            }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) c[j] = SECOND ? mfma(a, b[j], c[j], T()) : mfma(b[j], a, c[j], T());
+    }
 }
 // c plus the sum of a fragment's elements
 __device__ __forceinline__ float add_all(const v4u &a, float c, bf16)
@@ -382,8 +394,7 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
 #pragma unroll
         for (int i = 0; i < S::TM; ++i)
             if (i >= from && i < to) {
-#pragma unroll
-                for (int j = 0; j < S::TN; ++j) acc[i][j] = mfma(f.b[j], f.a[i], acc[i][j], T());
+                mfma_row<T, false>(f.b, f.a[i], acc[i]);
                 if (SUMS) sum[i] = add_all(f.a[i], sum[i], T());
             }
     };
@@ -426,9 +437,15 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     arrived();
     read(f0, stage0, 0);
     int t = t0;
-    for (; t < t1; t += 2) {   // a stage past the last one is zeros
+    // Large tiles: a stage past the last one is zeros.  (A loop's tail of its own costs registers that they do not have.)
+    for (; t + (S::NW == 8 ? 0 : 1) < t1; t += 2) {
         stage(stage0, stage1, t);
         stage(stage1, stage0, t + 1);
+    }
+    if (S::NW == 4 && t < t1) {
+        read(f1, stage0, 1);
+        multiply(f0, 0, S::TM);
+        multiply(f1, 0, S::TM);
     }
     arrived();
 
