@@ -221,19 +221,20 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
     // that 2048 x 4096 x 1024 takes less on the 128 large tiles that it has than on 512 small ones, which fill the chip.
     const int planes = e == E_GATED ? 2 : 1;
     double best = 1e300;
-    for (int large = type == DN_F32 ? 0 : 1; large >= 0; --large) {
-        const int64_t edge = large ? 256 : 128, cols = edge / planes, t = (M + edge - 1) / edge * ((N + cols - 1) / cols);
-        const int64_t room = large ? 256 : 512;
+    struct Way { ProductKernel kernel; int rows, cols, room; double stage, round; };
+    const Way small{K_SMALL, 128, 128, 512, 3.6, 6}, medium{K_MEDIUM, 128, 256, 256, 0.8, 6}, large{K_LARGE, 256, 256, 256, 1.5, 8};
+    for (const Way &w : {large, medium, small}) {
+        if ((w.kernel == K_SMALL) != (type == DN_F32)) continue;
+        const int64_t cols = w.cols / planes, t = (M + w.rows - 1) / w.rows * ((N + cols - 1) / cols);
         for (int split = 1; split <= 32 && split * 4 <= steps + 3; ++split) {
             int each = (steps + split - 1) / split;
-            if (large) each = (each + 1) / 2 * 2;
+            if (w.kernel == K_LARGE) each = (each + 1) / 2 * 2;
             const int parts = (steps + each - 1) / each;
-            const double rounds = (double)((t * parts + room - 1) / room);
-            double us = rounds * (each * (large ? 1.5 : type == DN_F32 ? 3.6 : 1.35) + (large ? 8 : 6));
+            double us = (double)((t * parts + w.room - 1) / w.room) * (each * w.stage + w.round);
             if (parts > 1) us += 3 + 8e-6 * parts * planes * M * N / 4.5;
             if (us < best) {
                 best = us;
-                plan.kernel = large ? K_LARGE : K_SMALL;
+                plan.kernel = w.kernel;
                 plan.split = parts;
                 plan.steps = each;
             }

@@ -13,7 +13,7 @@ hipError_t tiles(ProductArgs &a, bool sums, hipStream_t s)
     const int cols = EPI == E_GATED ? S::BN / 2 : S::BN;
     a.tiles_n = (a.N + cols - 1) / cols;
     const dim3 grid((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split);
-    if constexpr (P == P_GRAD && S::BM == 128) {
+    if constexpr (P == P_GRAD && S::TM != 8) {
         if (sums) {
             launch_kernel(product_kernel<T, P, EPI, S, true>, grid, dim3(S::NW * 64), 0, s, a);
             return hipGetLastError();
@@ -59,7 +59,12 @@ hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
     case K_FEW:
         if constexpr (P == P_FWD) return few<T, EPI>(a, s);
         return hipErrorInvalidValue;
-    case K_SMALL: e = tiles<T, P, EPI, Small>(a, sums, s); break;
+    case K_SMALL:
+        if constexpr (sizeof(T) == 4) e = tiles<T, P, EPI, Small>(a, sums, s);
+        break;
+    case K_MEDIUM:
+        if constexpr (sizeof(T) == 2) e = tiles<T, P, EPI, Medium>(a, sums, s);
+        break;
     case K_LARGE:
         if constexpr (sizeof(T) == 2) {
             if (P == P_GRAD && sums) {

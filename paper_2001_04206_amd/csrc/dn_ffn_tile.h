@@ -294,11 +294,14 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int &tm
     tn = in / high;
 }
 
-// every wave's loads into LDS are there, and every wave is done with what it read
+// All but the wave's last LATER loads into LDS are there, and every wave is done with what it read and has come here.
+template <int LATER>
 __device__ __forceinline__ void arrived()
 {
-    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    static_assert(LATER < 64, "the counter has six bits");
+    __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
+    __builtin_amdgcn_s_barrier();
+    __asm__ volatile("" ::: "memory");
 }
 
 // The order of a half stage's instructions.  First half: its TM rows of TN blocks (EACH matrix instructions a block) and the
@@ -342,13 +345,14 @@ __device__ __forceinline__ void order_second()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// WM x WN waves, each TM x TN blocks of 16 x 16
-template <int WM_, int WN_, int TM_, int TN_>
+// WM x WN waves, each TM x TN blocks of 16 x 16; NB stages in LDS
+template <int WM_, int WN_, int TM_, int TN_, int NB_>
 struct Shape {
-    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NB = NB_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
 };
-typedef Shape<2, 4, 8, 4> Large;   // 256 x 256, 8 waves
-typedef Shape<2, 2, 4, 4> Small;   // 128 x 128, 4 waves
+typedef Shape<2, 4, 8, 4, 2> Large;    // 256 x 256, 8 waves
+typedef Shape<2, 4, 4, 4, 3> Medium;   // 128 x 256, 8 waves; the third stage makes up for the shorter time of one
+typedef Shape<2, 2, 4, 4, 2> Small;    // 128 x 128, 4 waves, two workgroups a compute unit
 
 template <class T, int P, int EPI, class S, bool SUMS>
 __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs a)
@@ -358,8 +362,10 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     typedef Operand<T, S::BN, S::NW, P != P_FWD, PAIR> OpB;
     constexpr int COLS = PAIR ? S::BN / 2 : S::BN;
     constexpr int A_BYTES = OpA::STAGE;
+    constexpr int LOADS = OpA::Q + OpB::Q;   // of a wave and stage
     __shared__ __attribute__((aligned(1024))) char stage0[A_BYTES + OpB::STAGE];
     __shared__ __attribute__((aligned(1024))) char stage1[A_BYTES + OpB::STAGE];
+    __shared__ __attribute__((aligned(1024))) char stage2[S::NB == 3 ? A_BYTES + OpB::STAGE : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int tm, tn;
     tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
@@ -399,10 +405,10 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             }
     };
 
-    // Two stages in LDS, and in registers the fragments of the half stage at work.  Each row of blocks (TN matrix
+    // NB stages in LDS, and in registers the fragments of the half stage at work.  Each row of blocks (TN matrix
     // instructions) is followed by the read of its next fragment, which can go where the last one was; the other operand's
-    // fragments, which every row needs, come beforehand and into registers of their own.  The loads from memory have a whole
-    // stage's time.
+    // fragments, which every row needs, come beforehand and into registers of their own.  The loads from memory have the time of
+    // NB - 1 stages.
     Half f0, f1;
     typename OpA::Aim aim_a;
     typename OpB::Aim aim_b;
@@ -415,39 +421,49 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
         oa.fetch((lds_char *)stage, aim_a, wave);
         ob.fetch((lds_char *)stage + A_BYTES, aim_b, wave);
     };
-    constexpr int EACH = sizeof(T) == 4 ? 4 : 1, AHEAD = 2;   // matrix instructions of a block; rows before the barrier
+    constexpr int EACH = sizeof(T) == 4 ? 4 : 1, AHEAD = S::TM == 8 ? 2 : 0;   // matrix instructions of a block; rows before the barrier
     auto stage = [&](char *cur, char *next, int t) {
-        prepare(t + 2);
+        prepare(t + S::NB);
         read(f1, cur, 1);
         multiply(f0, 0, S::TM);
         order_first<OpB::READS, OpA::READS, S::TN, S::TM, EACH>();
         multiply(f1, 0, AHEAD);
         __builtin_amdgcn_sched_barrier(0);
-        arrived();            // `next` has come, and every wave has read all of `cur`
+        arrived<(S::NB - 2) * LOADS>();   // `next` has come, and every wave has read all of `cur`
         __builtin_amdgcn_sched_barrier(0);
         fetch(cur);
         read(f0, next, 0);
         multiply(f1, AHEAD, S::TM);
-        order_second<OpB::READS, OpA::READS, OpA::Q + OpB::Q, S::TN, S::TM, EACH, AHEAD>();
+        order_second<OpB::READS, OpA::READS, LOADS, S::TN, S::TM, EACH, AHEAD>();
     };
     prepare(t0);
     fetch(stage0);
     prepare(t0 + 1);
     fetch(stage1);
-    arrived();
+    if (S::NB == 3) {
+        prepare(t0 + 2);
+        fetch(stage2);
+    }
+    arrived<(S::NB - 1) * LOADS>();
     read(f0, stage0, 0);
     int t = t0;
-    // Large tiles: a stage past the last one is zeros.  (A loop's tail of its own costs registers that they do not have.)
-    for (; t + (S::NW == 8 ? 0 : 1) < t1; t += 2) {
-        stage(stage0, stage1, t);
-        stage(stage1, stage0, t + 1);
+    if constexpr (S::NB == 3) {
+        for (; t + 2 < t1; t += 3) {
+            stage(stage0, stage1, t);
+            stage(stage1, stage2, t + 1);
+            stage(stage2, stage0, t + 2);
+        }
+        if (t < t1) stage(stage0, stage1, t);
+        if (t + 1 < t1) stage(stage1, stage2, t + 1);
+    } else {
+        // Large tiles: a stage past the last one is zeros.  (A loop's tail of its own costs registers that they do not have.)
+        for (; t + (S::TM == 8 ? 0 : 1) < t1; t += 2) {
+            stage(stage0, stage1, t);
+            stage(stage1, stage0, t + 1);
+        }
+        if (S::TM != 8 && t < t1) stage(stage0, stage1, t);
     }
-    if (S::NW == 4 && t < t1) {
-        read(f1, stage0, 1);
-        multiply(f0, 0, S::TM);
-        multiply(f1, 0, S::TM);
-    }
-    arrived();
+    arrived<0>();
 
     // Epilogue.  A wave turns its sums through its own 16 KB of LDS, sixty-four rows at a time, so that a lane gets eight
     // neighbouring columns of a row: rows of 256 bytes, their 16-byte units u at u ^ (row mod 16).
@@ -466,7 +482,9 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             }
         }
     float *part = a.ws + blockIdx.y * plane * (PAIR ? 2 : 1);
-    char *own = (wave < S::NW / 2 ? stage0 : stage1) + wave % (S::NW / 2) * 16384;
+    constexpr int EACH_STAGE = (S::NW + S::NB - 1) / S::NB;   // waves
+    static_assert(EACH_STAGE * 16384 <= A_BYTES + OpB::STAGE, "a wave's 16 KB");
+    char *own = (wave < EACH_STAGE ? stage0 : wave < 2 * EACH_STAGE ? stage1 : stage2) + wave % EACH_STAGE * 16384;
     constexpr int LANES = PAIR ? 4 : 8;   // of a row
     const int c = lane % LANES, n = n0 + wn * (PAIR ? 32 : 64) + c * 8;
     static_assert(S::TN == 4, "a wave's 64 columns");
