@@ -10,6 +10,7 @@
 // normalised row and norm'(q) = r (q w - mean(q w) - ^ mean(q w ^)) (the first mean: layer norm only).  A workgroup takes a
 // run of rows and keeps its sums in registers; a second launch adds the parts of all workgroups in order.
 #include "dn_ffn.h"
+#include "dn_wave.h"
 
 namespace dn {
 namespace {
@@ -23,17 +24,17 @@ struct RowSum {
     int turn = 0;
     __device__ __forceinline__ v2f operator()(v2f v)
     {
-#pragma unroll
-        for (int o = 32; o; o >>= 1) {
-            v[0] += __shfl_xor(v[0], o);
-            v[1] += __shfl_xor(v[1], o);
-        }
+        v[0] = wave_sum(v[0]);
+        v[1] = wave_sum(v[1]);
         if (NT == 64) return v;
         // two sets of slots in turn: whoever writes one again has passed the barrier that its readers came to afterwards
         v2f *s = slots + turn * (NT / 64);
         turn ^= 1;
         if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-        __syncthreads();
+        // a barrier that leaves the next row's loads under way
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __asm__ volatile("" ::: "memory");
         v = s[0];
 #pragma unroll
         for (int w = 1; w < NT / 64; ++w) v += s[w];
@@ -41,15 +42,36 @@ struct RowSum {
     }
 };
 
+// A thread's C pieces of a row, as they lie in memory.
 template <class T, int NT, int C>
-__device__ __forceinline__ void load_row(float (&v)[C][8], const void *p, int64_t at, int t, int d)
-{
+struct Raw {
+    typename Eight<T>::type v[C];
+    __device__ __forceinline__ void get(const void *p, int64_t at, int t, int d)
+    {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int n = (c * NT + t) * 8;
-        load8<T>(v[c], p, at + n, d - n);
+        for (int c = 0; c < C; ++c) {
+            const int n = (c * NT + t) * 8;
+            v[c] = get8<T>(p, at + n, d - n);
+        }
     }
-}
+    __device__ __forceinline__ float operator()(int c, int j) const { return (float)v[c][j]; }
+    // keeps a loop from holding the numbers as fp32, in twice the registers
+    __device__ __forceinline__ void stay()
+    {
+        if constexpr (sizeof(T) == 2)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                v4u w = __builtin_bit_cast(v4u, v[c]);
+                __asm__("" : "+v"(w));
+                v[c] = __builtin_bit_cast(typename Eight<T>::type, w);
+            }
+    }
+};
+
+// every element of a thread's pieces
+#define EACH(c, j)                                                                                                                 \
+    _Pragma("unroll") for (int c = 0; c < C; ++c) _Pragma("unroll") for (int j = 0; j < 8; ++j)
+
 template <class T, int NT, int C>
 __device__ __forceinline__ void store_row(void *p, int64_t at, const float (&v)[C][8], int t, int d)
 {
@@ -60,158 +82,123 @@ __device__ __forceinline__ void store_row(void *p, int64_t at, const float (&v)[
     }
 }
 
-// v and w normalised in place; elements past the row stay 0.  r: the reciprocals of their deviations.
+// v and w normalised in place; elements past the row stay 0.  Returns the reciprocals of their deviations.
 template <int NT, int C>
 __device__ __forceinline__ v2f normalise(float (&v)[C][8], float (&w)[C][8], int how_v, int how_w, int t, int d, float eps,
                                          RowSum<NT> &sum)
 {
     if (how_v == DN_NORM_LAYER || how_w == DN_NORM_LAYER) {
         v2f s = {};
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                s[0] += v[c][j];
-                s[1] += w[c][j];
-            }
+        EACH(c, j)
+        {
+            s[0] += v[c][j];
+            s[1] += w[c][j];
+        }
         s = sum(s) / (float)d;
         const float mv = how_v == DN_NORM_LAYER ? s[0] : 0.f, mw = how_w == DN_NORM_LAYER ? s[1] : 0.f;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if ((c * NT + t) * 8 + j < d) {
-                    v[c][j] -= mv;
-                    w[c][j] -= mw;
-                }
+        EACH(c, j)
+        if ((c * NT + t) * 8 + j < d) {
+            v[c][j] -= mv;
+            w[c][j] -= mw;
+        }
     }
     v2f q = {};
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            q[0] += v[c][j] * v[c][j];
-            q[1] += w[c][j] * w[c][j];
-        }
+    EACH(c, j)
+    {
+        q[0] += v[c][j] * v[c][j];
+        q[1] += w[c][j] * w[c][j];
+    }
     q = sum(q) / (float)d;
     const v2f r = {how_v ? 1.f / sqrtf(q[0] + eps) : 1.f, how_w ? 1.f / sqrtf(q[1] + eps) : 1.f};
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[c][j] *= r[0];
-            w[c][j] *= r[1];
-        }
+    EACH(c, j)
+    {
+        v[c][j] *= r[0];
+        w[c][j] *= r[1];
+    }
     return r;
 }
 
-template <class T, int NT, int C>
+// AHEAD: a row's reads go out before the row before it is worked on.
+template <class T, int NT, int C, bool AHEAD>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_forward_kernel(const NormArgs a)
 {
     constexpr int RB = NT < 256 ? 256 / NT : 1;   // rows of a workgroup at a time
     __shared__ v2f slots[2 * (NT / 64)];
     RowSum<NT> sum{slots};
     const int t = threadIdx.x % NT;
-    for (int64_t m = (int64_t)blockIdx.x * RB + threadIdx.x / NT; m < a.rows; m += (int64_t)gridDim.x * RB) {
+    Raw<T, NT, C> post_w, post_b, pre_w, pre_b, raw_x, raw_b, raw_gate;
+    if (a.post_w) post_w.get(a.post_w, 0, t, a.d);
+    if (a.post_b) post_b.get(a.post_b, 0, t, a.d);
+    if (a.pre_w) pre_w.get(a.pre_w, 0, t, a.d);
+    if (a.pre_b) pre_b.get(a.pre_b, 0, t, a.d);
+    auto fetch = [&](int64_t m) {
+        raw_x.get(a.x, m * a.d, t, a.d);
+        if (a.b) raw_b.get(a.b, m * a.d, t, a.d);
+        if (a.gate) raw_gate.get(a.gate, m / a.group * a.d, t, a.d);
+    };
+    const int64_t step = (int64_t)gridDim.x * RB;
+    int64_t m = (int64_t)blockIdx.x * RB + threadIdx.x / NT;
+    if (AHEAD && m < a.rows) fetch(m);
+    for (; m < a.rows; m += step) {
+        if (!AHEAD) fetch(m);
+        post_w.stay();
+        post_b.stay();
+        pre_w.stay();
+        pre_b.stay();
         const int64_t at = m * a.d;
-        float x[C][8], none[C][8] = {};
-        load_row<T, NT, C>(x, a.x, at, t, a.d);
+        float x[C][8], b[C][8] = {}, gate[C][8], none[C][8] = {};
+        EACH(c, j) x[c][j] = raw_x(c, j);
+        if (a.b) EACH(c, j) b[c][j] = raw_b(c, j);
+        if (a.gate) EACH(c, j) gate[c][j] = raw_gate(c, j);
+        if (AHEAD && m + step < a.rows) fetch(m + step);
         if (a.b) {
-            float b[C][8], p[C][8];
-            load_row<T, NT, C>(b, a.b, at, t, a.d);
             if (a.post) {
                 normalise<NT, C>(b, none, a.post, 0, t, a.d, a.eps, sum);
-                if (a.post_w) {
-                    load_row<T, NT, C>(p, a.post_w, 0, t, a.d);
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) b[c][j] *= p[c][j];
-                }
-                if (a.post_b) {
-                    load_row<T, NT, C>(p, a.post_b, 0, t, a.d);
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) b[c][j] += p[c][j];
-                }
+                if (a.post_w) EACH(c, j) b[c][j] *= post_w(c, j);
+                if (a.post_b) EACH(c, j) b[c][j] += post_b(c, j);
             }
-            if (a.gate) {
-                load_row<T, NT, C>(p, a.gate, m / a.group * a.d, t, a.d);
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) b[c][j] *= p[c][j];
-            }
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[c][j] += a.scale * b[c][j];
+            if (a.gate) EACH(c, j) b[c][j] *= gate[c][j];
+            EACH(c, j) x[c][j] += a.scale * b[c][j];
             store_row<T, NT, C>(a.x_out, at, x, t, a.d);
         }
         if (a.pre) {   // of x' before it is rounded to T
-            float p[C][8];
             normalise<NT, C>(x, none, a.pre, 0, t, a.d, a.eps, sum);
-            if (a.pre_w) {
-                load_row<T, NT, C>(p, a.pre_w, 0, t, a.d);
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[c][j] *= p[c][j];
-            }
-            if (a.pre_b) {
-                load_row<T, NT, C>(p, a.pre_b, 0, t, a.d);
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[c][j] += p[c][j];
-            }
+            if (a.pre_w) EACH(c, j) x[c][j] *= pre_w(c, j);
+            if (a.pre_b) EACH(c, j) x[c][j] += pre_b(c, j);
             store_row<T, NT, C>(a.n_out, at, x, t, a.d);
         }
     }
 }
 
-// q becomes r (q w - mean(q w) - hat mean(q w hat))
-template <class T, int NT, int C>
-__device__ __forceinline__ void norm_back(float (&q)[C][8], const float (&hat)[C][8], const void *w, int how, float r, int t, int d,
-                                          RowSum<NT> &sum)
+// q becomes r (q - mean(q) - hat mean(q hat))
+template <int NT, int C>
+__device__ __forceinline__ void norm_back(float (&q)[C][8], const float (&hat)[C][8], int how, float r, int d, RowSum<NT> &sum)
 {
-    if (w) {
-        float p[C][8];
-        load_row<T, NT, C>(p, w, 0, t, d);
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[c][j] *= p[c][j];
-    }
     v2f s = {};
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s[0] += q[c][j] * hat[c][j];
-            s[1] += q[c][j];
-        }
+    EACH(c, j)
+    {
+        s[0] += q[c][j] * hat[c][j];
+        s[1] += q[c][j];
+    }
     s = sum(s) / (float)d;
     const float mean = how == DN_NORM_LAYER ? s[1] : 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[c][j] = r * (q[c][j] - hat[c][j] * s[0] - mean);
+    EACH(c, j) q[c][j] = r * (q[c][j] - hat[c][j] * s[0] - mean);
 }
 
 // The sums over rows that a workgroup hands on, in this order, [parts][d] each where they are wanted; the gate's are the last.
 enum Sums : int { S_POST_W, S_POST_B, S_PRE_W, S_PRE_B, S_GATE, S_COUNT };
 
-template <class T, int NT, int C>
-__global__ __launch_bounds__(NT) void norm_backward_kernel(const NormArgs a)
+// With a gate that all rows share, scale dx summed alone (s0) and times b^ (s1) give all of the block's sums: dpost_w = gate s1,
+// dpost_b = gate s0, dgate = w s1 + shift s0.  GROUPS: the part is whole groups, whose dgate is written as each ends and whose
+// dpost are added up.
+template <class T, int NT, int C, bool AHEAD, bool GROUPS>
+__global__ __launch_bounds__(NT, NT <= 512 && C == 1 && sizeof(T) == 2 && !GROUPS ? 4 : 1) void norm_backward_kernel(const NormArgs a)
 {
     __shared__ v2f slots[2 * (NT / 64)];
     RowSum<NT> sum{slots};
     const int t = threadIdx.x, part = blockIdx.x;
-    // rows of this part: a piece of one group, or whole groups
     int64_t m, end;
-    if (a.group_parts > 1) {
+    if (!GROUPS) {
         const int64_t g = part / a.group_parts;
         m = g * a.group + (int64_t)(part % a.group_parts) * a.part_rows;
         end = min(min(m + a.part_rows, (g + 1) * a.group), (int64_t)a.rows);
@@ -219,106 +206,97 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormArgs a)
         m = (int64_t)part * a.part_rows;
         end = min(m + a.part_rows, (int64_t)a.rows);
     }
-    float sums[S_COUNT][C][8] = {};
+    Raw<T, NT, C> post_w, post_b, pre_w, gate, raw_x, raw_b, raw_dx, raw_dn;
+    if (a.post_w) post_w.get(a.post_w, 0, t, a.d);
+    if (a.post_b) post_b.get(a.post_b, 0, t, a.d);
+    if (a.pre_w) pre_w.get(a.pre_w, 0, t, a.d);
+    if (a.gate) gate.get(a.gate, m / a.group * a.d, t, a.d);
+    auto fetch = [&](int64_t r) {
+        const int64_t at = r * a.d;
+        if (a.pre) raw_x.get(a.x, at, t, a.d);
+        if (a.b) raw_b.get(a.b, at, t, a.d);
+        if (a.pre) raw_dn.get(a.dn, at, t, a.d);
+        if (a.dx_out) raw_dx.get(a.dx_out, at, t, a.d);
+    };
+    float sums[S_GATE][C][8] = {}, s0[C][8] = {}, s1[C][8] = {};
+    auto close = [&]() {   // a gate's rows, or this part of them: their dpost, and dgate in s1
+        EACH(c, j)
+        {
+            const float k = a.gate ? gate(c, j) : 1.f;
+            sums[S_POST_W][c][j] += k * s1[c][j];
+            sums[S_POST_B][c][j] += k * s0[c][j];
+            s1[c][j] = (a.post_w ? s1[c][j] * post_w(c, j) : s1[c][j]) + (a.post_b ? s0[c][j] * post_b(c, j) : 0.f);
+        }
+    };
+    if (AHEAD) fetch(m);
     for (; m < end; ++m) {
+        if (!AHEAD) fetch(m);
+        post_w.stay();
+        post_b.stay();
+        pre_w.stay();
+        gate.stay();
         const int64_t at = m * a.d;
         float x[C][8] = {}, b[C][8] = {}, g[C][8] = {}, q[C][8] = {};
-        if (a.pre) load_row<T, NT, C>(x, a.x, at, t, a.d);
-        if (a.b) load_row<T, NT, C>(b, a.b, at, t, a.d);
-        if (a.pre) load_row<T, NT, C>(q, a.dn, at, t, a.d);
-        if (a.dx_out) load_row<T, NT, C>(g, a.dx_out, at, t, a.d);
+        if (a.pre) EACH(c, j) x[c][j] = raw_x(c, j);
+        if (a.b) EACH(c, j) b[c][j] = raw_b(c, j);
+        if (a.pre) EACH(c, j) q[c][j] = raw_dn(c, j);
+        if (a.dx_out) EACH(c, j) g[c][j] = raw_dx(c, j);
+        if (AHEAD && m + 1 < end) fetch(m + 1);
         v2f r = {1.f, 1.f};
         if (a.pre || a.post) r = normalise<NT, C>(x, b, a.pre, a.post, t, a.d, a.eps, sum);
         if (a.pre) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sums[S_PRE_W][c][j] += q[c][j] * x[c][j];
-                    sums[S_PRE_B][c][j] += q[c][j];
-                }
-            norm_back<T, NT, C>(q, x, a.pre_w, a.pre, r[0], t, a.d, sum);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[c][j] += q[c][j];
+            EACH(c, j)
+            {
+                sums[S_PRE_W][c][j] += q[c][j] * x[c][j];
+                sums[S_PRE_B][c][j] += q[c][j];
+            }
+            if (a.pre_w) EACH(c, j) q[c][j] *= pre_w(c, j);
+            norm_back<NT, C>(q, x, a.pre, r[0], a.d, sum);
+            EACH(c, j) g[c][j] += q[c][j];
         }
         store_row<T, NT, C>(a.dx, at, g, t, a.d);
         if (!a.b) continue;
-        float p[C][8];
-        if (a.dgate) {
-            // c = post(b)
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[c][j] = b[c][j];
-            if (a.post && a.post_w) {
-                load_row<T, NT, C>(p, a.post_w, 0, t, a.d);
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) q[c][j] *= p[c][j];
-            }
-            if (a.post && a.post_b) {
-                load_row<T, NT, C>(p, a.post_b, 0, t, a.d);
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) q[c][j] += p[c][j];
-            }
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sums[S_GATE][c][j] += a.scale * g[c][j] * q[c][j];
+        EACH(c, j)
+        {
+            g[c][j] *= a.scale;
+            s0[c][j] += g[c][j];
+            s1[c][j] += g[c][j] * b[c][j];
         }
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[c][j] *= a.scale;
-        if (a.gate) {
-            load_row<T, NT, C>(p, a.gate, m / a.group * a.d, t, a.d);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[c][j] *= p[c][j];
-        }
+        if (a.gate) EACH(c, j) g[c][j] *= gate(c, j);
         if (a.post) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sums[S_POST_W][c][j] += g[c][j] * b[c][j];
-                    sums[S_POST_B][c][j] += g[c][j];
-                }
-            norm_back<T, NT, C>(g, b, a.post_w, a.post, r[1], t, a.d, sum);
+            if (a.post_w) EACH(c, j) g[c][j] *= post_w(c, j);
+            norm_back<NT, C>(g, b, a.post, r[1], a.d, sum);
         }
         store_row<T, NT, C>(a.db, at, g, t, a.d);
-        if (a.dgate && a.group_parts == 1 && (m + 1 == end || (m + 1) % a.group == 0)) {   // a whole group's
-            const int64_t row = m / a.group * a.d;
-            if (a.f32_out) store_row<float, NT, C>(a.dgate, row, sums[S_GATE], t, a.d);
-            else store_row<T, NT, C>(a.dgate, row, sums[S_GATE], t, a.d);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sums[S_GATE][c][j] = 0.f;
+        if (GROUPS && (m + 1 == end || (m + 1) % a.group == 0)) {   // a gate's last row
+            close();
+            if (a.dgate) {
+                const int64_t row = m / a.group * a.d;
+                if (a.f32_out) store_row<float, NT, C>(a.dgate, row, s1, t, a.d);
+                else store_row<T, NT, C>(a.dgate, row, s1, t, a.d);
+            }
+            EACH(c, j) s0[c][j] = s1[c][j] = 0.f;
+            if (a.gate && m + 1 < end) gate.get(a.gate, (m + 1) / a.group * a.d, t, a.d);
         }
     }
-    void *const want[S_COUNT] = {a.dpost_w, a.dpost_b, a.dpre_w, a.dpre_b, a.group_parts > 1 ? a.dgate : nullptr};
+    if (!GROUPS) close();
+    void *const want[S_COUNT] = {a.dpost_w, a.dpost_b, a.dpre_w, a.dpre_b, GROUPS ? nullptr : a.dgate};
     float *ws = a.ws;
 #pragma unroll
     for (int k = 0; k < S_COUNT; ++k)
         if (want[k]) {
-            store_row<float, NT, C>(ws, (int64_t)part * a.d, sums[k], t, a.d);
+            store_row<float, NT, C>(ws, (int64_t)part * a.d, k < S_GATE ? sums[k < S_GATE ? k : 0] : s1, t, a.d);
             ws += (int64_t)a.parts * a.d;
         }
 }
+#undef EACH
 
-// Column sums of the workgroups' parts, in order.  A workgroup takes 32 columns of one set of parts, eight threads a column;
+// Column sums of the workgroups' parts, in order.  A workgroup takes 32 columns of one set of parts, sixteen threads a column;
 // blockIdx.y: a parameter, then the gate's groups.
 template <class T>
-__global__ __launch_bounds__(256) void norm_join_kernel(const NormArgs a)
+__global__ __launch_bounds__(512) void norm_join_kernel(const NormArgs a)
 {
-    __shared__ float share[8][32];
+    __shared__ float share[16][32];
     const int n = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
     void *const want[S_COUNT] = {a.dpost_w, a.dpost_b, a.dpre_w, a.dpre_b, a.group_parts > 1 ? a.dgate : nullptr};
     int which = 0, set = 0, y = blockIdx.y;
@@ -332,12 +310,13 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const NormArgs a)
     const int to = which == S_GATE ? min(a.parts, from + a.group_parts) : a.parts;
     float s = 0.f;
     if (n < a.d)
-        for (int p = from + lane; p < to; p += 8) s += a.ws[((int64_t)set * a.parts + p) * a.d + n];
+#pragma unroll 8
+        for (int p = from + lane; p < to; p += 16) s += a.ws[((int64_t)set * a.parts + p) * a.d + n];
     share[lane][threadIdx.x & 31] = s;
     __syncthreads();
     if (lane || n >= a.d) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s += share[k][threadIdx.x & 31];
+    for (int k = 1; k < 16; ++k) s += share[k][threadIdx.x & 31];
     const int64_t at = which == S_GATE ? (int64_t)y * a.d + n : n;
     if (a.f32_out) static_cast<float *>(want[which])[at] = s;
     else static_cast<T *>(want[which])[at] = (T)s;
@@ -348,20 +327,21 @@ hipError_t forward(const NormArgs &a, hipStream_t s)
 {
     constexpr int block = NT < 256 ? 256 : NT, rows = NT < 256 ? 256 / NT : 1;
     const int64_t need = ((int64_t)a.rows + rows - 1) / rows, most = 256 * (2048 / block);
-    launch_kernel(norm_forward_kernel<T, NT, C>, dim3((unsigned)(need < most ? need : most)), dim3(block), 0, s, a);
+    launch_kernel(norm_forward_kernel<T, NT, C, C == 1>, dim3((unsigned)(need < most ? need : most)), dim3(block), 0, s, a);
     return hipGetLastError();
 }
 
 template <class T, int NT, int C>
 hipError_t backward(const NormArgs &a, hipStream_t s)
 {
-    launch_kernel(norm_backward_kernel<T, NT, C>, dim3((unsigned)a.parts), dim3(NT), 0, s, a);
+    if (a.group_parts > 1) launch_kernel(norm_backward_kernel<T, NT, C, C == 1, false>, dim3((unsigned)a.parts), dim3(NT), 0, s, a);
+    else launch_kernel(norm_backward_kernel<T, NT, C, C == 1, true>, dim3((unsigned)a.parts), dim3(NT), 0, s, a);
     const hipError_t e = hipGetLastError();
     const bool gates = a.dgate && a.group_parts > 1;
     const int params = (a.dpost_w != nullptr) + (a.dpost_b != nullptr) + (a.dpre_w != nullptr) + (a.dpre_b != nullptr);
     const int groups = gates ? (int)(((int64_t)a.rows + a.group - 1) / a.group) : 0;
     if (e != hipSuccess || params + groups == 0) return e;
-    launch_kernel(norm_join_kernel<T>, dim3((unsigned)((a.d + 31) / 32), (unsigned)(params + groups)), dim3(256), 0, s, a);
+    launch_kernel(norm_join_kernel<T>, dim3((unsigned)((a.d + 31) / 32), (unsigned)(params + groups)), dim3(512), 0, s, a);
     return hipGetLastError();
 }
 
@@ -388,10 +368,11 @@ hipError_t backward_by_width(const NormArgs &a, hipStream_t s)
 
 size_t norm_backward_plan(NormArgs &a)
 {
-    // parts: as many as keep the chip full, so many threads a row being taken; more would write and read more partial sums
+    // parts: as many as keep the chip full, so many threads a row being taken; more, or fewer rows a part, would write and read more
+    // partial sums
     const int64_t threads = a.d <= 512 ? 64 : a.d <= 2048 ? 256 : 512, most = 256 * 1024 / threads;
     int64_t part = ((int64_t)a.rows + most - 1) / most;
-    if (part < 1) part = 1;
+    if (part < 4) part = 4;
     if (a.group > part) {
         a.group_parts = (int32_t)(((int64_t)a.group + part - 1) / part);
         if (a.group_parts == 1) part = a.group;
