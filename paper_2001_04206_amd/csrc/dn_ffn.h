@@ -10,11 +10,6 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef _Float16 f16;
 typedef __bf16 bf16;
 
-template <class T> struct Elem;
-template <> struct Elem<float> { static constexpr int TYPE = DN_F32; };
-template <> struct Elem<f16> { static constexpr int TYPE = DN_F16; };
-template <> struct Elem<bf16> { static constexpr int TYPE = DN_BF16; };
-
 // eight elements as they lie in memory, at any alignment of theirs
 template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
 

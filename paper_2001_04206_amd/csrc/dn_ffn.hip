@@ -211,16 +211,26 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
     ProductPlan plan;
     const int bk = type == DN_F32 ? 32 : 64, steps = (K + bk - 1) / bk * segments;
     plan.steps = steps;
-    if (p == P_FWD && M <= kFewRows) {
+    if (p == P_FWD && M <= 16) {
         plan.kernel = K_FEW;
         return plan;
     }
-    // Tiles of 256 x 256 or (always for fp32, where the instruction is the bound either way) of 128 x 128, and k in how many parts:
-    // whichever is expected to take less.  Microseconds a stage, a round of workgroups and bytes of parts, as measured: a stage of
-    // a large tile takes 1.5 us whether the chip is full or not, one of two small tiles on each compute unit 1.35 (fp32: 3.6), so
-    // that 2048 x 4096 x 1024 takes less on the 128 large tiles that it has than on 512 small ones, which fill the chip.
+    // Which kernel, and k in how many parts: whichever is expected to take least.  Microseconds a stage, a round of workgroups and
+    // bytes, as measured.  A stage of a 256 x 256 tile takes 1.5 us whether the chip is full or not, one of 128 x 256 0.8; fp32 is
+    // bound by its matrix instruction at any size, 3.6 us for two tiles of 128 x 128 on every compute unit.  2048 x 4096 x 1024 so
+    // takes 20 us on 256 medium tiles (128 large ones: 32), 8192 x 4096 x 4096 260 on 512 large ones (medium: 330).  Weights come
+    // at 4.6 TB/s, and up to 64 rows the kernel that stages nothing competes, whose workgroups of 16 columns each read all rows,
+    // at 11 TB/s: through a gated product of 4096 x 8192 x 2, 8 rows take 33 us there (tiles: 35), 32 rows 42 (tiles: 35), 64 rows
+    // 58 (tiles: 37).  Up to 16 rows it is taken without asking.  Tiles at widths that are no multiple of 16 bytes need a copy
+    // first.
     const int planes = e == E_GATED ? 2 : 1;
+    const double es = (double)size_of(type), weights = es * planes * N * K * segments / 4.6e6;
     double best = 1e300;
+    const double copies = (int64_t)K * size_of(type) % 16 == 0 ? 0 : 4 + 2 * (weights + es * M * K / 4.6e6);
+    if (p == P_FWD && M <= kFewRows) {
+        best = 6 + weights + (N + 15) / 16 * ((M + 15) / 16 * 16.) * K * es / 11e6 - copies;
+        plan.kernel = K_FEW;
+    }
     struct Way { ProductKernel kernel; int rows, cols, room; double stage, round; };
     const Way small{K_SMALL, 128, 128, 512, 3.6, 6}, medium{K_MEDIUM, 128, 256, 256, 0.8, 6}, large{K_LARGE, 256, 256, 256, 1.5, 8};
     for (const Way &w : {large, medium, small}) {
@@ -231,6 +241,7 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
             if (w.kernel == K_LARGE) each = (each + 1) / 2 * 2;
             const int parts = (steps + each - 1) / each;
             double us = (double)((t * parts + w.room - 1) / w.room) * (each * w.stage + w.round);
+            if (p == P_FWD && us < weights) us = weights;
             if (parts > 1) us += 3 + 8e-6 * parts * planes * M * N / 4.5;
             if (us < best) {
                 best = us;

@@ -7,7 +7,6 @@
 
 namespace dn {
 
-
 // sixteen bytes of a row of which `left` elements exist from here on
 template <class T, bool WHOLE>
 __device__ __forceinline__ v4u chunk(const T *p, int left)

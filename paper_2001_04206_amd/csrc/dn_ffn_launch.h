@@ -36,6 +36,7 @@ hipError_t few_of(const ProductArgs &a, hipStream_t s)
     const dim3 grid((unsigned)((a.N + 15) / 16)), block(512);
     if (a.M <= 16) launch_kernel(few_kernel<T, EPI, 1, WHOLE>, grid, block, 0, s, a);
     else if (a.M <= 32) launch_kernel(few_kernel<T, EPI, 2, WHOLE>, grid, block, 0, s, a);
+    else if (a.M <= 48) launch_kernel(few_kernel<T, EPI, 3, WHOLE>, grid, block, 0, s, a);
     else launch_kernel(few_kernel<T, EPI, 4, WHOLE>, grid, block, 0, s, a);
     return hipGetLastError();
 }
