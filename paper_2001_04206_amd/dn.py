@@ -345,12 +345,15 @@ def dn_sgd_step(param, grad, velocity, lr: float, momentum: float):
 
 # ---- the residual feed-forward block -----------------------------------------------------------------------------
 
-_TYPES = {}
+_TYPES = {}     # torch.dtype -> dn_type
+_torch = None
 
 
 def _type_of(t, what: str) -> int:
-    if not _TYPES:
+    global _torch
+    if _torch is None:
         import torch
+        _torch = torch
         _TYPES.update({torch.float32: DN_F32, torch.float16: DN_F16, torch.bfloat16: DN_BF16})
     kind = _TYPES.get(getattr(t, "dtype", None))
     if kind is None or not t.is_cuda:
@@ -358,26 +361,27 @@ def _type_of(t, what: str) -> int:
     return kind
 
 
-def _matrix(t, like, rows: int, cols: int, what: str):
-    """(pointer, elements between rows) of a matrix of `like`'s type and device; rows may lie apart."""
+def _matrix(t, dtype, dev: int, shape, what: str):
+    """(pointer, elements between rows) of a matrix of that type on that device; rows may lie apart."""
     if t is None:
         return None, 0
-    if t.dtype is not like.dtype or t.get_device() != like.get_device():
-        raise TypeError("%s must be a tensor of dtype %s on %s" % (what, like.dtype, like.device))
-    if t.shape != (rows, cols):
-        raise TypeError("%s must have shape %s, not %s" % (what, (rows, cols), tuple(t.shape)))
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise TypeError("%s must be a tensor of dtype %s on device %d" % (what, dtype, dev))
+    if t.shape != shape:
+        raise TypeError("%s must have shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
     step, one = t.stride()
+    rows, cols = shape
     if (one != 1 and cols > 1) or (step < cols and rows > 1):
         raise TypeError("%s must have contiguous rows that do not overlap" % what)
     return t.data_ptr(), step if rows > 1 else cols
 
 
-def _dense(t, like, shape, what: str, dtype=None):
-    """The pointer of a contiguous tensor of `like`'s type (or `dtype`) and device, None for None."""
+def _dense(t, dtype, dev: int, shape, what: str):
+    """The pointer of a contiguous tensor of that type and shape on that device, None for None."""
     if t is None:
         return None
-    if t.dtype is not (dtype or like.dtype) or t.get_device() != like.get_device() or not t.is_contiguous():
-        raise TypeError("%s must be a contiguous tensor of dtype %s on %s" % (what, dtype or like.dtype, like.device))
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous tensor of dtype %s on device %d" % (what, dtype, dev))
     if t.shape != shape:
         raise TypeError("%s must have shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
     return t.data_ptr()
@@ -391,21 +395,18 @@ def _grad_type(grad, like):
     return kind, like.dtype
 
 
-def _workspace(need: int, workspace, like, where: str):
+_REFUSED = C.c_size_t(-1).value
+
+
+def _workspace(need: int, workspace, like):
     """(the tensor, its pointer, its bytes); allocated here if the caller brings none."""
-    if need == 0 and workspace is None:
-        return None, None, 0
-    if need == _REFUSED:
-        return None, None, 0      # the call itself says what is wrong
-    import torch
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
-    elif workspace.dtype != torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
+        if need == 0 or need == _REFUSED:      # refused: the call itself says why
+            return None, None, 0
+        workspace = _torch.empty(need, dtype=_torch.uint8, device=like.device)
+    elif workspace.dtype != _torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous uint8 tensor on %s" % (like.device,))
     return workspace, workspace.data_ptr(), workspace.numel()
-
-
-_REFUSED = C.c_size_t(-1).value
 
 
 class _Here:
@@ -418,17 +419,15 @@ class _Here:
         return False
 
 
-_HERE_ALREADY = _Here()
+_here = _Here()
 
 
-def _on(like):
-    import torch
-    return _HERE_ALREADY if torch.cuda.current_device() == like.get_device() else torch.cuda.device(like.device)
+def _on(dev: int):
+    return _here if _torch.cuda.current_device() == dev else _torch.cuda.device(dev)
 
 
-def _stream(like) -> int:
-    import torch
-    return torch.cuda.current_stream(like.get_device()).cuda_stream
+def _stream(dev: int) -> int:
+    return _torch.cuda.current_stream(dev).cuda_stream
 
 
 def _two(t, what: str):
@@ -441,13 +440,14 @@ def _linear_desc(X, W, R, Y, Yname, act, drop, seed, offset, grad_type, grad_sca
     kind = _type_of(X, "X")
     rows, n_in = _two(X, "X")
     n_out = _two(W, "W")[0]
-    x, ldx = _matrix(X, X, rows, n_in, "X")
-    w, ldw = _matrix(W, X, n_out, n_in, "W")
-    r, ldr = _matrix(R, X, rows, n_out, "R")
-    y, ldy = _matrix(Y, X, rows, n_out, Yname)
-    d = LinearDesc(kind, kind if grad_type is None else grad_type, int(act), rows, n_in, n_out, ldx, ldw, ldr, ldy, float(drop),
-                   float(grad_scale), int(seed), int(offset))
-    return d, x, w, r, y, rows, n_in, n_out
+    dtype, dev = X.dtype, X.get_device()
+    x, ldx = _matrix(X, dtype, dev, (rows, n_in), "X")
+    w, ldw = _matrix(W, dtype, dev, (n_out, n_in), "W")
+    r, ldr = _matrix(R, dtype, dev, (rows, n_out), "R")
+    y, ldy = _matrix(Y, dtype, dev, (rows, n_out), Yname)
+    d = LinearDesc(kind, kind if grad_type is None else grad_type, act, rows, n_in, n_out, ldx, ldw, ldr, ldy, drop, grad_scale,
+                   seed, offset)
+    return d, x, w, r, y, rows, n_in, n_out, dtype, dev
 
 
 def dn_linear_forward(X, W, bias, R, Y, Z=None, act: int = DN_ACT_LINEAR, drop: float = 0.0, seed: int = 0, offset: int = 0,
@@ -455,12 +455,12 @@ def dn_linear_forward(X, W, bias, R, Y, Z=None, act: int = DN_ACT_LINEAR, drop: 
     """Y = R + D(f(X W^T + bias)); Z receives X W^T + bias.  bias, R and Z may be None.  Enqueued on torch's current stream, as
     everything below; `workspace`: a uint8 tensor of dn_linear_forward_workspace_bytes bytes (allocated here if None)."""
     l = lib()
-    d, x, w, r, y, rows, _, n_out = _linear_desc(X, W, R, Y, "Y", act, drop, seed, offset, None, 1.0)
-    b, z = _dense(bias, X, (n_out,), "bias"), _dense(Z, X, (rows, n_out), "Z")
-    with _on(X):
+    d, x, w, r, y, rows, _, n_out, dtype, dev = _linear_desc(X, W, R, Y, "Y", act, drop, seed, offset, None, 1.0)
+    b, z = _dense(bias, dtype, dev, (n_out,), "bias"), _dense(Z, dtype, dev, (rows, n_out), "Z")
+    with _on(dev):
         at = C.addressof(d)
-        _keep, ws, n = _workspace(l.dn_linear_forward_workspace_bytes(at), workspace, X, "dn_linear_forward")
-        _check(l.dn_linear_forward(at, x, w, b, r, y, z, ws, n, _stream(X)), "dn_linear_forward")
+        _keep, ws, n = _workspace(l.dn_linear_forward_workspace_bytes(at), workspace, X)
+        _check(l.dn_linear_forward(at, x, w, b, r, y, z, ws, n, _stream(dev)), "dn_linear_forward")
 
 
 def dn_linear_backward(X, W, Z, dY, dX, dW, dbias, act: int = DN_ACT_LINEAR, drop: float = 0.0, seed: int = 0, offset: int = 0,
@@ -469,25 +469,26 @@ def dn_linear_backward(X, W, Z, dY, dX, dW, dbias, act: int = DN_ACT_LINEAR, dro
     None without an activation; dX, dW, dbias may be None; dW and dbias are of X's type or float32."""
     l = lib()
     gt, gdtype = _grad_type(dW, X)
-    d, x, w, _, y, rows, n_in, n_out = _linear_desc(X, W, None, dY, "dY", act, drop, seed, offset, gt, grad_scale)
-    z, dx = _dense(Z, X, (rows, n_out), "Z"), _dense(dX, X, (rows, n_in), "dX")
-    dw, db = _dense(dW, X, (n_out, n_in), "dW", gdtype), _dense(dbias, X, (n_out,), "dbias", gdtype)
-    with _on(X):
+    d, x, w, _, y, rows, n_in, n_out, dtype, dev = _linear_desc(X, W, None, dY, "dY", act, drop, seed, offset, gt, grad_scale)
+    z, dx = _dense(Z, dtype, dev, (rows, n_out), "Z"), _dense(dX, dtype, dev, (rows, n_in), "dX")
+    dw, db = _dense(dW, gdtype, dev, (n_out, n_in), "dW"), _dense(dbias, gdtype, dev, (n_out,), "dbias")
+    with _on(dev):
         at = C.addressof(d)
-        _keep, ws, n = _workspace(l.dn_linear_backward_workspace_bytes(at), workspace, X, "dn_linear_backward")
-        _check(l.dn_linear_backward(at, x, w, z, y, dx, dw, db, ws, n, _stream(X)), "dn_linear_backward")
+        _keep, ws, n = _workspace(l.dn_linear_backward_workspace_bytes(at), workspace, X)
+        _check(l.dn_linear_backward(at, x, w, z, y, dx, dw, db, ws, n, _stream(dev)), "dn_linear_backward")
 
 
 def _ffn_desc(X, Wg, Wu, Wd, R, Y, Yname, act, drop, seed, offset, grad_type, grad_scale):
     kind = _type_of(X, "X")
     rows, d = _two(X, "X")
     f = _two(Wg, "Wg")[0]
-    x, ldx = _matrix(X, X, rows, d, "X")
-    r, ldr = _matrix(R, X, rows, d, "R")
-    y, ldy = _matrix(Y, X, rows, d, Yname)
-    desc = FfnDesc(kind, kind if grad_type is None else grad_type, int(act), rows, d, f, ldx, ldr, ldy, float(drop),
-                   float(grad_scale), int(seed), int(offset))
-    return desc, x, r, y, _dense(Wg, X, (f, d), "Wg"), _dense(Wu, X, (f, d), "Wu"), _dense(Wd, X, (d, f), "Wd"), rows, d, f
+    dtype, dev = X.dtype, X.get_device()
+    x, ldx = _matrix(X, dtype, dev, (rows, d), "X")
+    r, ldr = _matrix(R, dtype, dev, (rows, d), "R")
+    y, ldy = _matrix(Y, dtype, dev, (rows, d), Yname)
+    desc = FfnDesc(kind, kind if grad_type is None else grad_type, act, rows, d, f, ldx, ldr, ldy, drop, grad_scale, seed, offset)
+    w = _dense(Wg, dtype, dev, (f, d), "Wg"), _dense(Wu, dtype, dev, (f, d), "Wu"), _dense(Wd, dtype, dev, (d, f), "Wd")
+    return desc, x, r, y, w, rows, d, f, dtype, dev
 
 
 def dn_ffn_forward(X, Wg, bg, Wu, bu, Wd, bd, R, Y, GU=None, act: int = DN_ACT_SILU, drop: float = 0.0, seed: int = 0,
@@ -495,13 +496,13 @@ def dn_ffn_forward(X, Wg, bg, Wu, bu, Wd, bd, R, Y, GU=None, act: int = DN_ACT_S
     """Y = R + D((f(X Wg^T + bg) * (X Wu^T + bu)) Wd^T + bd); GU [rows][2 f] receives both net inputs.  The biases, R and GU
     may be None."""
     l = lib()
-    desc, x, r, y, wg, wu, wd, rows, d, f = _ffn_desc(X, Wg, Wu, Wd, R, Y, "Y", act, drop, seed, offset, None, 1.0)
-    g, u, b = _dense(bg, X, (f,), "bg"), _dense(bu, X, (f,), "bu"), _dense(bd, X, (d,), "bd")
-    gu = _dense(GU, X, (rows, 2 * f), "GU")
-    with _on(X):
+    desc, x, r, y, (wg, wu, wd), rows, d, f, dtype, dev = _ffn_desc(X, Wg, Wu, Wd, R, Y, "Y", act, drop, seed, offset, None, 1.0)
+    g, u = _dense(bg, dtype, dev, (f,), "bg"), _dense(bu, dtype, dev, (f,), "bu")
+    b, gu = _dense(bd, dtype, dev, (d,), "bd"), _dense(GU, dtype, dev, (rows, 2 * f), "GU")
+    with _on(dev):
         at = C.addressof(desc)
-        _keep, ws, n = _workspace(l.dn_ffn_forward_workspace_bytes(at), workspace, X, "dn_ffn_forward")
-        _check(l.dn_ffn_forward(at, x, wg, g, wu, u, wd, b, r, y, gu, ws, n, _stream(X)), "dn_ffn_forward")
+        _keep, ws, n = _workspace(l.dn_ffn_forward_workspace_bytes(at), workspace, X)
+        _check(l.dn_ffn_forward(at, x, wg, g, wu, u, wd, b, r, y, gu, ws, n, _stream(dev)), "dn_ffn_forward")
 
 
 def dn_ffn_backward(X, Wg, Wu, Wd, GU, dY, dX, dWg, dbg, dWu, dbu, dWd, dbd, act: int = DN_ACT_SILU, drop: float = 0.0,
@@ -509,22 +510,24 @@ def dn_ffn_backward(X, Wg, Wu, Wd, GU, dY, dX, dWg, dbg, dWu, dbu, dWd, dbd, act
     """The block's gradients; dX and the biases' may be None, the parameters' are all of X's type or all float32."""
     l = lib()
     gt, gdtype = _grad_type(dWg, X)
-    desc, x, _, y, wg, wu, wd, rows, d, f = _ffn_desc(X, Wg, Wu, Wd, None, dY, "dY", act, drop, seed, offset, gt, grad_scale)
-    gu, dx = _dense(GU, X, (rows, 2 * f), "GU"), _dense(dX, X, (rows, d), "dX")
-    dwg, dwu, dwd = (_dense(t, X, s, n, gdtype) for t, s, n in ((dWg, (f, d), "dWg"), (dWu, (f, d), "dWu"), (dWd, (d, f), "dWd")))
-    g, u, b = (_dense(t, X, (m,), n, gdtype) for t, m, n in ((dbg, f, "dbg"), (dbu, f, "dbu"), (dbd, d, "dbd")))
-    with _on(X):
+    desc, x, _, y, (wg, wu, wd), rows, d, f, dtype, dev = _ffn_desc(X, Wg, Wu, Wd, None, dY, "dY", act, drop, seed, offset, gt,
+                                                                    grad_scale)
+    gu, dx = _dense(GU, dtype, dev, (rows, 2 * f), "GU"), _dense(dX, dtype, dev, (rows, d), "dX")
+    dwg, dwu = _dense(dWg, gdtype, dev, (f, d), "dWg"), _dense(dWu, gdtype, dev, (f, d), "dWu")
+    dwd, b = _dense(dWd, gdtype, dev, (d, f), "dWd"), _dense(dbd, gdtype, dev, (d,), "dbd")
+    g, u = _dense(dbg, gdtype, dev, (f,), "dbg"), _dense(dbu, gdtype, dev, (f,), "dbu")
+    with _on(dev):
         at = C.addressof(desc)
-        _keep, ws, n = _workspace(l.dn_ffn_backward_workspace_bytes(at), workspace, X, "dn_ffn_backward")
-        _check(l.dn_ffn_backward(at, x, wg, wu, wd, gu, y, dx, dwg, g, dwu, u, dwd, b, ws, n, _stream(X)), "dn_ffn_backward")
+        _keep, ws, n = _workspace(l.dn_ffn_backward_workspace_bytes(at), workspace, X)
+        _check(l.dn_ffn_backward(at, x, wg, wu, wd, gu, y, dx, dwg, g, dwu, u, dwd, b, ws, n, _stream(dev)), "dn_ffn_backward")
 
 
-def _norm_desc(like, gate, post, pre, scale, eps, rows_per_gate, grad_type=None):
+def _norm_desc(like, post, pre, scale, eps, rows_per_gate, grad_type=None):
     kind = _type_of(like, "x")
     rows, d = _two(like, "x")
-    per = rows if rows_per_gate is None else int(rows_per_gate)
-    desc = NormDesc(kind, kind if grad_type is None else grad_type, rows, d, int(post), int(pre), max(per, 0), float(scale), float(eps))
-    return desc, rows, d, -(-rows // per) if per > 0 else 0
+    per = rows if rows_per_gate is None else rows_per_gate
+    desc = NormDesc(kind, kind if grad_type is None else grad_type, rows, d, post, pre, max(per, 0), scale, eps)
+    return desc, (rows, d), (d,), (-(-rows // per) if per > 0 else 0, d), like.dtype, like.get_device()
 
 
 def dn_norm_forward(x, b, gate, post_w, post_b, pre_w, pre_b, x_out, n_out, post: int = DN_NORM_RMS, pre: int = DN_NORM_RMS,
@@ -532,13 +535,13 @@ def dn_norm_forward(x, b, gate, post_w, post_b, pre_w, pre_b, x_out, n_out, post
     """x_out = x + scale gate post(b), n_out = pre(x_out).  b, gate, the norms' weights and shifts may be None (no block,
     ones, zeros); gate [ceil(rows / rows_per_gate)][d] (default: one row)."""
     l = lib()
-    desc, rows, d, groups = _norm_desc(x, gate, post, pre, scale, eps, rows_per_gate)
-    big, one = (rows, d), (d,)
-    p = [_dense(x, x, big, "x"), _dense(b, x, big, "b"), _dense(gate, x, (groups, d), "gate"), _dense(post_w, x, one, "post_w"),
-         _dense(post_b, x, one, "post_b"), _dense(pre_w, x, one, "pre_w"), _dense(pre_b, x, one, "pre_b"),
-         _dense(x_out, x, big, "x_out"), _dense(n_out, x, big, "n_out")]
-    with _on(x):
-        _check(l.dn_norm_forward(C.addressof(desc), *p, _stream(x)), "dn_norm_forward")
+    desc, big, one, gates, t, dev = _norm_desc(x, post, pre, scale, eps, rows_per_gate)
+    with _on(dev):
+        _check(l.dn_norm_forward(C.addressof(desc), _dense(x, t, dev, big, "x"), _dense(b, t, dev, big, "b"),
+                                 _dense(gate, t, dev, gates, "gate"), _dense(post_w, t, dev, one, "post_w"),
+                                 _dense(post_b, t, dev, one, "post_b"), _dense(pre_w, t, dev, one, "pre_w"),
+                                 _dense(pre_b, t, dev, one, "pre_b"), _dense(x_out, t, dev, big, "x_out"),
+                                 _dense(n_out, t, dev, big, "n_out"), _stream(dev)), "dn_norm_forward")
 
 
 def dn_norm_backward(x, b, gate, post_w, post_b, pre_w, dx_out, dn, dx, db, dgate, dpost_w, dpost_b, dpre_w, dpre_b,
@@ -550,28 +553,26 @@ def dn_norm_backward(x, b, gate, post_w, post_b, pre_w, dx_out, dn, dx, db, dgat
     like = x if x is not None else dx
     grads = [t for t in (dgate, dpost_w, dpost_b, dpre_w, dpre_b) if t is not None]
     gt, gdtype = _grad_type(grads[0] if grads else None, like)
-    desc, rows, d, groups = _norm_desc(like, gate, post, pre, scale, eps, rows_per_gate, gt)
-    big, one = (rows, d), (d,)
-    p = [_dense(x, like, big, "x"), _dense(b, like, big, "b"), _dense(gate, like, (groups, d), "gate"),
-         _dense(post_w, like, one, "post_w"), _dense(post_b, like, one, "post_b"), _dense(pre_w, like, one, "pre_w"),
-         _dense(dx_out, like, big, "dx_out"), _dense(dn, like, big, "dn"), _dense(dx, like, big, "dx"), _dense(db, like, big, "db"),
-         _dense(dgate, like, (groups, d), "dgate", gdtype), _dense(dpost_w, like, one, "dpost_w", gdtype),
-         _dense(dpost_b, like, one, "dpost_b", gdtype), _dense(dpre_w, like, one, "dpre_w", gdtype),
-         _dense(dpre_b, like, one, "dpre_b", gdtype)]
-    with _on(like):
+    desc, big, one, gates, t, dev = _norm_desc(like, post, pre, scale, eps, rows_per_gate, gt)
+    p = [_dense(v, t, dev, s, n) for v, s, n in ((x, big, "x"), (b, big, "b"), (gate, gates, "gate"), (post_w, one, "post_w"),
+                                                 (post_b, one, "post_b"), (pre_w, one, "pre_w"), (dx_out, big, "dx_out"),
+                                                 (dn, big, "dn"), (dx, big, "dx"), (db, big, "db"))]
+    p += [_dense(v, gdtype, dev, s, n) for v, s, n in ((dgate, gates, "dgate"), (dpost_w, one, "dpost_w"), (dpost_b, one, "dpost_b"),
+                                                       (dpre_w, one, "dpre_w"), (dpre_b, one, "dpre_b"))]
+    with _on(dev):
         at = C.addressof(desc)
-        _keep, ws, n = _workspace(l.dn_norm_backward_workspace_bytes(at), workspace, like, "dn_norm_backward")
-        _check(l.dn_norm_backward(at, *p, ws, n, _stream(like)), "dn_norm_backward")
+        _keep, ws, n = _workspace(l.dn_norm_backward_workspace_bytes(at), workspace, like)
+        _check(l.dn_norm_backward(at, *p, ws, n, _stream(dev)), "dn_norm_backward")
 
 
 def dn_dropout(X, Y, drop: float, seed: int, offset: int = 0):
     """Y = D(X), forward and backward alike; Y may be X, rows of either may lie apart."""
     kind = _type_of(X, "X")
-    rows, cols = _two(X, "X")
-    x, ldx = _matrix(X, X, rows, cols, "X")
-    y, ldy = _matrix(Y, X, rows, cols, "Y")
-    with _on(X):
-        _check(lib().dn_dropout(kind, x, y, rows, cols, ldx, ldy, float(drop), int(seed), int(offset), _stream(X)), "dn_dropout")
+    shape, dev = _two(X, "X"), X.get_device()
+    x, ldx = _matrix(X, X.dtype, dev, shape, "X")
+    y, ldy = _matrix(Y, X.dtype, dev, shape, "Y")
+    with _on(dev):
+        _check(lib().dn_dropout(kind, x, y, shape[0], shape[1], ldx, ldy, drop, seed, offset, _stream(dev)), "dn_dropout")
 
 
 class Net:
