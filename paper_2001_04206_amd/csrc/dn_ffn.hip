@@ -168,11 +168,11 @@ dn_status gated_of(const dn_ffn_desc *d, Gated &g)
     g.ldh = up8(d->f);
     if (2 * g.ldh * e > kRowBytes) return DN_ERR_SHAPE;
     g.h = up256((size_t)d->rows * (size_t)(g.ldh * e));
-    const size_t packed = packed_bytes(d->type, d->rows, d->d) + 2 * packed_bytes(d->type, d->f, d->d) + packed_bytes(d->type, d->d, d->f);
+    const size_t ups = packed_bytes(d->type, d->rows, d->d) + 2 * packed_bytes(d->type, d->f, d->d), packed = ups + packed_bytes(d->type, d->d, d->f);
     g.up = plan_product(d->type, P_FWD, E_GATED, d->rows, d->f, d->d, 1, false);
     g.down = plan_product(d->type, P_FWD, E_LINEAR, d->rows, d->d, d->f, 1, false);
     g.fwd_part = up256(g.up.ws_bytes > g.down.ws_bytes ? g.up.ws_bytes : g.down.ws_bytes);
-    g.fwd_bytes = g.h + (g.up.kernel == K_FEW ? 0 : g.fwd_part + packed);
+    g.fwd_bytes = g.h + g.fwd_part + (g.up.kernel == K_FEW ? 0 : ups) + (g.down.kernel == K_FEW ? 0 : packed - ups);
     g.dh = plan_product(d->type, P_DELTA, E_DGATED, d->rows, d->f, d->d, 1, false);
     g.dx = plan_product(d->type, P_DELTA, E_STORE, d->rows, d->d, d->f, 2, false);
     g.dwgu = plan_product(d->type, P_GRAD, E_STORE, (int)(2 * g.ldh), d->d, d->rows, 1, true);
@@ -211,7 +211,8 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
     ProductPlan plan;
     const int bk = type == DN_F32 ? 32 : 64, steps = (K + bk - 1) / bk * segments;
     plan.steps = steps;
-    if (p == P_FWD && M <= 16) {
+    const bool few = p == P_FWD && M <= kFewRows && (int64_t)K * size_of(type) >= 32;
+    if (few && M <= 16) {
         plan.kernel = K_FEW;
         return plan;
     }
@@ -220,14 +221,14 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
     // bound by its matrix instruction at any size, 3.6 us for two tiles of 128 x 128 on every compute unit.  2048 x 4096 x 1024 so
     // takes 20 us on 256 medium tiles (128 large ones: 32), 8192 x 4096 x 4096 260 on 512 large ones (medium: 330).  Weights come
     // at 4.6 TB/s, and up to 64 rows the kernel that stages nothing competes, whose workgroups of 16 columns each read all rows,
-    // at 11 TB/s: through a gated product of 4096 x 8192 x 2, 8 rows take 33 us there (tiles: 35), 32 rows 42 (tiles: 35), 64 rows
+    // at 11 TB/s: through a gated product of 4096 x 8192 x 2, 8 rows take 29 us there (tiles: 35), 32 rows 42 (tiles: 35), 64 rows
     // 58 (tiles: 37).  Up to 16 rows it is taken without asking.  Tiles at widths that are no multiple of 16 bytes need a copy
     // first.
     const int planes = e == E_GATED ? 2 : 1;
     const double es = (double)size_of(type), weights = es * planes * N * K * segments / 4.6e6;
     double best = 1e300;
     const double copies = (int64_t)K * size_of(type) % 16 == 0 ? 0 : 4 + 2 * (weights + es * M * K / 4.6e6);
-    if (p == P_FWD && M <= kFewRows) {
+    if (few) {
         best = 6 + weights + (N + 15) / 16 * ((M + 15) / 16 * 16.) * K * es / 11e6 - copies;
         plan.kernel = K_FEW;
     }
@@ -402,20 +403,20 @@ dn_status dn_ffn_forward(const dn_ffn_desc *d, const void *X_dev, const void *Wg
     const int64_t e = size_of(d->type);
     char *H = static_cast<char *>(workspace_dev);
     ProductArgs a{}, b{};
+    Packer pack{d->type, H + g.h + g.fwd_part};
     if (g.up.kernel == K_FEW) {
         operand_a(a, {X_dev, g.d.ldx * e, d->d});
         operand_b(a, {Wg_dev, d->d * e, d->d});
         a.b[1] = Wu_dev;
-        operand_b(b, {Wd_dev, d->f * e, d->f});
     } else {
-        Packer pack{d->type, H + g.h + g.fwd_part};
         operand_a(a, pack.take(X_dev, g.d.ldx, d->rows, d->d));
         const bool both = !pieces(d->type, Wg_dev, d->d, d->d) || !pieces(d->type, Wu_dev, d->d, d->d);   // they share a stride
         operand_b(a, pack.take(Wg_dev, d->d, d->f, d->d, both));
         a.b[1] = pack.take(Wu_dev, d->d, d->f, d->d, both).p;
-        operand_b(b, pack.take(Wd_dev, d->f, d->d, d->f));
-        if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
     }
+    if (g.down.kernel == K_FEW) operand_b(b, {Wd_dev, d->f * e, d->f});
+    else operand_b(b, pack.take(Wd_dev, d->f, d->d, d->f));
+    if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
     a.M = d->rows;
     a.N = d->f;
     a.K = d->d;
