@@ -243,8 +243,8 @@ struct PackArgs {
     int32_t n;
     int64_t groups;
 };
-hipError_t launch_pack(int type, const PackArgs &a, hipStream_t s);
-hipError_t launch_mask(int type, const MaskArgs &a, hipStream_t s);
+// either or both; `a` may be NULL, and `p` may hold none
+hipError_t launch_mask_pack(int type, const MaskArgs *a, const PackArgs &p, hipStream_t s);
 
 // ---- norms ------------------------------------------------------------------------------------------------------
 struct NormArgs {

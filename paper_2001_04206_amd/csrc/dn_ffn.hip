@@ -96,7 +96,7 @@ struct Packer {
         at += packed_bytes(type, rows, cols);
         return {m.y, up8(cols) * size_of(type), (int32_t)up8(cols)};
     }
-    hipError_t run(hipStream_t s) const { return a.n ? launch_pack(type, a, s) : hipSuccess; }
+    hipError_t run(hipStream_t s, const MaskArgs *mask = nullptr) const { return launch_mask_pack(type, mask, a, s); }
 };
 void operand_a(ProductArgs &a, const Packer::Rows &r)
 {
@@ -328,9 +328,10 @@ dn_status dn_linear_backward(const dn_linear_desc *d, const void *X_dev, const v
     char *ws = static_cast<char *>(workspace_dev);
     // delta, without dropout's scale, by which the products' sums are multiplied; dY itself where it is that and lies well
     Packer::Rows delta{dY_dev, l.d.ldy * e, d->n_out};
-    if (d->act != DN_ACT_LINEAR || l.drop.t || !pieces(d->type, dY_dev, l.d.ldy, d->n_out)) {
+    const bool mask = d->act != DN_ACT_LINEAR || l.drop.t || !pieces(d->type, dY_dev, l.d.ldy, d->n_out);
+    MaskArgs m{};
+    if (mask) {
         const int64_t ld = up8(d->n_out);
-        MaskArgs m{};
         m.x = dY_dev;
         m.z = Z_dev;
         m.y = ws;
@@ -343,13 +344,12 @@ dn_status dn_linear_backward(const dn_linear_desc *d, const void *X_dev, const v
         m.act = d->act;
         m.drop = l.drop;
         m.drop.scale = 1.f;
-        if (launch_mask(d->type, m, stream) != hipSuccess) return DN_ERR_DEVICE;
         delta = {ws, ld * e, (int32_t)ld};
     }
     Packer pack{d->type, ws + l.delta + l.bwd_part};
     const Packer::Rows X = dW_dev ? pack.take(X_dev, l.d.ldx, d->rows, d->n_in) : Packer::Rows{};
     const Packer::Rows W = dX_dev ? pack.take(W_dev, l.d.ldw, d->n_out, d->n_in) : Packer::Rows{};
-    if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    if (pack.run(stream, mask ? &m : nullptr) != hipSuccess) return DN_ERR_DEVICE;
     ProductArgs a{};
     a.segments = 1;
     a.ws = reinterpret_cast<float *>(ws + l.delta);
@@ -467,9 +467,10 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
     // dZ without dropout's scale, by which the sums of the two products that read it are multiplied; dY itself where it is that
     // and lies well
     Packer::Rows dZ{dY_dev, g.d.ldy * e, d->d};
-    if (g.drop.t || !pieces(d->type, dY_dev, g.d.ldy, d->d)) {
+    const bool mask = g.drop.t || !pieces(d->type, dY_dev, g.d.ldy, d->d);
+    MaskArgs m{};
+    if (mask) {
         const int64_t ld = up8(d->d);
-        MaskArgs m{};
         m.x = dY_dev;
         m.y = ws + g.h + g.dgu;
         m.ldx = g.d.ldy;
@@ -480,7 +481,6 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
         m.act = -1;
         m.drop = g.drop;
         m.drop.scale = 1.f;
-        if (launch_mask(d->type, m, stream) != hipSuccess) return DN_ERR_DEVICE;
         dZ = {m.y, ld * e, (int32_t)ld};
     }
     Packer pack{d->type, ws + g.h + g.dgu + g.dz + g.bwd_part};
@@ -488,7 +488,7 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
     const bool both = !pieces(d->type, Wg_dev, d->d, d->d) || !pieces(d->type, Wu_dev, d->d, d->d);   // they share a stride
     const Packer::Rows Wg = dX_dev ? pack.take(Wg_dev, d->d, f, d->d, both) : Packer::Rows{};
     const Packer::Rows Wu = dX_dev ? pack.take(Wu_dev, d->d, f, d->d, both) : Packer::Rows{};
-    if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    if (pack.run(stream, mask ? &m : nullptr) != hipSuccess) return DN_ERR_DEVICE;
     float *part = reinterpret_cast<float *>(ws + g.h + g.dgu + g.dz);
     const bool f32_out = d->grad_type == DN_F32;
     {   // dH, and from it dG, dU and H
@@ -646,7 +646,7 @@ dn_status dn_dropout(int32_t type, const void *X_dev, void *Y_dev, int32_t rows,
     m.rows = rows;
     m.cols = cols;
     m.act = -1;
-    return device(launch_mask(type, m, (hipStream_t)hip_stream));
+    return device(launch_mask_pack(type, &m, {}, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

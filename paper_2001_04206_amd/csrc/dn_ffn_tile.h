@@ -584,32 +584,42 @@ __global__ __launch_bounds__(256) void sum_join_kernel(const ProductArgs a)
     finish_sum<T>(a.f, m, v);
 }
 
-// The parts of a product whose k was split, added in order, and its epilogue.  A thread takes eight columns of one row.
+// The parts of a product whose k was split, added in order, and its epilogue.  A thread takes eight columns of one row, four parts
+// loaded at a time.
 template <class T, int EPI>
 __global__ __launch_bounds__(256) void join_kernel(const ProductArgs a, int sums)
 {
-    constexpr int PLANES = EPI == E_GATED ? 2 : 1;
-    const int eights = (a.N + 7) / 8;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, plane = (int64_t)a.M * a.N;
-    if (at < (int64_t)a.M * eights) {
-        const int m = (int)(at / eights), n = (int)(at % eights) * 8;
-        float v[8] = {}, w[8] = {};
-        for (int s = 0; s < a.split; ++s) {
-            const float *p = a.ws + s * plane * PLANES;
-            float x[8];
-            load8<float>(x, p, (int64_t)m * a.N + n, a.N - n);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += x[j];
-            if (PLANES == 2) {
-                load8<float>(x, p + plane, (int64_t)m * a.N + n, a.N - n);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] += x[j];
-            }
-        }
+    constexpr int PLANES = EPI == E_GATED ? 2 : 1, AT_ONCE = 4;
+    // the workgroup's first eight columns by one uniform division, the thread's by a short one
+    const uint32_t eights = ((uint32_t)a.N + 7) / 8;
+    const int64_t first = (int64_t)blockIdx.x * 256, plane = (int64_t)a.M * a.N;
+    const uint32_t row0 = (uint32_t)((uint64_t)first / eights), c0 = (uint32_t)((uint64_t)first % eights) + threadIdx.x, more = c0 / eights;
+    const int64_t row = (int64_t)row0 + more;
+    if (row < a.M) {
+        const int m = (int)row, n = (int)(c0 - more * eights) * 8;
         Beside<T, EPI> side;
         side.template get<false>(a.f, m, n, a.N - n);
+        float v[8] = {}, w[8] = {};
+        const float *p = a.ws + row * a.N + n;
+        for (int s = 0; s < a.split; s += AT_ONCE) {
+            float x[AT_ONCE][PLANES][8] = {};
+#pragma unroll
+            for (int q = 0; q < AT_ONCE; ++q)
+                if (s + q < a.split) {
+#pragma unroll
+                    for (int c = 0; c < PLANES; ++c) load8<float>(x[q][c], p, ((int64_t)(s + q) * PLANES + c) * plane, a.N - n);
+                }
+#pragma unroll
+            for (int q = 0; q < AT_ONCE; ++q)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] += x[q][0][j];
+                    w[j] += x[q][PLANES - 1][j];
+                }
+        }
         finish8<T, EPI, false>(a.f, side, m, n, a.N - n, v, w);
     }
+    const int64_t at = first + threadIdx.x;
     if (EPI == E_STORE && sums && at < a.M) {
         float v = 0.f;
         for (int s = 0; s < a.split; ++s) v += a.ws[a.split * plane + (int64_t)s * a.M + at];

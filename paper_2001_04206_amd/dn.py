@@ -346,14 +346,14 @@ def dn_sgd_step(param, grad, velocity, lr: float, momentum: float):
 # ---- the residual feed-forward block -----------------------------------------------------------------------------
 
 _TYPES = {}     # torch.dtype -> dn_type
-_torch = None
+_torch = _raw_stream = None
 
 
 def _type_of(t, what: str) -> int:
-    global _torch
+    global _torch, _raw_stream
     if _torch is None:
         import torch
-        _torch = torch
+        _torch, _raw_stream = torch, getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _TYPES.update({torch.float32: DN_F32, torch.float16: DN_F16, torch.bfloat16: DN_BF16})
     kind = _TYPES.get(getattr(t, "dtype", None))
     if kind is None or not t.is_cuda:
@@ -427,7 +427,8 @@ def _on(dev: int):
 
 
 def _stream(dev: int) -> int:
-    return _torch.cuda.current_stream(dev).cuda_stream
+    # torch's own short way to current_stream(dev).cuda_stream, a microsecond less, where it has it
+    return _raw_stream(dev) if _raw_stream else _torch.cuda.current_stream(dev).cuda_stream
 
 
 def _two(t, what: str):
