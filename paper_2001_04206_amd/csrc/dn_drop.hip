@@ -20,14 +20,11 @@ __device__ __forceinline__ void mask8(const MaskArgs &a, uint32_t eights)
     float v[8];
     load8<T>(v, a.x, m * a.ldx + n, left);
     if (a.act > DN_ACT_LINEAR) {
-        float z[8];
+        float z[8], f[8], df[8];
         load8<T>(z, a.z, m * a.ldz + n, left);
+        act8<sizeof(T) == 2>(a.act, z, f, df);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float f, df;
-            act_both<sizeof(T) == 2>(a.act, z[j], f, df);
-            v[j] *= df;
-        }
+        for (int j = 0; j < 8; ++j) v[j] *= df[j];
     }
     if (a.drop.t) drop8(a.drop, (int)m, n, v);
     store8<T>(a.y, m * a.ldy + n, v, left + a.zeros);

@@ -121,48 +121,52 @@ template <> struct Math<true> {
 };
 
 // f(z), and f'(z) with it
-template <bool FAST>
-__device__ __forceinline__ void act_both(int act, float z, float &f, float &df)
+template <int ACT, bool FAST>
+__device__ __forceinline__ void act_one(float z, float &f, float &df)
 {
     typedef Math<FAST> K;
-    switch (act) {
-    case DN_ACT_SIGMOID:
+    if (ACT == DN_ACT_SIGMOID) {
         f = K::inv(1.f + K::exp(-z));
         df = f * (1.f - f);
-        break;
-    case DN_ACT_TANH:
+    } else if (ACT == DN_ACT_TANH) {
         f = K::tanh(z);
         df = 1.f - f * f;
-        break;
-    case DN_ACT_RELU:   // a comparison that a NaN fails would hide it
+    } else if (ACT == DN_ACT_RELU) {   // a comparison that a NaN fails would hide it
         f = z < 0.f ? 0.f : z;
         df = z > 0.f ? 1.f : 0.f;
-        break;
-    case DN_ACT_SILU: {
+    } else if (ACT == DN_ACT_SILU) {
         const float s = K::inv(1.f + K::exp(-z));
         const bool far = fabsf(z) > 1e4f;   // where s is 0 or 1: inf * 0
         f = far && z < 0.f ? 0.f : z * s;
         df = far ? s : s * (1.f + z * (1.f - s));
-        break;
-    }
-    case DN_ACT_GELU: {
+    } else if (ACT == DN_ACT_GELU) {
         float c, p;
         K::normal(z, c, p);
         f = z < -30.f ? 0.f : z * c;
         df = fabsf(z) > 30.f ? c : c + z * p;   // inf * 0
-        break;
-    }
-    default:
+    } else {
         f = z;
         df = 1.f;
     }
 }
-template <bool FAST>
-__device__ __forceinline__ float act_value(int act, float z)
+// of eight, the choice made once for all
+template <int ACT, bool FAST>
+__device__ __forceinline__ void act_each(const float (&z)[8], float (&f)[8], float (&df)[8])
 {
-    float f, df;
-    act_both<FAST>(act, z, f, df);
-    return f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) act_one<ACT, FAST>(z[j], f[j], df[j]);
+}
+template <bool FAST>
+__device__ __forceinline__ void act8(int act, const float (&z)[8], float (&f)[8], float (&df)[8])
+{
+    switch (act) {
+    case DN_ACT_SIGMOID: act_each<DN_ACT_SIGMOID, FAST>(z, f, df); break;
+    case DN_ACT_TANH: act_each<DN_ACT_TANH, FAST>(z, f, df); break;
+    case DN_ACT_RELU: act_each<DN_ACT_RELU, FAST>(z, f, df); break;
+    case DN_ACT_SILU: act_each<DN_ACT_SILU, FAST>(z, f, df); break;
+    case DN_ACT_GELU: act_each<DN_ACT_GELU, FAST>(z, f, df); break;
+    default: act_each<DN_ACT_LINEAR, FAST>(z, f, df);
+    }
 }
 
 // ---- matrix products ---------------------------------------------------------------------------------------------

@@ -120,6 +120,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_kernel(const ProductArgs a)
     const int t = threadIdx.x, m = t >> 1, n = n0 + 8 * (t & 1);
     if (t >= 32 * MB || m >= a.M || n >= a.N) return;
     Beside<T, EPI> side;
+    side.template columns<false>(a.f, n, a.N - n);
     side.template get<false>(a.f, m, n, a.N - n);
     float v[8] = {}, u[8] = {};
 #pragma unroll 4
@@ -232,6 +233,7 @@ __global__ __launch_bounds__(256) void token_kernel(const ProductArgs a)
         u[j] = share[PLANES - 1][m][j];
     }
     Beside<T, EPI> side;
+    side.template columns<false>(a.f, n0, a.N - n0);
     side.template get<false>(a.f, m, n0, a.N - n0);
     finish8<T, EPI, false>(a.f, side, m, n0, a.N - n0, v, u);
 }

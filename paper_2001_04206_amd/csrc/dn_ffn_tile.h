@@ -75,7 +75,14 @@ __device__ __forceinline__ float add_all(const v4u &a, float c, float)
 // finish8 so that a thread's reads of several rows can be under way together.  ALL: all eight columns exist.
 template <class T, int EPI>
 struct Beside {
-    typename Eight<T>::type r, u;
+    typename Eight<T>::type r, u;    // a row's
+    typename Eight<T>::type b, b2;   // its columns'
+    template <bool ALL>
+    __device__ __forceinline__ void columns(const Finish &e, int n, int left)
+    {
+        if ((EPI == E_LINEAR || EPI == E_GATED) && e.bias) b = get8<T, ALL>(e.bias, n, left);
+        if (EPI == E_GATED && e.bias2) b2 = get8<T, ALL>(e.bias2, n, left);
+    }
     template <bool ALL>
     __device__ __forceinline__ void get(const Finish &e, int m, int n, int left)
     {
@@ -93,51 +100,46 @@ __device__ __forceinline__ void finish8(const Finish &e, const Beside<T, EPI> &s
 {
     constexpr bool FAST = sizeof(T) == 2;
     if constexpr (EPI == E_LINEAR) {
-        if (e.bias) {
-            float b[8];
-            load8<T, ALL>(b, e.bias, n, left);
+        if (e.bias)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += b[j];
-        }
+            for (int j = 0; j < 8; ++j) v[j] += (float)side.b[j];
         if (e.y2) store8<T, ALL>(e.y2, m * e.ldy2 + n, v, left);
-        if (e.act != DN_ACT_LINEAR)
+        float f[8], df[8];
+        act8<FAST>(e.act, v, f, df);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = act_value<FAST>(e.act, v[j]);
+        for (int j = 0; j < 8; ++j) v[j] = f[j];
         if (e.drop.t) drop8(e.drop, m, n, v);
         if (e.r)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += (float)side.r[j];
         store8<T, ALL>(e.y, m * e.ldy + n, v, left);
     } else if constexpr (EPI == E_GATED) {
-        if (e.bias) {
-            float b[8];
-            load8<T, ALL>(b, e.bias, n, left);
+        if (e.bias)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += b[j];
-        }
-        if (e.bias2) {
-            float b[8];
-            load8<T, ALL>(b, e.bias2, n, left);
+            for (int j = 0; j < 8; ++j) v[j] += (float)side.b[j];
+        if (e.bias2)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] += b[j];
-        }
+            for (int j = 0; j < 8; ++j) w[j] += (float)side.b2[j];
         if (e.y2) {
             store8<T, ALL>(e.y2, m * e.ldy2 + n, v, left);
             store8<T, ALL>(e.y2, m * e.ldy2 + n + e.half, w, left);
         }
+        float f[8], df[8];
+        act8<FAST>(e.act, v, f, df);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = !ALL && j >= left ? 0.f : act_value<FAST>(e.act, v[j]) * w[j];
+        for (int j = 0; j < 8; ++j) v[j] = !ALL && j >= left ? 0.f : f[j] * w[j];
         store8<T, ALL>(e.y, m * e.ldy + n, v, left + e.zeros);
     } else if constexpr (EPI == E_DGATED) {
-        float h[8];
+        float g[8], f[8], df[8], h[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = (float)side.r[j];
+        act8<FAST>(e.act, g, f, df);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float f, df;
-            act_both<FAST>(e.act, (float)side.r[j], f, df);
             v[j] *= e.alpha;
-            w[j] = v[j] * f;
-            v[j] *= (float)side.u[j] * df;
-            h[j] = (float)side.u[j] * f;
+            w[j] = v[j] * f[j];
+            v[j] *= (float)side.u[j] * df[j];
+            h[j] = (float)side.u[j] * f[j];
             if (!ALL && j >= left) v[j] = w[j] = h[j] = 0.f;
         }
         store8<T, ALL>(e.y, m * e.ldy + n, v, left + e.zeros);
@@ -507,6 +509,16 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     };
     constexpr int STEP = 64 / LANES, TOGETHER = EPI == E_GATED ? 2 : 4;   // rows apart; rows whose reads go together
     const bool whole = m0 + S::BM <= a.M && n0 + COLS <= a.N && a.split == 1;
+    // what lies beside the result: the columns' once, the rows' a round ahead
+    Beside<T, EPI> next[TOGETHER];
+    if (whole) next[0].template columns<true>(a.f, n, 8);
+    else if (a.split == 1) next[0].template columns<false>(a.f, n, a.N - n);
+#pragma unroll
+    for (int q = 0; q < TOGETHER; ++q) {
+        next[q].b = next[0].b;
+        next[q].b2 = next[0].b2;
+        if (whole) next[q].template get<true>(a.f, row0 + lane / LANES + q * STEP, n, 8);
+    }
 #pragma unroll
     for (int i0 = 0; i0 < S::TM; i0 += 4) {
 #pragma unroll
@@ -519,8 +531,12 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
 #pragma unroll 1
             for (int r = lane / LANES; r < 64; r += STEP * TOGETHER) {
                 Beside<T, EPI> side[TOGETHER];
+                const int after = min(first + r + STEP * TOGETHER, row0 + S::TM * 16 - STEP * TOGETHER + lane / LANES);
 #pragma unroll
-                for (int q = 0; q < TOGETHER; ++q) side[q].template get<true>(a.f, first + r + q * STEP, n, 8);
+                for (int q = 0; q < TOGETHER; ++q) {
+                    side[q] = next[q];
+                    next[q].template get<true>(a.f, after + q * STEP, n, 8);
+                }
 #pragma unroll
                 for (int q = 0; q < TOGETHER; ++q) {
                     float v[8], w[8];
@@ -539,9 +555,8 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
                     store8<float>(part, (int64_t)m * a.N + n, v, a.N - n);
                     if (PAIR) store8<float>(part, plane + (int64_t)m * a.N + n, w, a.N - n);
                 } else {
-                    Beside<T, EPI> side;
-                    side.template get<false>(a.f, m, n, a.N - n);
-                    finish8<T, EPI, false>(a.f, side, m, n, a.N - n, v, w);
+                    next[0].template get<false>(a.f, m, n, a.N - n);
+                    finish8<T, EPI, false>(a.f, next[0], m, n, a.N - n, v, w);
                 }
             }
         }
@@ -598,6 +613,7 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs a, int sums
     if (row < a.M) {
         const int m = (int)row, n = (int)(c0 - more * eights) * 8;
         Beside<T, EPI> side;
+        side.template columns<false>(a.f, n, a.N - n);
         side.template get<false>(a.f, m, n, a.N - n);
         float v[8] = {}, w[8] = {};
         const float *p = a.ws + row * a.N + n;
