@@ -403,7 +403,7 @@ dn_status dn_cnn_train_epoch(dn_cnn *net, const float *X_dev, const int32_t *lab
  * two products (the gated hidden layer, its deltas) is rounded to `type` as the caller's own tensors are.
  *
  * Tensors are row-major device memory of the caller's, rows of X, W, R, Y and dY any distance apart (ld*, in elements; 0:
- * contiguous), everything else contiguous.  Any alignment of an element will do; operands of more than 64 rows whose rows
+ * contiguous), everything else contiguous.  Any alignment of an element will do; operands of more than 16 rows whose rows
  * do not lie at multiples of 16 bytes and end at some are copied to the workspace first.  A result may be the residual itself (Y = R), no other two
  * tensors of a call may overlap.
  * Workspaces: device memory, 256-byte aligned, as many bytes as the query says (0: none, NULL will do); the query returns

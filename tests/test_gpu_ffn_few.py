@@ -70,3 +70,30 @@ def test_not_finite_past_the_end_of_a_row():
             Y = torch.full((rows, 24), float("nan"), dtype=dtype, device=DEV)
             dn.dn_linear_forward(wide[:, :37], weights[:, :37], None, None, Y, act=ACTS["linear"])
             assert (Y == 18.5).all()
+
+
+@pytest.mark.parametrize("rows", [1, 20, 64, 200])
+@pytest.mark.parametrize("kind", TYPES)
+def test_tensors_that_begin_anywhere(kind, rows):
+    """Every tensor one element past a multiple of 16 bytes, with rows whose lengths are such multiples."""
+    announce("tensors that begin anywhere %s %d" % (kind, rows))
+    dtype, make, t = block(kind, (rows, 128, 256), "silu", True, 0.0, 0)
+
+    def shift(v):
+        flat = torch.full((v.numel() + 2,), float("nan"), dtype=v.dtype, device=DEV)
+        flat[1:-1] = v.flatten()
+        return flat, flat[1:-1].view(v.shape)
+
+    s = {k: shift(v)[1] for k, v in t.items() if v is not None}
+    (whole, Y), (_, GU) = shift(make.out(rows, 128)), shift(make.out(rows, 512))
+    dn.dn_ffn_forward(s["X"], s["Wg"], s["bg"], s["Wu"], s["bu"], s["Wd"], s["bd"], s["R"], Y, GU)
+    w = {k: v.double() for k, v in t.items() if v is not None}
+    g, u = w["X"] @ w["Wg"].t() + w["bg"], w["X"] @ w["Wu"].t() + w["bu"]
+    close(Y, (f64(g, "silu").to(DEV) * u) @ w["Wd"].t() + w["bd"] + w["R"], tolerance(dtype, 384, 2), "Y")
+    close(GU, torch.cat((g, u), 1), tolerance(dtype, 128), "GU")
+    assert whole[0].isnan() and whole[-1].isnan()
+    dX, dW = shift(make.out(rows, 128))[1], [shift(make.out(*t[k].shape))[1] for k in ("Wg", "Wu", "Wd")]
+    dn.dn_ffn_backward(s["X"], s["Wg"], s["Wu"], s["Wd"], s["GU"], s["dY"], dX, dW[0], None, dW[1], None, dW[2], None)
+    same, sameW = make.out(rows, 128), [make.out(*t[k].shape) for k in ("Wg", "Wu", "Wd")]
+    dn.dn_ffn_backward(t["X"], t["Wg"], t["Wu"], t["Wd"], t["GU"], t["dY"], same, sameW[0], None, sameW[1], None, sameW[2], None)
+    assert torch.equal(dX, same) and all(torch.equal(a, b) for a, b in zip(dW, sameW))   # copied to where the other lies: the same sums
