@@ -71,6 +71,9 @@ hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
     case K_SMALL:
         if constexpr (sizeof(T) == 4) e = tiles<T, P, EPI, Small>(a, sums, s);
         break;
+    case K_TINY:
+        if constexpr (sizeof(T) == 4) e = tiles<T, P, EPI, Tiny>(a, sums, s);
+        break;
     case K_MEDIUM:
         if constexpr (sizeof(T) == 2) e = tiles<T, P, EPI, Medium>(a, sums, s);
         break;

@@ -355,6 +355,7 @@ struct Shape {
 typedef Shape<2, 4, 8, 4, 2> Large;    // 256 x 256, 8 waves
 typedef Shape<2, 4, 4, 4, 3> Medium;   // 128 x 256, 8 waves; the third stage makes up for the shorter time of one
 typedef Shape<2, 2, 4, 4, 2> Small;    // 128 x 128, 4 waves, two workgroups a compute unit
+typedef Shape<2, 2, 2, 4, 2> Tiny;     // 64 x 128, 4 waves, three
 
 template <class T, int P, int EPI, class S, bool SUMS>
 __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs a)
@@ -467,7 +468,7 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     }
     arrived<0>();
 
-    // Epilogue.  A wave turns its sums through its own 16 KB of LDS, sixty-four rows at a time, so that a lane gets eight
+    // Epilogue.  A wave turns its sums through its own 16 KB of LDS, sixty-four rows (or all it has) at a time, so that a lane gets eight
     // neighbouring columns of a row: rows of 256 bytes, their 16-byte units u at u ^ (row mod 16).
     const int i16 = lane & 15, h = lane >> 4;
     const int64_t plane = (int64_t)a.M * a.N;
@@ -485,8 +486,9 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
         }
     float *part = a.ws + blockIdx.y * plane * (PAIR ? 2 : 1);
     constexpr int EACH_STAGE = (S::NW + S::NB - 1) / S::NB;   // waves
-    static_assert(EACH_STAGE * 16384 <= A_BYTES + OpB::STAGE, "a wave's 16 KB");
-    char *own = (wave < EACH_STAGE ? stage0 : wave < 2 * EACH_STAGE ? stage1 : stage2) + wave % EACH_STAGE * 16384;
+    constexpr int BLOCKS = S::TM < 4 ? S::TM : 4, ROWS = BLOCKS * 16;   // at a time
+    static_assert(EACH_STAGE * ROWS * 256 <= A_BYTES + OpB::STAGE, "a wave's own part of a stage");
+    char *own = (wave < EACH_STAGE ? stage0 : wave < 2 * EACH_STAGE ? stage1 : stage2) + wave % EACH_STAGE * ROWS * 256;
     constexpr int LANES = PAIR ? 4 : 8;   // of a row
     const int c = lane % LANES, n = n0 + wn * (PAIR ? 32 : 64) + c * 8;
     static_assert(S::TN == 4, "a wave's 64 columns");
@@ -520,16 +522,16 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
         if (whole) next[q].template get<true>(a.f, row0 + lane / LANES + q * STEP, n, 8);
     }
 #pragma unroll
-    for (int i0 = 0; i0 < S::TM; i0 += 4) {
+    for (int i0 = 0; i0 < S::TM; i0 += BLOCKS) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j)   // a pair's blocks alternate: those of the first matrix first
                 *unit(i * 16 + i16, (PAIR ? (j >> 1) + (j & 1) * 2 : j) * 4 + h) = acc[i0 + i][j];
         const int first = row0 + i0 * 16;
         if (whole) {
 #pragma unroll 1
-            for (int r = lane / LANES; r < 64; r += STEP * TOGETHER) {
+            for (int r = lane / LANES; r < ROWS; r += STEP * TOGETHER) {
                 Beside<T, EPI> side[TOGETHER];
                 const int after = min(first + r + STEP * TOGETHER, row0 + S::TM * 16 - STEP * TOGETHER + lane / LANES);
 #pragma unroll
@@ -546,7 +548,7 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             }
         } else {
 #pragma unroll 1
-            for (int r = lane / LANES; r < 64; r += STEP) {
+            for (int r = lane / LANES; r < ROWS; r += STEP) {
                 const int m = first + r;
                 if (m >= a.M || n >= a.N) break;
                 float v[8], w[8];
