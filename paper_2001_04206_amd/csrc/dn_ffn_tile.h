@@ -6,6 +6,8 @@
 // lane = 16 h + i: D register r is column 4 h + r, row i.
 #pragma once
 
+#include <type_traits>
+
 #include "dn_ffn.h"
 
 namespace dn {
@@ -509,59 +511,68 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             }
         }
     };
-    constexpr int STEP = 64 / LANES, TOGETHER = EPI == E_GATED ? 2 : 4;   // rows apart; rows whose reads go together
-    const bool whole = m0 + S::BM <= a.M && n0 + COLS <= a.N && a.split == 1;
-    // what lies beside the result: the columns' once, the rows' a round ahead
-    Beside<T, EPI> next[TOGETHER];
-    if (whole) next[0].template columns<true>(a.f, n, 8);
-    else if (a.split == 1) next[0].template columns<false>(a.f, n, a.N - n);
-#pragma unroll
-    for (int q = 0; q < TOGETHER; ++q) {
-        next[q].b = next[0].b;
-        next[q].b2 = next[0].b2;
-        if (whole) next[q].template get<true>(a.f, row0 + lane / LANES + q * STEP, n, 8);
-    }
-#pragma unroll
-    for (int i0 = 0; i0 < S::TM; i0 += BLOCKS) {
+    auto turn = [&](int i0) {
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j)   // a pair's blocks alternate: those of the first matrix first
                 *unit(i * 16 + i16, (PAIR ? (j >> 1) + (j & 1) * 2 : j) * 4 + h) = acc[i0 + i][j];
-        const int first = row0 + i0 * 16;
-        if (whole) {
+    };
+    constexpr int STEP = 64 / LANES;   // rows apart
+    // Sixty-four rows at a time; what lies beside the result is read once for the columns, and a round ahead for the rows.  ALL: the tile
+    // lies inside the result.
+    auto finish = [&](auto all) {
+        constexpr bool ALL = decltype(all)::value;
+        constexpr int TOGETHER = ALL && EPI != E_GATED ? 4 : 2;   // rows whose reads go together
+        const int last = ALL ? row0 + S::TM * 16 - 1 : a.M - 1, left = ALL ? 8 : a.N - n;
+        Beside<T, EPI> next[TOGETHER];
+        next[0].template columns<ALL>(a.f, n, left);
+#pragma unroll
+        for (int q = 0; q < TOGETHER; ++q) {
+            next[q].b = next[0].b;
+            next[q].b2 = next[0].b2;
+            next[q].template get<ALL>(a.f, min(row0 + lane / LANES + q * STEP, last), n, left);
+        }
+#pragma unroll
+        for (int i0 = 0; i0 < S::TM; i0 += BLOCKS) {
+            turn(i0);
+            const int first = row0 + i0 * 16;
 #pragma unroll 1
             for (int r = lane / LANES; r < ROWS; r += STEP * TOGETHER) {
                 Beside<T, EPI> side[TOGETHER];
-                const int after = min(first + r + STEP * TOGETHER, row0 + S::TM * 16 - STEP * TOGETHER + lane / LANES);
 #pragma unroll
                 for (int q = 0; q < TOGETHER; ++q) {
                     side[q] = next[q];
-                    next[q].template get<true>(a.f, after + q * STEP, n, 8);
+                    next[q].template get<ALL>(a.f, min(first + r + (TOGETHER + q) * STEP, last), n, left);
                 }
 #pragma unroll
                 for (int q = 0; q < TOGETHER; ++q) {
+                    const int m = first + r + q * STEP;
                     float v[8], w[8];
                     sums_of(r + q * STEP, v, w);
-                    finish8<T, EPI, true>(a.f, side[q], first + r + q * STEP, n, 8, v, w);
-                }
-            }
-        } else {
-#pragma unroll 1
-            for (int r = lane / LANES; r < ROWS; r += STEP) {
-                const int m = first + r;
-                if (m >= a.M || n >= a.N) break;
-                float v[8], w[8];
-                sums_of(r, v, w);
-                if (a.split > 1) {
-                    store8<float>(part, (int64_t)m * a.N + n, v, a.N - n);
-                    if (PAIR) store8<float>(part, plane + (int64_t)m * a.N + n, w, a.N - n);
-                } else {
-                    next[0].template get<false>(a.f, m, n, a.N - n);
-                    finish8<T, EPI, false>(a.f, next[0], m, n, a.N - n, v, w);
+                    if (ALL || (m < a.M && n < a.N)) finish8<T, EPI, ALL>(a.f, side[q], m, n, left, v, w);
                 }
             }
         }
+    };
+    if (a.split > 1) {
+#pragma unroll
+        for (int i0 = 0; i0 < S::TM; i0 += BLOCKS) {
+            turn(i0);
+#pragma unroll 1
+            for (int r = lane / LANES; r < ROWS; r += STEP) {
+                const int m = row0 + i0 * 16 + r;
+                if (m >= a.M || n >= a.N) break;
+                float v[8], w[8];
+                sums_of(r, v, w);
+                store8<float>(part, (int64_t)m * a.N + n, v, a.N - n);
+                if (PAIR) store8<float>(part, plane + (int64_t)m * a.N + n, w, a.N - n);
+            }
+        }
+    } else if (m0 + S::BM <= a.M && n0 + COLS <= a.N) {
+        finish(std::true_type());
+    } else {
+        finish(std::false_type());
     }
 }
 
