@@ -219,7 +219,7 @@ constexpr int kFewRows = 64;    // most rows of the kernel that stages nothing
 constexpr int kSumParts = 32;   // parts of k that a launch of its own adds A's columns in
 
 // How a product is run.  `ws_bytes`: workspace that it needs.
-enum ProductKernel : int { K_FEW, K_TINY, K_SMALL, K_MEDIUM, K_LARGE };   // K_TINY and K_SMALL: fp32, the other two: 16 bits
+enum ProductKernel : int { K_FEW, K_TINY, K_SMALL, K_MEDIUM, K_LARGE };   // K_TINY: fp32, K_MEDIUM and K_LARGE: 16 bits
 struct ProductPlan {
     ProductKernel kernel = K_SMALL;
     int split = 1, steps = 0;

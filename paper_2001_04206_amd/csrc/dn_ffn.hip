@@ -221,7 +221,9 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
     // Which kernel, and k in how many parts: whichever is expected to take least.  Microseconds a stage, a round of workgroups and
     // bytes, as measured.  A stage of a 256 x 256 tile takes 1.5 us whether the chip is full or not, one of 128 x 256 0.8; fp32 is
     // bound by its matrix instruction at any size, 1.8 us for a tile of 128 x 128 and 0.95 for one of 64 x 128.  2048 x 4096 x 1024
-    // so takes 20 us on 256 medium tiles (128 large ones: 32), 8192 x 4096 x 4096 260 on 512 large ones (medium: 330), and in fp32
+    // so takes 20 us on 256 medium tiles (128 large ones: 32), 8192 x 4096 x 4096 260 on 512 large ones (medium: 330); few short tiles
+    // are better small, more waves sharing their epilogue: 700 x 1024 x 512 11.8 us (medium: 16.2), but 1024 x 2048 x 8192 61 for
+    // the medium ones' 43, as a stage of any tile takes what memory does.  In fp32
     // 1301 x 1021 x 777 32 us on 168 tiny tiles (small ones in parts: 33 and 5 to join them), 8192 x 4096 x 4096 1941 on 2048 small
     // ones (tiny: 1988).  Weights come at 4.6 TB/s, and up to 64 rows the kernel that stages nothing competes, whose workgroups of 16
     // columns each read all rows, at 11 TB/s: through a gated product of 4096 x 8192 x 2, 8 rows take 29 us there (tiles: 35), 32 rows
@@ -235,18 +237,19 @@ ProductPlan plan_product(int type, Product p, Epilogue e, int M, int N, int K, i
         best = 6 + weights + (N + 15) / 16 * ((M + 15) / 16 * 16.) * K * es / 11e6 - copies;
         plan.kernel = K_FEW;
     }
-    struct Way { ProductKernel kernel; int rows, cols, together; double stage, round; };
-    const Way tiny{K_TINY, 64, 128, 3, 0.95, 6}, small{K_SMALL, 128, 128, 2, 1.8, 6};
-    const Way medium{K_MEDIUM, 128, 256, 1, 0.8, 6}, large{K_LARGE, 256, 256, 1, 1.5, 8};
+    struct Way { ProductKernel kernel; int rows, cols, together; double stage, least, round; };   // least: of a stage, when alone
+    const Way tiny{K_TINY, 64, 128, 3, 0.95, 0.95, 6}, large{K_LARGE, 256, 256, 1, 1.5, 1.5, 8}, medium{K_MEDIUM, 128, 256, 1, 0.8, 0.8, 6};
+    const Way small = type == DN_F32 ? Way{K_SMALL, 128, 128, 2, 1.8, 1.8, 6} : Way{K_SMALL, 128, 128, 2, 0.5, 0.9, 4};
     for (const Way &w : {large, medium, small, tiny}) {
-        if ((w.kernel <= K_SMALL) != (type == DN_F32)) continue;
+        if (type == DN_F32 ? w.kernel > K_SMALL : w.kernel == K_TINY) continue;
         const int64_t cols = w.cols / planes, t = (M + w.rows - 1) / w.rows * ((N + cols - 1) / cols);
         for (int split = 1; split <= 32 && split * 4 <= steps + 3; ++split) {
             int each = (steps + split - 1) / split;
             if (w.kernel == K_LARGE) each = (each + 1) / 2 * 2;
             const int parts = (steps + each - 1) / each;
-            const int64_t deep = (t * parts + kUnits - 1) / kUnits;   // tiles on a compute unit
-            double us = (double)deep * each * w.stage + (double)((deep + w.together - 1) / w.together) * w.round;
+            const int64_t deep = (t * parts + kUnits - 1) / kUnits, rounds = (deep + w.together - 1) / w.together;   // on a compute unit
+            const double stage = deep * w.stage > rounds * w.least ? deep * w.stage : rounds * w.least;
+            double us = each * stage + rounds * w.round;
             if (p == P_FWD && us < weights) us = weights;
             if (parts > 1) us += 3 + 8e-6 * parts * planes * M * N / 4.5;
             if (us < best) {

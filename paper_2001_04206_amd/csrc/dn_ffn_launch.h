@@ -69,7 +69,7 @@ hipError_t run(const ProductPlan &plan, ProductArgs &a, hipStream_t s)
         if constexpr (P == P_FWD) return few<T, EPI>(a, s);
         return hipErrorInvalidValue;
     case K_SMALL:
-        if constexpr (sizeof(T) == 4) e = tiles<T, P, EPI, Small>(a, sums, s);
+        e = tiles<T, P, EPI, Small>(a, sums, s);
         break;
     case K_TINY:
         if constexpr (sizeof(T) == 4) e = tiles<T, P, EPI, Tiny>(a, sums, s);
