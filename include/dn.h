@@ -419,7 +419,8 @@ dn_status dn_cnn_train_epoch(dn_cnn *net, const float *X_dev, const int32_t *lab
  *
  * Errors: INVALID_ARG (NULL, an enum out of range, drop not in [0, 1), a scale or eps that is not finite, eps < 0, a
  * workspace that is NULL or misaligned where one is needed, a pointer that is no multiple of its element), SHAPE (rows or
- * widths < 1, rows of more than 8 MB, ld smaller than the row, d above 16384 in dn_norm_*, a workspace too small),
+ * widths < 1, rows of more than 8 MB, 2^29 rows or matrices of 2^35 elements and more, ld smaller than the row, d above 16384
+ * in dn_norm_*, a workspace too small),
  * UNSUPPORTED (softmax as the activation), DEVICE.
  */
 

@@ -71,7 +71,7 @@ hipError_t run(const MaskArgs *a, const PackArgs &p, hipStream_t s)
 {
     const uint32_t eights = a ? ((uint32_t)a->cols + 7) / 8 : 0;
     const unsigned masks = a ? (unsigned)(((uint64_t)a->rows * eights + 255) / 256) : 0, packs = (unsigned)((p.groups + 255) / 256);
-    if (masks && packs && (uint64_t)masks + packs < 1u << 31) {
+    if (masks && packs && (uint64_t)masks + packs < 1u << 24) {   // fewer than 2^32 threads
         launch_kernel(mask_pack_kernel<T>, dim3(masks + packs), dim3(256), 0, s, *a, eights, p, masks);
         return hipGetLastError();
     }

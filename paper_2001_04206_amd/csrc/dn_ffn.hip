@@ -45,6 +45,12 @@ dn_status row_length(int type, int64_t &ld, int64_t n)
     if (ld == 0) ld = n;
     return ld < n || ld * size_of(type) > kRowBytes ? DN_ERR_SHAPE : DN_OK;
 }
+// more threads than a launch can have: one for eight columns, or 512 for a tile, 64 x 64 the smallest one
+bool too_many(int64_t rows, int64_t cols)
+{
+    constexpr int64_t kThreads = (int64_t)1 << 32;
+    return rows * ((cols + 7) / 8) >= kThreads || (rows + 63) / 64 * ((cols + 63) / 64) >= kThreads / 512;
+}
 dn_status common(int type, int grad_type, int act, int32_t rows, int32_t n, int32_t m, float grad_scale)
 {
     if (!type_ok(type) || (grad_type != type && grad_type != DN_F32)) return DN_ERR_INVALID_ARG;
@@ -52,9 +58,7 @@ dn_status common(int type, int grad_type, int act, int32_t rows, int32_t n, int3
     if (act < DN_ACT_LINEAR || act > DN_ACT_GELU || !isfinite(grad_scale)) return DN_ERR_INVALID_ARG;
     if (rows < 1 || n < 1 || m < 1) return DN_ERR_SHAPE;
     if ((int64_t)n * size_of(type) > kRowBytes || (int64_t)m * size_of(type) > kRowBytes) return DN_ERR_SHAPE;
-    // tiles of a launch, at 128 x 64 columns the smallest ones
-    if (((int64_t)rows + 127) / 128 * (((int64_t)(n > m ? n : m) + 63) / 64) > 0x7fffffff) return DN_ERR_SHAPE;
-    return DN_OK;
+    return too_many(rows, n) || too_many(rows, m) || too_many(n, m) ? DN_ERR_SHAPE : DN_OK;
 }
 template <class... P>
 bool multiples(int type, const P *...p)
@@ -645,7 +649,7 @@ dn_status dn_dropout(int32_t type, const void *X_dev, void *Y_dev, int32_t rows,
     MaskArgs m{};
     dn_status s = drop_of(drop, seed, offset, m.drop);
     if (s != DN_OK) return s;
-    if (rows < 1 || cols < 1) return DN_ERR_SHAPE;
+    if (rows < 1 || cols < 1 || too_many(rows, cols)) return DN_ERR_SHAPE;
     if ((s = row_length(type, ldx, cols)) != DN_OK || (s = row_length(type, ldy, cols)) != DN_OK) return s;
     m.x = X_dev;
     m.y = Y_dev;
