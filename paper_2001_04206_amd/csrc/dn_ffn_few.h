@@ -12,8 +12,8 @@ namespace dn {
 // all loads of a step are out, so that no branch or wait lies between them.  Where the row ends inside, its last 32 bytes are taken,
 // and zeros put in place of the elements that the piece before holds: both operands are read alike, so their products stay paired.
 // WORDS: 16-bit rows may begin in the middle of a word, and the memory path then takes several cycles for each lane; the nine words
-// are loaded that hold the piece (each holds some element of it), and shifted.  37 rows of 2731 by 1024, f16: 30 us as they lie, 16 so
-// (12 where every row begins at a word).  A single row, whose lanes are neighbours, takes 5.5 us as it lies and 6.3 so.
+// are loaded that hold the piece (each holds some element of it), and shifted.  37 rows of 2731 by 1024, f16: 30 us as they lie, 14 so
+// (11 where every row begins at a word).  A single row, whose lanes are neighbours, takes 5.5 us as it lies and 6.3 so.
 template <class T> struct Any { typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
 template <class T, bool WHOLE, bool WORDS, int APART> struct Piece {
     static constexpr int E = 16 / (int)sizeof(T);
@@ -52,11 +52,8 @@ template <class T, bool WHOLE, bool WORDS, int APART> struct Piece {
         }
     }
 };
-// whether any piece of 16-bit elements may begin in the middle of a word: a row, or its last 32 bytes
-__device__ __forceinline__ bool odd_pieces(const ProductArgs &a)
-{
-    return ((uintptr_t)a.a[0] | (uintptr_t)a.b[0] | (uintptr_t)a.b[1] | (uintptr_t)a.lda | (uintptr_t)a.ldb | (uintptr_t)a.K * 2) & 2;
-}
+// whether 16-bit rows may begin in the middle of a word
+__device__ __forceinline__ bool odd_rows(const void *p, const void *q, int64_t ld) { return ((uintptr_t)p | (uintptr_t)q | (uintptr_t)ld) & 2; }
 
 // MB: blocks of sixteen rows.  The matrix instructions work on sixteen rows at least; rows that do not exist repeat the last.  Bound by
 // reading the weights, and past some rows by reading those again in every workgroup: 8 rows by 4096 x 8192 x 2, bf16, 29 us (4.6 TB/s), 64
@@ -78,27 +75,28 @@ __global__ __launch_bounds__(WAVES * 64) void few_kernel(const ProductArgs a)
     for (int b = 0; b < MB; ++b)
         x[b] = reinterpret_cast<const T *>(static_cast<const char *>(a.a[0]) + min(b * 16 + i, a.M - 1) * a.lda) + h * 2 * E;
     v4f acc[PLANES][MB] = {};
-    const bool odd = odd_pieces(a);
+    const bool odd_x = odd_rows(a.a[0], a.a[0], a.lda), odd_w = odd_rows(a.b[0], a.b[PLANES - 1], a.ldb);
     for (int k0 = wave * BK; k0 < a.K; k0 += WAVES * BK * AHEAD) {
+        const bool ends = !WHOLE && k0 + ((AHEAD - 1) * WAVES + 1) * BK > a.K, last = ends && (a.K & 1);   // then a row's last pieces are odd
+        const bool ox = odd_x || last, ow = odd_w || last;
         Piece<T, WHOLE, !WHOLE && sizeof(T) == 2, E> fw[AHEAD][PLANES], fx[AHEAD][MB];
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) {
             const int k = k0 + s * WAVES * BK, left = a.K - k - h * 2 * E;
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) fw[s][p].load(w[p] + k, left, odd);
+            for (int p = 0; p < PLANES; ++p) fw[s][p].load(w[p] + k, left, ow);
 #pragma unroll
-            for (int b = 0; b < MB; ++b) fx[s][b].load(x[b] + k, left, odd);
+            for (int b = 0; b < MB; ++b) fx[s][b].load(x[b] + k, left, ox);
         }
         if constexpr (!WHOLE) {
             __builtin_amdgcn_sched_barrier(0);
-            const bool ends = k0 + ((AHEAD - 1) * WAVES + 1) * BK > a.K;
 #pragma unroll
             for (int s = 0; s < AHEAD; ++s) {
                 const int left = a.K - (k0 + s * WAVES * BK) - h * 2 * E;
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) fw[s][p].settle(w[p], left, odd, ends);
+                for (int p = 0; p < PLANES; ++p) fw[s][p].settle(w[p], left, ow, ends);
 #pragma unroll
-                for (int b = 0; b < MB; ++b) fx[s][b].settle(x[b], left, odd, ends);
+                for (int b = 0; b < MB; ++b) fx[s][b].settle(x[b], left, ox, ends);
             }
         }
 #pragma unroll
