@@ -31,7 +31,8 @@ __device__ __forceinline__ void load8(float (&v)[8], const void *p, int64_t at, 
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
 }
-template <class T, bool ALL = false>
+// STREAM: past the caches' own order, for results that nothing near reads again
+template <class T, bool ALL = false, bool STREAM = false>
 __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8], int left)
 {
     T *q = static_cast<T *>(p) + at;
@@ -39,7 +40,8 @@ __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8],
         typename Eight<T>::type x;
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
-        *reinterpret_cast<typename Eight<T>::type *>(q) = x;
+        if (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<typename Eight<T>::type *>(q));
+        else *reinterpret_cast<typename Eight<T>::type *>(q) = x;
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
