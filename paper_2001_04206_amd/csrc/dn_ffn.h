@@ -20,6 +20,7 @@ __device__ __forceinline__ typename Eight<T>::type get8(const void *p, int64_t a
     const T *q = static_cast<const T *>(p) + at;
     if (ALL || left >= 8) return *reinterpret_cast<const typename Eight<T>::type *>(q);
     typename Eight<T>::type x;
+    if (left <= 0) return typename Eight<T>::type{};   // without this a wave whose lanes have all or nothing would take what follows too
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = j < left ? q[j] : (T)0.f;
     return x;
@@ -42,7 +43,7 @@ __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8],
         for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
         if (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<typename Eight<T>::type *>(q));
         else *reinterpret_cast<typename Eight<T>::type *>(q) = x;
-    } else {
+    } else if (left > 0) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < left) q[j] = (T)v[j];
@@ -271,6 +272,6 @@ hipError_t launch_norm_forward(int type, const NormArgs &a, hipStream_t s);
 hipError_t launch_norm_backward(int type, const NormArgs &a, hipStream_t s);
 constexpr int kNormWidth = 16384;   // largest d
 // how the backward pass is divided, and its workspace
-size_t norm_backward_plan(NormArgs &a);
+size_t norm_backward_plan(int type, NormArgs &a);
 
 }  // namespace dn

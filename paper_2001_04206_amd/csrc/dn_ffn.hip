@@ -580,7 +580,7 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
 size_t dn_norm_backward_workspace_bytes(const dn_norm_desc *d)
 {
     NormArgs a;
-    return norm_of(d, a) == DN_OK ? up256(norm_backward_plan(a)) : kBad;
+    return norm_of(d, a) == DN_OK ? up256(norm_backward_plan(d->type, a)) : kBad;
 }
 
 dn_status dn_norm_forward(const dn_norm_desc *d, const void *x_dev, const void *b_dev, const void *gate_dev,
@@ -622,7 +622,7 @@ dn_status dn_norm_backward(const dn_norm_desc *d, const void *x_dev, const void 
     if (!multiples(d->type, x_dev, b_dev, gate_dev, post_w_dev, post_b_dev, pre_w_dev, dx_out_dev, dn_dev, dx_dev, db_dev) ||
         !multiples(d->grad_type, dgate_dev, dpost_w_dev, dpost_b_dev, dpre_w_dev, dpre_b_dev))
         return DN_ERR_INVALID_ARG;
-    if ((s = workspace(up256(norm_backward_plan(a)), workspace_dev, workspace_bytes)) != DN_OK) return s;
+    if ((s = workspace(up256(norm_backward_plan(d->type, a)), workspace_dev, workspace_bytes)) != DN_OK) return s;
     a.x = x_dev;
     a.b = b_dev;
     a.gate = gate_dev;
