@@ -2,7 +2,7 @@
 //     c = post(b),  x' = x + scale gate * c,  n = pre(x')
 // A row lives in the registers of the NT threads that share it, C pieces of eight elements each; its statistics are sums over
 // those threads, in fp32, the mean first and then the centred squares.  Bound by memory: forward four rows of d elements read or
-// written, backward six; 16384 x 4096, bf16, 98 us (5.5 TB/s) and 177 + 8 (4.6).  The backward pass forms the statistics again
+// written, backward six; 16384 x 4096, bf16, 98 to 101 us (5.4 TB/s) and 177 + 8 (4.6).  The backward pass forms the statistics again
 // from the rows that it reads anyway, so nothing is kept from the forward pass.
 //
 // Backward, from dx' and dn (x is x'):  dx = dx' + pre'(dn),  dc = scale gate * dx,  db = post'(dc),  and sums over rows:
@@ -357,7 +357,7 @@ hipError_t forward_by_width(const NormArgs &a, hipStream_t s)
     if (a.d <= 1024) return forward<T, 128, 1>(a, s);
     if (a.d <= 1536) return forward<T, 192, 1>(a, s);
     if (a.d <= 2048) return forward<T, 256, 1>(a, s);
-    if (a.d <= 3 << 10) return forward<T, 384, 1>(a, s);
+    if (a.d <= 8 * 384) return forward<T, 384, 1>(a, s);
     if (a.d <= 4096) return forward<T, 512, 1>(a, s);
     if (a.d <= 8192) return forward<T, 512, 2>(a, s);
     return forward<T, 1024, 2>(a, s);
@@ -369,7 +369,7 @@ hipError_t backward_by_width(const NormArgs &a, hipStream_t s)
     if (a.d <= 1024) return backward<T, 128, 1>(a, s);
     if (a.d <= 1536) return backward<T, 192, 1>(a, s);
     if (a.d <= 2048) return backward<T, 256, 1>(a, s);
-    if (a.d <= 3 << 10) return backward<T, 384, 1>(a, s);
+    if (a.d <= 8 * 384) return backward<T, 384, 1>(a, s);
     if (a.d <= 4096) return backward<T, 512, 1>(a, s);
     if (a.d <= 8192) return backward<T, 512, 2>(a, s);
     return backward<T, 1024, 2>(a, s);
@@ -381,7 +381,7 @@ size_t norm_backward_plan(int type, NormArgs &a)
 {
     // parts: as many workgroups as run at once, so that they end together (more parts would write and read more partial sums too).
     // Waves of a compute unit go by the registers: 16, 8 of fp32 and of rows of two pieces a thread.
-    const int64_t threads = a.d <= 512 ? 64 : a.d <= 1024 ? 128 : a.d <= 1536 ? 192 : a.d <= 2048 ? 256 : a.d <= 3 << 10 ? 384 : a.d <= 8192 ? 512 : 1024;
+    const int64_t threads = a.d <= 512 ? 64 : a.d <= 1024 ? 128 : a.d <= 1536 ? 192 : a.d <= 2048 ? 256 : a.d <= 8 * 384 ? 384 : a.d <= 8192 ? 512 : 1024;
     auto rows_of = [&](int waves) {
         const int64_t most = 256 * (waves * 64 / threads > 0 ? waves * 64 / threads : 1), part = ((int64_t)a.rows + most - 1) / most;
         return part < 4 ? (int64_t)4 : part;
