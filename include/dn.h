@@ -480,6 +480,7 @@ dn_status dn_ffn_backward(const dn_ffn_desc *d, const void *X_dev, const void *W
  * Between two blocks:  c = post(b),  x' = x + scale * gate * c,  n = pre(x').
  *   x, b [rows][d]; gate [ceil(rows / rows_per_gate)][d]: row i takes row i div rows_per_gate, NULL: ones
  *   post_w, post_b, pre_w, pre_b [d]: weights and shifts of the norms, NULL: ones and zeros (a shift: layer norm only)
+ *   (the weight of a norm that is DN_NORM_NONE takes no part)
  *   x_out, n_out [rows][d]; x_out may be x or b, n_out may be b
  * b NULL: no block; x' = x and x_out is not written.  pre DN_NORM_NONE: n_out is not written (a block is needed then).
  * n is formed from x' before x' is rounded to `type`.

@@ -596,9 +596,9 @@ dn_status dn_norm_forward(const dn_norm_desc *d, const void *x_dev, const void *
     a.x = x_dev;
     a.b = b_dev;
     a.gate = gate_dev;
-    a.post_w = post_w_dev;
+    a.post_w = d->post ? post_w_dev : nullptr;   // a weight without its norm takes no part
     a.post_b = post_b_dev;
-    a.pre_w = pre_w_dev;
+    a.pre_w = d->pre ? pre_w_dev : nullptr;
     a.pre_b = pre_b_dev;
     a.x_out = x_out_dev;
     a.n_out = n_out_dev;
@@ -626,9 +626,9 @@ dn_status dn_norm_backward(const dn_norm_desc *d, const void *x_dev, const void 
     a.x = x_dev;
     a.b = b_dev;
     a.gate = gate_dev;
-    a.post_w = post_w_dev;
+    a.post_w = d->post ? post_w_dev : nullptr;   // a weight without its norm takes no part
     a.post_b = post_b_dev;
-    a.pre_w = pre_w_dev;
+    a.pre_w = d->pre ? pre_w_dev : nullptr;
     a.dx_out = dx_out_dev;
     a.dn = dn_dev;
     a.dx = dx_dev;
