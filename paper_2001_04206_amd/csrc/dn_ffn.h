@@ -100,7 +100,7 @@ template <> struct Math<false> {
     // the normal distribution's function and density
     static __device__ __forceinline__ void normal(float x, float &cdf, float &pdf)
     {
-        cdf = 0.5f * (1.f + erff(x * 0.70710678f));
+        cdf = 0.5f * erfcf(x * -0.70710678f);   // 1 + erf would lose the tail: 5 % of it at -5
         pdf = 0.39894228f * expf(-0.5f * x * x);
     }
 };
