@@ -96,7 +96,12 @@ template <bool FAST> struct Math;
 template <> struct Math<false> {
     static __device__ __forceinline__ float exp(float x) { return expf(x); }
     static __device__ __forceinline__ float inv(float x) { return 1.f / x; }
-    static __device__ __forceinline__ float tanh(float x) { return tanhf(x); }
+    static __device__ __forceinline__ void tanh(float x, float &f, float &df)
+    {
+        const float e = exp(-2.f * fabsf(x)), q = inv(1.f + e);
+        f = tanhf(x);
+        df = 4.f * e * q * q;
+    }
     // the normal distribution's function and density
     static __device__ __forceinline__ void normal(float x, float &cdf, float &pdf)
     {
@@ -107,11 +112,12 @@ template <> struct Math<false> {
 template <> struct Math<true> {
     static __device__ __forceinline__ float exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
     static __device__ __forceinline__ float inv(float x) { return __builtin_amdgcn_rcpf(x); }
-    static __device__ __forceinline__ float tanh(float x)
+    static __device__ __forceinline__ void tanh(float x, float &f, float &df)
     {
         // 1 - 2 / (e^2x + 1) loses the leading bits of small results: their series instead
-        const float big = 1.f - 2.f * inv(exp(2.f * x) + 1.f), s = x * x;
-        return s < 0.01f ? x * (1.f + s * (-0.33333333f + s * 0.13333333f)) : big;
+        const float e = exp(2.f * x), q = inv(e + 1.f), big = 1.f - 2.f * q, s = x * x;
+        f = s < 0.01f ? x * (1.f + s * (-0.33333333f + s * 0.13333333f)) : big;
+        df = 4.f * q * (x < 0.f ? e * q : 1.f - q);
     }
     static __device__ __forceinline__ void normal(float x, float &cdf, float &pdf)
     {
@@ -123,17 +129,18 @@ template <> struct Math<true> {
     }
 };
 
-// f(z), and f'(z) with it
+// f(z), and f'(z) with it.  1 - f of a unit that is all but 1 would be rounding: a sigmoid's comes of exp(-z), which is small there, and so
+// do both ends of a tanh's derivative, 4 q (1 - q) with q = 1 / (1 + exp(2 z)).
 template <int ACT, bool FAST>
 __device__ __forceinline__ void act_one(float z, float &f, float &df)
 {
     typedef Math<FAST> K;
     if (ACT == DN_ACT_SIGMOID) {
-        f = K::inv(1.f + K::exp(-z));
-        df = f * (1.f - f);
+        const float e = K::exp(-z);
+        f = K::inv(1.f + e);
+        df = f * (z > 0.f ? e * f : 1.f - f);
     } else if (ACT == DN_ACT_TANH) {
-        f = K::tanh(z);
-        df = 1.f - f * f;
+        K::tanh(z, f, df);
     } else if (ACT == DN_ACT_RELU) {   // a comparison that a NaN fails would hide it
         f = z < 0.f ? 0.f : z;
         df = z > 0.f ? 1.f : 0.f;

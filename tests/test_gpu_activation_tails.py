@@ -47,3 +47,20 @@ def test_gelu_of_fp32():
     got, want = derivative(torch.float32, z, ACTS["gelu"]), c + z64 * p
     off = (got - want).abs() / (gelu_unit(z64) * (c + (z64 * p).abs()))
     assert off.max() <= 1, (z64[off.argmax()], off.max())
+
+
+@pytest.mark.parametrize("act", ["sigmoid", "tanh"])
+@pytest.mark.parametrize("kind", TYPES)
+def test_derivatives_of_saturated_units(kind, act):
+    """A sigmoid's derivative e / (1 + e)^2 with e = exp(-|z|), a tanh's 4 e / (1 + e)^2 with e = exp(-2 |z|), where 1 - f would
+    have lost them: 16 units of fp32, in 16 bits 2^-24 |z| times 6 for the exponential's argument, then one rounding to the type, whose
+    smallest step (f16) is 2^-24."""
+    announce("saturated %s %s" % (act, kind))
+    dtype = TYPES[kind]
+    z = net_inputs(dtype, 16.0 if act == "sigmoid" else 8.0)
+    z64 = z.double().cpu()
+    e = torch.exp(-z64.abs() * (1 if act == "sigmoid" else 2))
+    want = (1 if act == "sigmoid" else 4) * e / (1 + e) ** 2
+    unit = 2.0 ** -24 * 16 if kind == "f32" else 2.0 ** -24 * (16 + 6 * z64.abs()) + UNIT[dtype]
+    off = (derivative(dtype, z, ACTS[act]) - want).abs() / (unit * want + (2.0 ** -25 if kind == "f16" else 0))
+    assert off.max() <= 1, (z64[off.argmax()], off.max())
