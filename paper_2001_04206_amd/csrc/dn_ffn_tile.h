@@ -316,6 +316,15 @@ __device__ __forceinline__ void arrived()
     __asm__ volatile("" ::: "memory");
 }
 
+// What a wave's lanes have written to LDS is what its other lanes read next, and what they have read may be written over: a wave's LDS
+// instructions run in order, so all that this takes is that the compiler, which sees one lane, leaves them in it.
+__device__ __forceinline__ void exchanged()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // The order of a half stage's instructions.  First half: its TM rows of TN blocks (EACH matrix instructions a block) and the
 // reads of the second half's fragments, READS_B and READS_A instructions each, those of a row of A after the row whose
 // registers they can take.
@@ -544,6 +553,7 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
 #pragma unroll
         for (int i0 = 0; i0 < S::TM; i0 += BLOCKS) {
             turn(i0);
+            exchanged();
             const int first = row0 + i0 * 16;
 #pragma unroll 1
             for (int r = lane / LANES; r < ROWS; r += STEP * TOGETHER) {
@@ -561,12 +571,14 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
                     if (ALL || (m < a.M && n < a.N)) finish8<T, EPI, ALL>(a.f, side[q], m, n, left, v, w);
                 }
             }
+            exchanged();
         }
     };
     if (a.split > 1) {
 #pragma unroll
         for (int i0 = 0; i0 < S::TM; i0 += BLOCKS) {
             turn(i0);
+            exchanged();
 #pragma unroll 1
             for (int r = lane / LANES; r < ROWS; r += STEP) {
                 const int m = row0 + i0 * 16 + r;
@@ -576,6 +588,7 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
                 store8<float>(part, (int64_t)m * a.N + n, v, a.N - n);
                 if (PAIR) store8<float>(part, plane + (int64_t)m * a.N + n, w, a.N - n);
             }
+            exchanged();
         }
     } else if (m0 + S::BM <= a.M && n0 + COLS <= a.N) {
         finish(std::true_type());
