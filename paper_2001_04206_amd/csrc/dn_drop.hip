@@ -40,7 +40,7 @@ __device__ __forceinline__ void pack8(const PackArgs &a, uint32_t block)
     const auto &m = a.m[k];
     const uint32_t eights = ((uint32_t)m.cols + 7) / 8;
     const int64_t in = at - m.first;
-    const int64_t row = a.groups >> 32 ? in / eights : (uint32_t)in / eights, n = (in - row * eights) * 8;
+    const int64_t row = (uint32_t)in / eights, n = (in - row * eights) * 8;   // one matrix has fewer than 2^32
     const auto v = get8<T>(m.x, row * m.ldx + n, (int)(m.cols - n));
     *reinterpret_cast<typename Eight<T>::type *>(static_cast<T *>(m.y) + (row * eights * 8 + n)) = v;
 }
@@ -52,9 +52,9 @@ __global__ __launch_bounds__(256) void mask_kernel(const MaskArgs a, uint32_t ei
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(const PackArgs a)
+__global__ __launch_bounds__(256) void pack_kernel(const PackArgs a, uint32_t first)
 {
-    pack8<T>(a, blockIdx.x);
+    pack8<T>(a, first + blockIdx.x);
 }
 
 // Both at once, on workgroups of their own: neither fills the chip for long.  1301 x 777 and 1301 x 1021 with 777 x 1021, fp32: 7 us,
@@ -76,7 +76,10 @@ hipError_t run(const MaskArgs *a, const PackArgs &p, hipStream_t s)
         return hipGetLastError();
     }
     if (masks) launch_kernel(mask_kernel<T>, dim3(masks), dim3(256), 0, s, *a, eights);
-    if (packs) launch_kernel(pack_kernel<T>, dim3(packs), dim3(256), 0, s, p);
+    // four matrices together may take more threads than a launch can have
+    constexpr unsigned most = 1u << 23;
+    for (unsigned first = 0; first < packs; first += most)
+        launch_kernel(pack_kernel<T>, dim3(packs - first < most ? packs - first : most), dim3(256), 0, s, p, first);
     return hipGetLastError();
 }
 
