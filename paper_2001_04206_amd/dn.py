@@ -434,7 +434,10 @@ def _stream(dev: int) -> int:
 def _two(t, what: str):
     if t.dim() != 2:
         raise TypeError("%s must be a matrix" % what)
-    return t.shape
+    rows, cols = t.shape
+    if (rows | cols) >> 31:     # the descriptors hold 32 bits
+        raise DnError(DN_ERR_SHAPE, "%s of shape %s" % (what, tuple(t.shape)))
+    return rows, cols
 
 
 def _linear_desc(X, W, R, Y, Yname, act, drop, seed, offset, grad_type, grad_scale):
@@ -527,7 +530,8 @@ def _norm_desc(like, post, pre, scale, eps, rows_per_gate, grad_type=None):
     kind = _type_of(like, "x")
     rows, d = _two(like, "x")
     per = rows if rows_per_gate is None else rows_per_gate
-    desc = NormDesc(kind, kind if grad_type is None else grad_type, rows, d, post, pre, max(per, 0), scale, eps)
+    # (more rows a gate than there are is one gate, and need not fit 32 bits)
+    desc = NormDesc(kind, kind if grad_type is None else grad_type, rows, d, post, pre, max(min(per, rows), 0), scale, eps)
     return desc, (rows, d), (d,), (-(-rows // per) if per > 0 else 0, d), like.dtype, like.get_device()
 
 
