@@ -1,4 +1,5 @@
 """What the residual feed-forward block's calls launch, asked of the library itself on a device that does not exist (fake_block.cpp)."""
+import math
 import os
 import re
 import subprocess
@@ -39,3 +40,31 @@ def product(launch):
     """(product, epilogue, shape, whether sums come with it, parts of k) of a launch of a matrix product in tiles, or None."""
     m = re.search(r"product_kernelI\w*?Li(\d)ELi(\d)ENS_5ShapeILi(\d)ELi(\d)ELi(\d)ELi(\d)ELi(\d)EEELb([01])E", launch[0])
     return m and (PRODUCT[int(m[1])], EPILOGUE[int(m[2])], SHAPE[",".join(m.group(3, 4, 5, 6, 7))], m[8] == "1", launch[2])
+
+
+def kernels(exe, calls):
+    """What each call launches: tiles with their epilogue, segments and whether k is in parts; kernels for few rows; norms."""
+    found = []
+    for at in range(0, len(calls), 500):
+        for call, passes in zip(calls[at:at + 500], ask(exe, calls[at:at + 500])):
+            seen = set()
+            for status, launches in passes:
+                assert status == dn.DN_OK, call
+                for launch in launches:
+                    p = product(launch)
+                    few = re.search(r"(few|token)_kernelI(.*?)Li(\d)E(.*?)EvNS", launch[0])
+                    norm = re.search(r"(norm_(?:forward|backward)_kernel)I(.*?)EvNS", launch[0])
+                    if p:
+                        seen.add((call[1],) + p[:4] + (call[0] == "block" and p[:2] == ("delta", "store"), p[4] > 1))
+                    elif few:
+                        seen.add((call[1], few[1], EPILOGUE[int(few[3])], few[4]))
+                    elif norm:
+                        seen.add((norm[1], norm[2]))
+            found.append(seen)
+    return found
+
+
+def sizes(rng, lo, hi):
+    """A size of that range, evenly over its logarithm; four in ten a multiple of 8, the others odd."""
+    n = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    return max(1, n // 8 * 8) if rng.random() < 0.4 else n | 1

@@ -5,6 +5,7 @@
 //   fake_block COMMAND...
 //     linear:0:100:64:48:0      dn_linear_forward, then dn_linear_backward: type, rows, n_in, n_out, bytes by which every tensor misses 256
 //     block:2:100:64:48:0       dn_ffn_forward, then dn_ffn_backward: type, rows, d, f, the same; dropout and every bias, fp32 gradients
+//     norm:1:100:64:7:0         dn_norm_forward, then dn_norm_backward: type, rows, d, rows of a gate, the same; layer norms with everything
 // One line per call: its status and its launches (name/x/y/threads).
 #include <cstdint>
 #include <cstdio>
@@ -68,6 +69,12 @@ int main(int argc, char **argv)
             status[0] = dn_linear_forward(&d, p, p, p, p, p, p, ws, dn_linear_forward_workspace_bytes(&d), nullptr);
             made[0].swap(launches);
             status[1] = dn_linear_backward(&d, p, p, p, p, p, p, p, ws, dn_linear_backward_workspace_bytes(&d), nullptr);
+            made[1].swap(launches);
+        } else if (kind[0] == 'n') {
+            const dn_norm_desc d = {type, DN_F32, rows, n, DN_NORM_LAYER, DN_NORM_LAYER, m, 1.f, 1e-5f};
+            status[0] = dn_norm_forward(&d, p, p, p, p, p, p, p, p, p, nullptr);
+            made[0].swap(launches);
+            status[1] = dn_norm_backward(&d, p, p, p, p, p, p, p, p, p, p, p, p, p, p, p, ws, dn_norm_backward_workspace_bytes(&d), nullptr);
             made[1].swap(launches);
         } else {
             const dn_ffn_desc d = {type, DN_F32, DN_ACT_SILU, rows, n, m, 0, 0, 0, 0.1f, 1.f, 1, 2};
