@@ -389,8 +389,7 @@ size_t norm_backward_plan(int type, NormArgs &a)
     const bool few = type == DN_F32 || a.d > 4096;
     int64_t part = rows_of(few ? 8 : 16);
     if (a.group > part) {
-        a.group_parts = (int32_t)(((int64_t)a.group + part - 1) / part);
-        if (a.group_parts == 1) part = a.group;
+        a.group_parts = (int32_t)(((int64_t)a.group + part - 1) / part);   // two at least
     } else {
         a.group_parts = 1;
         part = part / a.group * a.group;
