@@ -400,18 +400,19 @@ dn_status dn_cnn_train_epoch(dn_cnn *net, const float *X_dev, const int32_t *lab
  *
  * Types: every tensor of a call is of the descriptor's `type` (DN_F32, DN_F16, DN_BF16); parameter gradients are of it
  * too or, with grad_type DN_F32, fp32.  Sums and statistics are held in fp32 and results rounded once; what a call keeps between
- * two products (the gated hidden layer, its deltas) is rounded to `type` as the caller's own tensors are.
+ * two products (the gated hidden layer, its deltas) is rounded to `type` as the caller's own tensors are, and so are the deltas that
+ * the biases' gradients are sums of.
  *
  * Tensors are row-major device memory of the caller's, rows of X, W, R, Y and dY any distance apart (ld*, in elements; 0:
- * contiguous), everything else contiguous.  Any alignment of an element will do; operands of more than 16 rows whose rows
- * do not lie at multiples of 16 bytes and end at some are copied to the workspace first.  A result may be the residual itself (Y = R), no other two
- * tensors of a call may overlap.
+ * contiguous), everything else contiguous.  Any alignment of an element will do; operands whose rows do not lie at multiples
+ * of 16 bytes and end at some are copied to the workspace first (forward calls of up to 16 rows, and some of up to 64, read them as
+ * they lie).  A result may be the residual itself (Y = R), no other two tensors of a call may overlap.
  * Workspaces: device memory, 256-byte aligned, as many bytes as the query says (0: none, NULL will do); the query returns
  * (size_t)-1 for a descriptor that the call would refuse.  Nothing in them outlives a call.
  * Results are the same bits for the same call whatever else runs (no atomics).
  *
- * Dropout: the element in row i, column j is kept if its number is at least t, the nearest whole number to 65536 p, and
- * then multiplied by 65536 / (65536 - t); it becomes 0 otherwise.  The numbers are 16-bit ones from the counter-based
+ * Dropout: the element in row i, column j is kept if its number is at least t, the nearest whole number to 65536 p (at most
+ * 65535), and then multiplied by 65536 / (65536 - t); it becomes 0 otherwise.  The numbers are 16-bit ones from the counter-based
  * generator Philox 4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) with the key
  * `seed` and the counter (j div 8, i, offset): number j mod 8 of the eight in its four words, low halves first.  No mask is
  * stored; the backward calls compute it again from the same seed and offset.  A step that needs several masks takes another

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a, uint32_t fi
     pack8<T>(a, first + blockIdx.x);
 }
 
-// Both at once, on workgroups of their own: neither fills the chip for long.  1301 x 777 and 1301 x 1021 with 777 x 1021, fp32: 7 us,
+// Both at once, on workgroups of their own: neither fills the chip for long.  1301 x 777 and 1301 x 1021 with 777 x 1021, fp32: 8 us,
 // one after the other 5.4 and 5.7.
 template <class T>
 __global__ __launch_bounds__(256) void mask_pack_kernel(const MaskArgs a, uint32_t eights, const PackArgs p, uint32_t masks)

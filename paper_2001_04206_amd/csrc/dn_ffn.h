@@ -91,7 +91,8 @@ __device__ __forceinline__ void drop8(const Dropout &d, int m, int n, float (&v)
 // ---- activations ------------------------------------------------------------------------------------------------
 // fp32 results come from the library's functions.  Results that are rounded to 16 bits come from the hardware's exp2 and
 // reciprocal (1 ulp each), and their error function from Abramowitz and Stegun 7.1.26 (|error| <= 1.5e-7): a few
-// instructions instead of some sixty, which would be a quarter of a wide layer's time.
+// instructions instead of some sixty, which would be a quarter of a wide layer's time.  A 16-bit GELU is so within 2.2e-7 everywhere before
+// it is rounded; of its own size it is off by up to 0.05 % above -4, 0.4 % above -6 and 1.5 % above -9, where it is 10^-4, 10^-8 and 10^-18.
 template <bool FAST> struct Math;
 template <> struct Math<false> {
     static __device__ __forceinline__ float exp(float x) { return expf(x); }

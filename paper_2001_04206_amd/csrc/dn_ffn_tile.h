@@ -6,8 +6,9 @@
 // lane = 16 h + i: D register r is column 4 h + r, row i.
 //
 // Bound by the matrix instructions and, as the chip's power limit sets its clock, by what feeds them.  Measured: a gated block of 8192 rows,
-// 4096 wide with 8192 hidden, bf16, 897 + 438 us forward (1290 TFLOP/s; a library product of 8192 x 8192 x 8192 reaches 1500), its four
-// products backward 540 + 800 + 390 + 395; fp32 2048 x 1024 x 4096 at 115 of the library's 154.
+// 4096 wide with 8192 hidden, bf16, 831 + 410 us forward (1330 TFLOP/s; a library product of 8192 x 8192 x 8192 reaches 1500; by card and
+// warmth up to 897 + 438), its four products backward 509 + 763 + 750 + 379 (1440 to 1470 but for the first, whose epilogue moves 655 MB);
+// fp32 2048 x 1024 x 4096 at 115 of the library's 154.
 #pragma once
 
 #include <type_traits>
@@ -102,9 +103,10 @@ struct Beside {
 
 // The epilogue: `v` the sums, E_GATED: `w` those of the second matrix.  All of it is fp32, and each result is rounded once.  H, dG and dU
 // are rounded to T because the next product reads them as operands of the 16-bit matrix instruction: one more rounding in what comes of
-// them.  The activation's derivative is taken of G and U as the forward call stored them.  Whole tiles' results other than Y stream past the
-// L2, which leaves it to the operands: backward of 1024 rows, 2048 wide with 4096 hidden, 170 -> 162 us; not those of the gated product,
-// whose rows of 64 bytes are half lines (903 -> 945 us at 8192 rows, 4096 wide with 8192 hidden).
+// them, the biases' gradients among it, which are sums of the same operands.  The activation's derivative is taken of G and U as the
+// forward call stored them.  Whole tiles' results other than Y stream past the L2, which leaves it to the operands: backward of 1024 rows,
+// 2048 wide with 4096 hidden, 170 -> 162 us; not those of the gated product, whose rows of 64 bytes are half lines (903 -> 945 us at 8192
+// rows, 4096 wide with 8192 hidden).
 template <class T, int EPI, bool ALL>
 __device__ __forceinline__ void finish8(const Finish &e, const Beside<T, EPI> &side, int m, int n, int left, float (&v)[8], float (&w)[8])
 {
@@ -488,7 +490,8 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     arrived<0>();
 
     // Epilogue.  A wave turns its sums through its own 16 KB of LDS, sixty-four rows (or all it has) at a time, so that a lane gets eight
-    // neighbouring columns of a row: rows of 256 bytes, their 16-byte units u at u ^ (row mod 16).
+    // neighbouring columns of a row: rows of 256 bytes, their 16-byte units u at u ^ (row mod 16).  No bank conflicts but a pair's: sixteen of its
+    // lanes read eight units twice (2.1e6 cycles over the chip at 8192 x 8192, of 8.4e8 that its waves live).
     const int i16 = lane & 15, h = lane >> 4;
     const int64_t plane = (int64_t)a.M * a.N;
     const int row0 = m0 + wm * S::TM * 16;

@@ -2,8 +2,10 @@
 //     c = post(b),  x' = x + scale gate * c,  n = pre(x')
 // A row lives in the registers of the NT threads that share it, C pieces of eight elements each; its statistics are sums over
 // those threads, in fp32, the mean first and then the centred squares.  Bound by memory: forward four rows of d elements read or
-// written, backward six; 16384 x 4096, bf16, 98 to 101 us (5.4 TB/s) and 177 + 8 (4.6).  The backward pass forms the statistics again
-// from the rows that it reads anyway, so nothing is kept from the forward pass.
+// written, backward six; 16384 x 4096, bf16, 98 to 101 us (5.4 TB/s) and 174 to 192, with 8 for the join (4.4).  The backward pass forms the
+// statistics again from the rows that it reads anyway, so nothing is kept from the forward pass.
+// Wider rows keep their sums in scratch memory too: bf16 8192 x 8192 120 us (4.5 TB/s) and 320 (2.5), 4096 x 16384 243 (2.2) and 1206
+// (0.7); fp32 backward 441 (3.7) and 1417 (1.1).
 //
 // Backward, from dx' and dn (x is x'):  dx = dx' + pre'(dn),  dc = scale gate * dx,  db = post'(dc),  and sums over rows:
 // dgate = scale dx * c (rows of its group), dpost_w = dc * b^, dpost_b = dc, dpre_w = dn * x^, dpre_b = dn, where ^ is the
@@ -327,7 +329,8 @@ template <class T, int NT, int C>
 hipError_t forward(const NormArgs &a, hipStream_t s)
 {
     constexpr int block = NT < 128 ? 256 : NT, rows = NT < 128 ? 256 / NT : 1;
-    // as many workgroups as run at once, so that they end together: 20 waves a compute unit, 16 of fp32, by their registers
+    // as many workgroups as run at once, so that they end together: 20 waves a compute unit, 16 of fp32, by their registers.  (Rows of two
+    // pieces a thread take more: of 512 threads one workgroup runs at a time, and twice as many are launched.)
     constexpr int most = 256 * ((sizeof(T) == 2 ? 1280 : 1024) / block > 0 ? (sizeof(T) == 2 ? 1280 : 1024) / block : 1);
     const int64_t need = ((int64_t)a.rows + rows - 1) / rows;
     launch_kernel(norm_forward_kernel<T, NT, C, C == 1>, dim3((unsigned)(need < most ? need : most)), dim3(block), 0, s, a);
@@ -380,7 +383,9 @@ hipError_t backward_by_width(const NormArgs &a, hipStream_t s)
 size_t norm_backward_plan(int type, NormArgs &a)
 {
     // parts: as many workgroups as run at once, so that they end together (more parts would write and read more partial sums too).
-    // Waves of a compute unit go by the registers: 16, 8 of fp32 and of rows of two pieces a thread.
+    // Waves of a compute unit go by the registers: 16, 8 of fp32 and of rows of two pieces a thread.  (That is the kernel for parts of a
+    // gate's rows.  The one for whole gates takes 155 to 159 registers in 16 bits, so that 12 waves run, and of 512 threads one workgroup at
+    // a time, where two are planned: 16384 x 4096 with a gate a row 278 us, 3.9 TB/s.)
     const int64_t threads = a.d <= 512 ? 64 : a.d <= 1024 ? 128 : a.d <= 1536 ? 192 : a.d <= 2048 ? 256 : a.d <= 8 * 384 ? 384 : a.d <= 8192 ? 512 : 1024;
     auto rows_of = [&](int waves) {
         const int64_t most = 256 * (waves * 64 / threads > 0 ? waves * 64 / threads : 1), part = ((int64_t)a.rows + most - 1) / most;
