@@ -16,8 +16,8 @@
  * "Performance Analysis" and "Conclusions").
  *
  * Conventions
- *   - All arithmetic and all tensors are fp32, row-major, contiguous (dn_linear_*, dn_ffn_*, dn_norm_* and dn_dropout
- *     also take f16 and bf16 tensors).
+ *   - All arithmetic and all tensors are fp32, row-major, contiguous (dn_linear_*, dn_ffn_*, dn_norm_*, dn_dropout,
+ *     dn_route_*, dn_experts_* and dn_clip also take f16 and bf16 tensors).
  *   - Layers l = 1..L, widths n_0 (input) .. n_L (output).  W_l is
  *     [n_l][n_{l-1}], b_l is [n_l].  A batch of B samples is [B][n].
  *   - Labels are int32 class ids in [0, n_L); targets are their one-hot rows
@@ -510,6 +510,109 @@ dn_status dn_norm_backward(const dn_norm_desc *d, const void *x_dev, const void 
 /* Dropout by itself, forward and backward alike: Y = D(X), [rows][cols], rows ldx and ldy elements apart (0: cols); Y may be X. */
 dn_status dn_dropout(int32_t type, const void *X_dev, void *Y_dev, int32_t rows, int32_t cols, int64_t ldx, int64_t ldy,
                      float drop, uint64_t seed, uint64_t offset, void *hip_stream);
+
+/* ---- a block of experts -----------------------------------------------------------
+ * The residual feed-forward block with many gated blocks side by side, of which every row takes a few: dn_route_* says
+ * which and with what weights, dn_experts_* is the block, dn_clip bounds the norm of all gradients of a model before dn_sgd_step takes
+ * them.  The router's logits are a dense layer's (dn_linear_*); dn_norm_*, dn_dropout and the dense nets go around the block as they do
+ * around dn_ffn_*, whose section says what holds here too: types, fp32 sums, alignment, workspaces, no atomics on results.
+ *
+ * Lists.  P = rows * k pairs of a row and a choice; pair t * k + j is choice j of row t.  All int32, in device memory:
+ *   expert [rows][k]    the expert of a pair; a number outside 0 .. experts - 1: none
+ *   starts [experts + 1]  place of each expert's first pair; starts[experts] pairs have an expert
+ *   order [P]           the pair at a place: by expert, then by pair; -1 behind the last
+ *   place [P]           the place of a pair; -1 for one without an expert
+ * The experts' calls read the lists on the device.  Whatever numbers they hold, no call reads or writes outside its tensors; what it
+ * computes is then meaningless.
+ *
+ * Limits: experts 1 .. 1024, k 1 .. 32, rows below 2^26, P below 2^30; in dn_experts_* P below 2^24, X and dY within 2^31 bytes, and matrices whose
+ * widths are multiples of 16 bytes must begin at one.
+ *
+ * Errors: as for the block's calls; INVALID_ARG also for a scale, grad_scale or max_norm that is not finite or has no meaning (max_norm:
+ * negative or NaN), score or group_best out of range, results of dn_clip that overlap; SHAPE also for sizes beyond the limits,
+ * experts that are no multiple of groups, top_groups outside 1 .. groups, k above what the top groups hold, group_best above a group.
+ */
+
+typedef enum { DN_SCORE_SOFTMAX = 0, DN_SCORE_SIGMOID = 1 } dn_score;
+
+/*
+ * Routing.  With l a row's logits, s = softmax(l) or sigmoid(l), c = s + bias (bias NULL: 0):
+ *   groups > 1: `groups` groups of experts / groups neighbouring experts; a group's score is the sum of its group_best (1 or 2)
+ *   highest c; the top_groups highest groups stay, ties go to the lower group
+ *   choices: the k highest c of what stays, highest first, ties to the lower expert
+ *   weight = scale * s / (renorm: the sum of the chosen s; else: 1)
+ * An expert whose logit (or c) is -inf cannot be had: a row with fewer than k left gets expert -1 and weight 0 in the other choices (all
+ * of them where the row is padding, every logit -inf); a group with none left cannot either.  NaN ranks as +inf, and so do the weights of its
+ * row become NaN (sigmoid: its own weight, and the others through the sum).
+ * Without a bias c orders as l does, and the choice is made by l; with one, and for group scores of two, s is formed in 64 bits, so
+ * that neighbouring scores are told apart.  With renorm, weights are ratios of the chosen scores however small these are.
+ *   L, dL [rows][experts] of `type`, rows of L ldl elements apart (0: contiguous); bias [experts] and weight, dweight [rows][k] fp32
+ *   starts, order, place: all three (the lists of expert[][]) or none
+ * dn_route_lists makes the lists of any table of experts.  The workspace is the same for both, and none where there are no lists.
+ * Backward: dL from dweight = dE/dweight, for the choices as they were made; the bias has no gradient.
+ */
+typedef struct {
+    int32_t type, score; /* dn_type, dn_score */
+    int32_t rows, experts, k;
+    int32_t groups, top_groups, group_best;
+    int32_t renorm;      /* 0 or 1 */
+    float scale;
+    int64_t ldl;
+} dn_route_desc;
+size_t dn_route_workspace_bytes(int32_t rows, int32_t experts, int32_t k);
+dn_status dn_route_forward(const dn_route_desc *d, const void *L_dev, const float *bias_dev, int32_t *expert_dev, float *weight_dev,
+                           int32_t *starts_dev, int32_t *order_dev, int32_t *place_dev, void *workspace_dev,
+                           size_t workspace_bytes, void *hip_stream);
+dn_status dn_route_lists(const int32_t *expert_dev, int32_t rows, int32_t experts, int32_t k, int32_t *starts_dev, int32_t *order_dev,
+                         int32_t *place_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+dn_status dn_route_backward(const dn_route_desc *d, const void *L_dev, const int32_t *expert_dev, const float *dweight_dev,
+                            void *dL_dev, void *hip_stream);
+
+/*
+ * The block.  For the pair at place p, of row t and expert e, with weight w:
+ *   G = x_t Wg[e]^T,  U = x_t Wu[e]^T,  H = act(G) * U,  z_p = H Wd[e]^T;   Y_t = R_t + the sum of w z over row t's pairs
+ *   X [rows][d], Wg and Wu [experts][f][d], Wd [experts][d][f], weight [rows][k] fp32, R [rows][d] or NULL, Y [rows][d]
+ *   GU [P][2 f]: row p receives G and, beside it, U for the backward pass, or NULL; rows of places behind the last pair stay as they are
+ * Backward, with dh = dY_t Wd[e]:  dG = w dh * U * act'(G),  dU = w dh * act(G),  dX_t = the sum of dG Wg[e] + dU Wu[e] over its
+ * pairs,  dweight = the sum of dh * H over f (0 for a pair without an expert), and grad_scale times dWg[e] = dG^T X,  dWu[e] = dU^T X,
+ * dWd[e] = dY^T (w H) over the expert's pairs (0 for an expert without any).  dX and dweight may be NULL (not computed).
+ * z, H, dG and dU are rounded to `type`, each pair's dX too before they are added.
+ */
+typedef struct {
+    int32_t type, grad_type; /* dn_type */
+    int32_t act;             /* dn_act other than softmax */
+    int32_t rows, d, f, experts, k;
+    int64_t ldx, ldr, ldy;   /* ldy: of Y and of dY */
+    float grad_scale;
+} dn_experts_desc;
+size_t dn_experts_forward_workspace_bytes(const dn_experts_desc *d);
+size_t dn_experts_backward_workspace_bytes(const dn_experts_desc *d);
+dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
+                             const float *weight_dev, const int32_t *starts_dev, const int32_t *order_dev, const int32_t *place_dev,
+                             const void *R_dev, void *Y_dev, void *GU_dev, void *workspace_dev, size_t workspace_bytes,
+                             void *hip_stream);
+dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
+                              const float *weight_dev, const int32_t *starts_dev, const int32_t *order_dev, const int32_t *place_dev,
+                              const void *GU_dev, const void *dY_dev, void *dX_dev, void *dWg_dev, void *dWu_dev, void *dWd_dev,
+                              float *dweight_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Clipping by the norm of many tensors together:  n = sqrt(the sum of g^2 over all of them),  out = g * min(1, max_norm / n).
+ *   spans [n_spans] (host, read before the call returns): count elements of `type` at grad; the result goes to out, of out_type
+ *   (`type` or DN_F32): grad itself where out_type is type, or memory apart from every grad and every other out.  count 0: nothing there
+ *   norm [1] (device, fp32) receives n.  Squares are added in 64 bits, in an order that depends on the spans alone.
+ * An n that is not finite (an element is not) bounds nothing: results are the gradients, and the caller reads it in norm.  max_norm INFINITY
+ * and out NULL everywhere: the norm only.  Results in place are written only where they change (n > max_norm).
+ */
+typedef struct {
+    const void *grad_dev;
+    void *out_dev;           /* NULL: only the norm takes part of this span */
+    int64_t count;
+    int32_t type, out_type;  /* dn_type */
+} dn_span;
+size_t dn_clip_workspace_bytes(const dn_span *spans, int32_t n_spans);
+dn_status dn_clip(const dn_span *spans, int32_t n_spans, float max_norm, float *norm_dev, void *workspace_dev,
+                  size_t workspace_bytes, void *hip_stream);
 
 /*
  * Measurement hooks (the paper times its two offloaded methods with wall-clock

@@ -1,0 +1,234 @@
+// Clipping by the norm of many tensors together.
+//
+// Two passes over memory: squares, and (where there is something to write) products.  Pieces of all tensors of a launch are numbered on
+// end; workgroup b takes pieces b, b + grid, .., so that what is added to what depends on the tensors' sizes alone.  The squares are added
+// in 64 bits, which neither overflow nor lose small tensors beside large ones, at two instructions an element.
+#include <stdlib.h>
+
+#include <algorithm>
+
+#include "dn_ffn_host.h"
+
+namespace dn {
+namespace {
+
+constexpr int kSpans = 80;            // of a launch: its arguments stay within 4 KB
+constexpr int kPiece = 256 * 8 * 4;   // elements
+constexpr int kGroups = 1024;         // workgroups of a launch, four a compute unit
+
+struct ClipArgs {
+    struct Span { const void *g; void *y; int64_t n; int32_t first; int16_t type, out_type; } s[kSpans];   // first: its first piece
+    double *parts;         // this launch's (squares); all of them (products)
+    float *norm;           // written by one workgroup, NULL: not by this launch
+    int32_t n, pieces, all_parts;
+    float max_norm;
+};
+static_assert(sizeof(ClipArgs) <= 4096, "a launch's arguments");
+
+__device__ __forceinline__ double sum_of_block(double v, double *share)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) share[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (share[0] + share[1]) + (share[2] + share[3]);
+}
+
+__device__ __forceinline__ int span_of(const ClipArgs &a, int piece)
+{
+    int lo = 0, hi = a.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.s[mid].first <= piece) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <class T>
+__device__ __forceinline__ double squares(const void *g, int64_t at, int64_t n)
+{
+    double s[4] = {};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int64_t i = at + q * 2048 + threadIdx.x * 8;
+        float v[8];
+        load8<T>(v, g, i, (int)(n - i < 8 ? n - i : 8));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[q] = fma((double)v[j], (double)v[j], s[q]);
+    }
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+__global__ __launch_bounds__(256) void squares_kernel(const ClipArgs a)
+{
+    __shared__ double share[4];
+    double sum = 0.;
+    for (int p = blockIdx.x; p < a.pieces; p += gridDim.x) {
+        const ClipArgs::Span &s = a.s[span_of(a, p)];
+        const int64_t at = (int64_t)(p - s.first) * kPiece;
+        sum += s.type == DN_F32 ? squares<float>(s.g, at, s.n) : s.type == DN_F16 ? squares<f16>(s.g, at, s.n) : squares<bf16>(s.g, at, s.n);
+    }
+    sum = sum_of_block(sum, share);
+    if (threadIdx.x == 0) a.parts[blockIdx.x] = sum;
+}
+
+template <class T, class U>
+__device__ __forceinline__ void times(const ClipArgs::Span &s, int64_t at, float by)
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int64_t i = at + q * 2048 + threadIdx.x * 8;
+        const int left = (int)(s.n - i < 8 ? s.n - i : 8);
+        float v[8];
+        load8<T>(v, s.g, i, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= by;
+        store8<U>(s.y, i, v, left);
+    }
+}
+
+__global__ __launch_bounds__(256) void times_kernel(const ClipArgs a)
+{
+    __shared__ double share[4];
+    double sum = 0.;
+    for (int i = threadIdx.x; i < a.all_parts; i += 256) sum += a.parts[i];
+    const double norm = sqrt(sum_of_block(sum, share));
+    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
+    const bool clip = norm > (double)a.max_norm && norm < (double)INFINITY;
+    const float by = clip ? (float)((double)a.max_norm / norm) : 1.f;
+    for (int p = a.pieces - 1 - (int)blockIdx.x; p >= 0; p -= gridDim.x) {   // what was read last may still be near
+        const ClipArgs::Span &s = a.s[span_of(a, p)];
+        if (!s.y || (!clip && s.y == s.g)) continue;
+        const int64_t at = (int64_t)(p - s.first) * kPiece;
+        if (s.type == DN_F32) times<float, float>(s, at, by);
+        else if (s.type == DN_F16) s.out_type == DN_F32 ? times<f16, float>(s, at, by) : times<f16, f16>(s, at, by);
+        else s.out_type == DN_F32 ? times<bf16, float>(s, at, by) : times<bf16, bf16>(s, at, by);
+    }
+}
+
+int groups_of(int64_t pieces) { return pieces < 1 ? 1 : pieces < kGroups ? (int)pieces : kGroups; }
+
+// Spans in runs of a launch each: at most kSpans, and pieces that 31 bits can number.  f(args, pieces, run): false ends it.
+template <class F>
+bool runs(const dn_span *spans, int32_t n, F f)
+{
+    ClipArgs a{};
+    int64_t pieces = 0;
+    int run = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (!spans[i].count) continue;
+        const int64_t more = (spans[i].count + kPiece - 1) / kPiece;
+        if (a.n == kSpans || (a.n && pieces + more > 0x7fffffff)) {
+            a.pieces = (int32_t)pieces;
+            if (!f(a, run++)) return false;
+            a.n = 0;
+            pieces = 0;
+        }
+        a.s[a.n++] = {spans[i].grad_dev, spans[i].out_dev, spans[i].count, (int32_t)pieces, (int16_t)spans[i].type, (int16_t)spans[i].out_type};
+        pieces += more;
+    }
+    a.pieces = (int32_t)pieces;
+    return f(a, run);   // the last one, if only to write the norm
+}
+
+dn_status check(const dn_span *spans, int32_t n)
+{
+    if (n < 0 || (n && !spans)) return DN_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < n; ++i) {
+        const dn_span &s = spans[i];
+        if (!type_ok(s.type) || (s.out_type != s.type && s.out_type != DN_F32)) return DN_ERR_INVALID_ARG;
+        if (s.count < 0 || s.count > (int64_t)1 << 43) return DN_ERR_SHAPE;   // 2^31 pieces and fewer
+        if (!s.count) continue;
+        if (!s.grad_dev || !multiples(s.type, s.grad_dev) || !multiples(s.out_type, s.out_dev)) return DN_ERR_INVALID_ARG;
+    }
+    return DN_OK;
+}
+
+// No result may lie where another tensor's gradient or result does: two workgroups would write there, or one read what the other wrote.
+dn_status apart(const dn_span *spans, int32_t n)
+{
+    struct Range { uintptr_t from, to; int32_t span; bool written; };
+    Range *r = static_cast<Range *>(malloc(sizeof(Range) * 2 * (size_t)(n > 0 ? n : 1)));
+    if (!r) return DN_ERR_OOM;
+    int64_t m = 0;
+    bool sorted = true;
+    auto add = [&](const void *p, int64_t bytes, int32_t i, bool written) {
+        r[m] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, i, written};
+        sorted = sorted && (!m || r[m - 1].from <= r[m].from);
+        ++m;
+    };
+    for (int32_t i = 0; i < n; ++i)
+        if (spans[i].count) {
+            const bool same = spans[i].out_dev == spans[i].grad_dev && spans[i].out_type == spans[i].type;
+            add(spans[i].grad_dev, spans[i].count * size_of(spans[i].type), i, same);
+            if (spans[i].out_dev && !same) add(spans[i].out_dev, spans[i].count * size_of(spans[i].out_type), i, true);
+        }
+    if (!sorted) std::sort(r, r + m, [](const Range &x, const Range &y) { return x.from < y.from; });
+    // the furthest end so far of what is read, and of what is written
+    uintptr_t read = 0, written = 0;
+    dn_status s = DN_OK;
+    for (int64_t i = 0; i < m; ++i) {
+        if (r[i].from < written || (r[i].written && r[i].from < read)) s = DN_ERR_INVALID_ARG;
+        uintptr_t &end = r[i].written ? written : read;
+        end = end > r[i].to ? end : r[i].to;
+    }
+    free(r);
+    return s;
+}
+
+size_t parts_of(const dn_span *spans, int32_t n)
+{
+    size_t parts = 0;
+    runs(spans, n, [&](const ClipArgs &a, int) {
+        parts += (size_t)groups_of(a.pieces);
+        return true;
+    });
+    return parts;
+}
+
+}  // namespace
+}  // namespace dn
+
+using namespace dn;
+
+extern "C" {
+
+size_t dn_clip_workspace_bytes(const dn_span *spans, int32_t n_spans)
+{
+    return check(spans, n_spans) == DN_OK ? up256(parts_of(spans, n_spans) * sizeof(double)) : kBad;
+}
+
+dn_status dn_clip(const dn_span *spans, int32_t n_spans, float max_norm, float *norm_dev, void *workspace_dev,
+                  size_t workspace_bytes, void *hip_stream)
+{
+    dn_status st = check(spans, n_spans);
+    if (st != DN_OK) return st;
+    if (!(max_norm >= 0.f) || !norm_dev || !multiples(DN_F32, norm_dev)) return DN_ERR_INVALID_ARG;
+    if ((st = apart(spans, n_spans)) != DN_OK) return st;
+    const size_t parts = parts_of(spans, n_spans);
+    if ((st = workspace(up256(parts * sizeof(double)), workspace_dev, workspace_bytes)) != DN_OK) return st;
+    const hipStream_t s = (hipStream_t)hip_stream;
+    double *ws = static_cast<double *>(workspace_dev), *at = ws;
+    const bool summed = runs(spans, n_spans, [&](ClipArgs &a, int) {
+        a.parts = at;
+        at += groups_of(a.pieces);
+        launch_kernel(squares_kernel, dim3(groups_of(a.pieces)), dim3(256), 0, s, a);
+        return hipGetLastError() == hipSuccess;
+    });
+    if (!summed) return DN_ERR_DEVICE;
+    const bool done = runs(spans, n_spans, [&](ClipArgs &a, int run) {
+        bool any = run == 0;
+        for (int i = 0; i < a.n; ++i) any = any || a.s[i].y;
+        if (!any) return true;
+        a.parts = ws;
+        a.all_parts = (int32_t)parts;
+        a.norm = run == 0 ? norm_dev : nullptr;
+        a.max_norm = max_norm;
+        launch_kernel(times_kernel, dim3(groups_of(a.pieces)), dim3(256), 0, s, a);
+        return hipGetLastError() == hipSuccess;
+    });
+    return done ? DN_OK : DN_ERR_DEVICE;
+}
+
+}  // extern "C"

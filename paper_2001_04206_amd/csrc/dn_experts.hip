@@ -1,0 +1,396 @@
+// A block of experts: checks, plans, workspaces and launches, and what lies between its products: rows into the experts' order, and the
+// pairs' results back together.
+#include "dn_experts.h"
+#include "dn_ffn_host.h"
+
+namespace dn {
+namespace {
+
+constexpr int kMostExperts = 1024, kMostChoices = 32;
+constexpr int64_t kMostRows = (int64_t)1 << 26, kMostPairs = (int64_t)1 << 24, kMostBytes = ((int64_t)1 << 31) - 1;
+
+// ---- rows ------------------------------------------------------------------------------------------------------------
+
+// Rows of up to two matrices of the same width into the experts' order and 16-byte rows, zeros following; and the pairs' weights.
+struct SortArgs {
+    const void *x[2];
+    void *y[2];
+    int64_t ldx[2];
+    const float *weight;
+    float *sorted;
+    Group group;
+    int32_t cols;
+};
+template <class T>
+__global__ __launch_bounds__(256) void sort_rows_kernel(const SortArgs a)
+{
+    const uint32_t eights = ((uint32_t)a.cols + 7) / 8;
+    const uint64_t first = (uint64_t)blockIdx.x * 256;
+    const uint32_t row0 = (uint32_t)(first / eights), c0 = (uint32_t)(first % eights) + threadIdx.x, more = c0 / eights;
+    const int64_t p = (int64_t)row0 + more;
+    const uint32_t c = c0 - more * eights;
+    if (p >= min(a.group.starts[a.group.experts], a.group.pairs)) return;
+    const int t = token_of(a.group, (int)p), k = blockIdx.y, left = a.cols - (int)c * 8;
+    const auto v = get8<T>(a.x[k], t * a.ldx[k] + c * 8, left);
+    *reinterpret_cast<typename Eight<T>::type *>(static_cast<T *>(a.y[k]) + (p * eights + c) * 8) = v;
+    if (k == 0 && c == 0) a.sorted[p] = a.weight[min((uint32_t)max(a.group.order[p], 0), (uint32_t)a.group.pairs - 1)];
+}
+
+// Y_t = R_t + the sum over its pairs of (weight) z, in the order of the choices, in fp32.  A thread: eight columns of a row.
+struct JoinArgs {
+    const void *z, *r;
+    void *y;
+    int64_t ldz, ldr, ldy;
+    const float *weight;       // NULL: ones
+    const int32_t *place;
+    int32_t rows, cols, k, pairs;
+};
+template <class T>
+__global__ __launch_bounds__(256) void join_pairs_kernel(const JoinArgs a)
+{
+    const uint32_t eights = ((uint32_t)a.cols + 7) / 8;
+    const uint64_t first = (uint64_t)blockIdx.x * 256;
+    const uint32_t row0 = (uint32_t)(first / eights), c0 = (uint32_t)(first % eights) + threadIdx.x, more = c0 / eights;
+    const int64_t t = (int64_t)row0 + more;
+    if (t >= a.rows) return;
+    const int n = (int)(c0 - more * eights) * 8, left = a.cols - n;
+    float v[8] = {};
+    if (a.r) load8<T>(v, a.r, t * a.ldr + n, left);
+    for (int j0 = 0; j0 < a.k; j0 += 4) {
+        typename Eight<T>::type z[4];
+        float w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int j = min(j0 + q, a.k - 1), p = a.place[t * a.k + j];
+            const bool has = j0 + q < a.k && (uint32_t)p < (uint32_t)a.pairs;
+            w[q] = !has ? 0.f : a.weight ? a.weight[t * a.k + j] : 1.f;
+            z[q] = has ? get8<T>(a.z, p * a.ldz + n, left) : typename Eight<T>::type{};
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = fmaf(w[q], (float)z[q][j], v[j]);
+    }
+    store8<T>(a.y, t * a.ldy + n, v, left);
+}
+
+// The weights' derivatives from the parts that the tiles of dh left, one for 64 columns, in order.
+__global__ __launch_bounds__(256) void dots_kernel(const float *dots, int parts, Group g, const int32_t *place, float *dweight)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= g.pairs) return;
+    if (i < g.starts[g.experts]) {
+        float v = 0.f;
+        for (int s = 0; s < parts; ++s) v += dots[(int64_t)s * g.pairs + i];
+        const int q = g.order[i];
+        if ((uint32_t)q < (uint32_t)g.pairs) dweight[q] = v;
+    }
+    if (place[i] < 0) dweight[i] = 0.f;
+}
+
+template <class T>
+hipError_t join_as(const JoinArgs &a, hipStream_t s)
+{
+    const uint64_t threads = (uint64_t)a.rows * (((uint32_t)a.cols + 7) / 8);
+    launch_kernel(join_pairs_kernel<T>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_join(int type, const JoinArgs &a, hipStream_t s)
+{
+    return type == DN_F32 ? join_as<float>(a, s) : type == DN_F16 ? join_as<f16>(a, s) : join_as<bf16>(a, s);
+}
+template <class T>
+hipError_t sort_as(const SortArgs &a, hipStream_t s)
+{
+    const uint64_t threads = (uint64_t)a.group.pairs * (((uint32_t)a.cols + 7) / 8);
+    launch_kernel(sort_rows_kernel<T>, dim3((unsigned)((threads + 255) / 256), 2), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_sort(int type, const SortArgs &a, hipStream_t s)
+{
+    return type == DN_F32 ? sort_as<float>(a, s) : type == DN_F16 ? sort_as<f16>(a, s) : sort_as<bf16>(a, s);
+}
+hipError_t launch_experts(int type, Product p, Epilogue e, ProductKernel kernel, const ProductArgs &a, int64_t tiles, hipStream_t s)
+{
+    return type == DN_F32   ? launch_experts_f32(p, e, kernel, a, tiles, s)
+           : type == DN_F16 ? launch_experts_f16(p, e, kernel, a, tiles, s)
+                            : launch_experts_bf16(p, e, kernel, a, tiles, s);
+}
+
+// ---- plans -----------------------------------------------------------------------------------------------------------
+
+// Tiles of rows: at most, whatever the lists hold.
+int64_t most_tiles(int64_t pairs, int experts, int rows) { return pairs / rows + (pairs < experts ? pairs : experts); }
+
+// Which kernel a product of the experts takes: the one expected to take least, by the times that plan_product goes by.  How the pairs
+// are spread is not known here: each expert's last tile is taken to be half full.
+ProductKernel plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, int N, int K, int segments)
+{
+    const int planes = e == E_GATED ? 2 : 1, bk = type == DN_F32 ? 32 : 64;
+    const double es = (double)size_of(type), met = (double)(pairs < experts ? pairs : experts);
+    const double weights = p == P_GRAD ? 0 : es * met * planes * N * K * segments / 4.6e6;
+    double best = 1e300;
+    ProductKernel kernel = K_SMALL;
+    auto tiles_of = [&](int rows) {
+        const double t = (double)pairs / rows + met / 2;
+        return t > met ? t : met;
+    };
+    if (p == P_FWD && (int64_t)K * size_of(type) >= 32 && most_tiles(pairs, experts, 16) * ((N + 15) / 16) < 1 << 23) {   // 2^32 threads
+        best = 6 + es * tiles_of(16) * planes * N * K / 4.6e6;
+        kernel = K_FEW;
+    }
+    struct Way { ProductKernel kernel; int rows, cols, together; double stage, least, round; };
+    const Way tiny{K_TINY, 64, 128, 3, 0.95, 0.95, 6}, large{K_LARGE, 256, 256, 1, 1.5, 1.5, 8}, medium{K_MEDIUM, 128, 256, 1, 0.8, 0.8, 6};
+    const Way small = type == DN_F32 ? Way{K_SMALL, 128, 128, 2, 1.8, 1.8, 6} : Way{K_SMALL, 128, 128, 2, 0.5, 0.9, 4};
+    for (const Way &w : {large, medium, small, tiny}) {
+        if (type == DN_F32 ? w.kernel > K_SMALL : w.kernel == K_TINY) continue;
+        const int64_t cols = w.cols / planes;
+        double tiles = (double)((N + cols - 1) / cols), steps;
+        if (p == P_GRAD) {   // K: the result's rows; its terms are the pairs
+            tiles *= (double)experts * ((K + w.rows - 1) / w.rows);
+            steps = (double)pairs / met / bk + 0.5;
+        } else {
+            tiles *= tiles_of(w.rows);
+            steps = (double)((K + bk - 1) / bk * segments);
+        }
+        const double deep = ceil(tiles / 256), rounds = ceil(deep / w.together);
+        const double stage = deep * w.stage > rounds * w.least ? deep * w.stage : rounds * w.least;
+        double us = steps * stage + rounds * w.round;
+        if (us < weights) us = weights;
+        if (us < best) {
+            best = us;
+            kernel = w.kernel;
+        }
+    }
+    return kernel;
+}
+
+struct Block {
+    dn_experts_desc d;
+    int64_t pairs, ldh, ldz;     // between rows of H, of z
+    ProductKernel up, down, dh, dx, dwgu, dwd;
+    bool pack_w;                 // the matrices are copied to 16-byte rows
+    int parts;                   // of the weights' derivatives
+    size_t h, z, x, w1, w2, fwd_bytes;                        // bytes of H, z, X, Wg (and Wu), Wd; workspace
+    size_t sorted, dots, dgu, bwd_bytes;
+};
+
+dn_status block_of(const dn_experts_desc *d, Block &b)
+{
+    if (!d) return DN_ERR_INVALID_ARG;
+    b.d = *d;
+    dn_status s = common(d->type, d->grad_type, d->act, d->rows, d->d, d->f, d->grad_scale);
+    if (s != DN_OK) return s;
+    if (d->experts < 1 || d->experts > kMostExperts || d->k < 1 || d->k > kMostChoices || d->rows >= kMostRows) return DN_ERR_SHAPE;
+    if ((s = row_length(d->type, b.d.ldx, d->d)) != DN_OK || (s = row_length(d->type, b.d.ldr, d->d)) != DN_OK ||
+        (s = row_length(d->type, b.d.ldy, d->d)) != DN_OK)
+        return s;
+    const int64_t e = size_of(d->type), n = d->experts;
+    b.pairs = (int64_t)d->rows * d->k;
+    b.ldh = up8(d->f);
+    b.ldz = up8(d->d);
+    if (b.pairs >= kMostPairs || 2 * b.ldh * e > kRowBytes || n * b.ldh >= kMostBytes || n * b.ldz >= kMostBytes) return DN_ERR_SHAPE;
+    if (most_tiles(b.pairs, d->experts, 64) * (((b.ldh > b.ldz ? b.ldh : b.ldz) + 63) / 64) >= 1 << 23) return DN_ERR_SHAPE;   // a launch's threads
+    if (too_many(b.pairs, d->d) || too_many(b.pairs, 2 * b.ldh) || too_many(n * d->f, d->d) || too_many(n * d->d, d->f)) return DN_ERR_SHAPE;
+    const int64_t wide = b.d.ldx > b.ldz ? b.d.ldx : b.ldz, wider = b.d.ldy > wide ? b.d.ldy : wide;
+    if (d->rows * wider * e > kMostBytes) return DN_ERR_SHAPE;
+    b.up = plan_experts(d->type, P_FWD, E_GATED, b.pairs, d->experts, d->f, d->d, 1);
+    b.down = plan_experts(d->type, P_FWD, E_STORE, b.pairs, d->experts, d->d, d->f, 1);
+    b.dh = plan_experts(d->type, P_DELTA, E_DEXPERT, b.pairs, d->experts, d->f, d->d, 1);
+    b.dx = plan_experts(d->type, P_DELTA, E_STORE, b.pairs, d->experts, d->d, d->f, 2);
+    b.dwgu = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->d, (int)(2 * b.ldh), 1);
+    b.dwd = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->f, d->d, 1);
+    b.pack_w = d->d * e % 16 || d->f * e % 16;
+    const size_t wgu = b.pack_w ? packed_bytes(d->type, n * d->f, d->d) : 0, wd = b.pack_w ? packed_bytes(d->type, n * d->d, d->f) : 0;
+    b.h = up256((size_t)(b.pairs * b.ldh * e));
+    b.z = up256((size_t)(b.pairs * b.ldz * e));
+    b.x = packed_bytes(d->type, d->rows, d->d);
+    b.w1 = wgu;
+    b.w2 = wd;
+    b.fwd_bytes = b.h + b.z + (b.up == K_FEW ? 0 : b.x + 2 * wgu) + (b.down == K_FEW ? 0 : wd);
+    b.parts = (int)((d->f + 255) / 256 * 4);   // of 64 columns, whole tiles
+    b.sorted = up256((size_t)b.pairs * sizeof(float));
+    b.dots = up256((size_t)b.pairs * b.parts * sizeof(float));
+    b.dgu = up256((size_t)(b.pairs * 2 * b.ldh * e));
+    b.bwd_bytes = 2 * b.z + b.sorted + b.dots + b.h + b.dgu + b.z + 2 * wgu + wd;
+    return DN_OK;
+}
+
+ProductArgs product(const Group &g, int M, int N, int K, int segments, int64_t b_stride)
+{
+    ProductArgs a{};
+    a.M = M;
+    a.N = N;
+    a.K = K;
+    a.segments = segments;
+    a.group = g;
+    a.group.b_stride = b_stride;
+    return a;
+}
+
+}  // namespace
+
+int rows_of_tile(ProductKernel kernel) { return kernel == K_FEW ? 16 : kernel == K_TINY ? 64 : kernel == K_LARGE ? 256 : 128; }
+
+}  // namespace dn
+
+using namespace dn;
+
+extern "C" {
+
+size_t dn_experts_forward_workspace_bytes(const dn_experts_desc *d)
+{
+    Block b;
+    return block_of(d, b) == DN_OK ? b.fwd_bytes : kBad;
+}
+
+size_t dn_experts_backward_workspace_bytes(const dn_experts_desc *d)
+{
+    Block b;
+    return block_of(d, b) == DN_OK ? b.bwd_bytes : kBad;
+}
+
+dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
+                             const float *weight_dev, const int32_t *starts_dev, const int32_t *order_dev, const int32_t *place_dev,
+                             const void *R_dev, void *Y_dev, void *GU_dev, void *workspace_dev, size_t workspace_bytes,
+                             void *hip_stream)
+{
+    Block b;
+    dn_status s = block_of(d, b);
+    if (s != DN_OK) return s;
+    if (!X_dev || !Wg_dev || !Wu_dev || !Wd_dev || !weight_dev || !starts_dev || !order_dev || !place_dev || !Y_dev) return DN_ERR_INVALID_ARG;
+    if (!multiples(d->type, X_dev, Wg_dev, Wu_dev, Wd_dev, R_dev, Y_dev, GU_dev) || !multiples(DN_F32, weight_dev, starts_dev, order_dev, place_dev))
+        return DN_ERR_INVALID_ARG;
+    if (!b.pack_w && ((uintptr_t)Wg_dev | (uintptr_t)Wu_dev | (uintptr_t)Wd_dev) % 16) return DN_ERR_INVALID_ARG;
+    if ((s = workspace(b.fwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const int64_t e = size_of(d->type), n = d->experts;
+    char *H = static_cast<char *>(workspace_dev), *z = H + b.h;
+    const Group g{starts_dev, order_dev, d->experts, d->k, (int32_t)b.pairs, d->rows, 0, 0};
+    ProductArgs a = product(g, 0, d->f, d->d, 1, 0), c = product(g, 0, d->d, d->f, 1, 0);
+    Packer pack{d->type, z + b.z};
+    if (b.up == K_FEW) {
+        operand_a(a, {X_dev, b.d.ldx * e, d->d});
+        operand_b(a, {Wg_dev, d->d * e, d->d});
+        a.b[1] = Wu_dev;
+    } else {
+        operand_a(a, pack.take(X_dev, b.d.ldx, d->rows, d->d));
+        operand_b(a, pack.take(Wg_dev, d->d, n * d->f, d->d, b.pack_w));
+        a.b[1] = pack.take(Wu_dev, d->d, n * d->f, d->d, b.pack_w).p;
+    }
+    if (b.down == K_FEW) operand_b(c, {Wd_dev, d->f * e, d->f});
+    else operand_b(c, pack.take(Wd_dev, d->f, n * d->d, d->f, b.pack_w));
+    if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    a.group.b_stride = a.ldb * d->f;
+    a.f.y = H;
+    a.f.ldy = b.ldh;
+    a.f.zeros = (int)(b.ldh - d->f);
+    a.f.y2 = GU_dev;
+    a.f.ldy2 = 2 * (int64_t)d->f;
+    a.f.half = d->f;
+    a.f.act = d->act;
+    if (launch_experts(d->type, P_FWD, E_GATED, b.up, a, most_tiles(b.pairs, d->experts, rows_of_tile(b.up)), stream) != hipSuccess) return DN_ERR_DEVICE;
+    operand_a(c, {H, b.ldh * e, (int32_t)b.ldh});
+    c.group.b_stride = c.ldb * d->d;
+    c.f.y = z;
+    c.f.ldy = b.ldz;
+    if (launch_experts(d->type, P_FWD, E_STORE, b.down, c, most_tiles(b.pairs, d->experts, rows_of_tile(b.down)), stream) != hipSuccess) return DN_ERR_DEVICE;
+    return device(launch_join(d->type, {z, R_dev, Y_dev, b.ldz, b.d.ldr, b.d.ldy, weight_dev, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream));
+}
+
+dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
+                              const float *weight_dev, const int32_t *starts_dev, const int32_t *order_dev, const int32_t *place_dev,
+                              const void *GU_dev, const void *dY_dev, void *dX_dev, void *dWg_dev, void *dWu_dev, void *dWd_dev,
+                              float *dweight_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    Block b;
+    dn_status s = block_of(d, b);
+    if (s != DN_OK) return s;
+    if (!X_dev || !Wg_dev || !Wu_dev || !Wd_dev || !weight_dev || !starts_dev || !order_dev || !place_dev || !GU_dev || !dY_dev || !dWg_dev ||
+        !dWu_dev || !dWd_dev)
+        return DN_ERR_INVALID_ARG;
+    if (!multiples(d->type, X_dev, Wg_dev, Wu_dev, Wd_dev, GU_dev, dY_dev, dX_dev) || !multiples(d->grad_type, dWg_dev, dWu_dev, dWd_dev) ||
+        !multiples(DN_F32, weight_dev, starts_dev, order_dev, place_dev, dweight_dev))
+        return DN_ERR_INVALID_ARG;
+    if (!b.pack_w && ((uintptr_t)Wg_dev | (uintptr_t)Wu_dev | (uintptr_t)Wd_dev) % 16) return DN_ERR_INVALID_ARG;
+    if ((s = workspace(b.bwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const int64_t e = size_of(d->type), n = d->experts, f = d->f;
+    char *xs = static_cast<char *>(workspace_dev), *dys = xs + b.z, *sorted = dys + b.z, *dots = sorted + b.sorted, *H = dots + b.dots;
+    char *dG = H + b.h, *dU = dG + b.ldh * e, *dx = dG + b.dgu;
+    const Group g{starts_dev, order_dev, d->experts, d->k, (int32_t)b.pairs, d->rows, 0, 0};
+    Packer pack{d->type, dx + b.z};
+    const Packer::Rows Wd = pack.take(Wd_dev, f, n * d->d, f, b.pack_w);
+    const Packer::Rows Wg = dX_dev ? pack.take(Wg_dev, d->d, n * f, d->d, b.pack_w) : Packer::Rows{};
+    const Packer::Rows Wu = dX_dev ? pack.take(Wu_dev, d->d, n * f, d->d, b.pack_w) : Packer::Rows{};
+    if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
+    if (launch_sort(d->type, {{X_dev, dY_dev}, {xs, dys}, {b.d.ldx, b.d.ldy}, weight_dev, reinterpret_cast<float *>(sorted), g, d->d}, stream) != hipSuccess)
+        return DN_ERR_DEVICE;
+    auto tiles = [&](ProductKernel k) { return most_tiles(b.pairs, d->experts, rows_of_tile(k)); };
+    const Packer::Rows Xs{xs, b.ldz * e, (int32_t)b.ldz}, dYs{dys, b.ldz * e, (int32_t)b.ldz};
+    {   // dh, and from it dG, dU, w H and the weights' derivatives
+        ProductArgs a = product(g, 0, d->f, d->d, 1, Wd.ld * d->d);
+        operand_a(a, dYs);
+        operand_b(a, Wd);
+        a.f.y = dG;
+        a.f.ldy = 2 * b.ldh;
+        a.f.half_y = b.ldh;
+        a.f.zeros = (int)(b.ldh - f);
+        a.f.y2 = H;
+        a.f.ldy2 = b.ldh;
+        a.f.r = GU_dev;
+        a.f.ldr = 2 * f;
+        a.f.half = f;
+        a.f.act = d->act;
+        a.f.row_scale = reinterpret_cast<const float *>(sorted);
+        a.f.dots = reinterpret_cast<float *>(dots);
+        a.f.dots_ld = b.pairs;
+        if (launch_experts(d->type, P_DELTA, E_DEXPERT, b.dh, a, tiles(b.dh), stream) != hipSuccess) return DN_ERR_DEVICE;
+    }
+    if (dweight_dev) {
+        const int cols = b.dh == K_SMALL || b.dh == K_TINY ? 128 : 256, parts = (int)((f + cols - 1) / cols * (cols / 64));
+        launch_kernel(dots_kernel, dim3((unsigned)((b.pairs + 255) / 256)), dim3(256), 0, stream, reinterpret_cast<const float *>(dots), parts, g, place_dev,
+                      dweight_dev);
+        if (hipGetLastError() != hipSuccess) return DN_ERR_DEVICE;
+    }
+    if (dX_dev) {
+        ProductArgs a = product(g, 0, d->d, d->f, 2, Wg.ld * f);
+        operand_a(a, {dG, 2 * b.ldh * e, (int32_t)b.ldh});
+        a.a[1] = dU;
+        operand_b(a, Wg);
+        a.b[1] = Wu.p;
+        a.f.y = dx;
+        a.f.ldy = b.ldz;
+        if (launch_experts(d->type, P_DELTA, E_STORE, b.dx, a, tiles(b.dx), stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_join(d->type, {dx, nullptr, dX_dev, b.ldz, 0, d->d, nullptr, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream) != hipSuccess)
+            return DN_ERR_DEVICE;
+    }
+    const bool f32_out = d->grad_type == DN_F32;
+    const int64_t matrix = (int64_t)d->d * f * size_of(d->grad_type);
+    {   // dWg and dWu: the columns of dG (and of the zeros up to ldh), then those of dU
+        ProductArgs a = product(g, (int)(2 * b.ldh), d->d, 0, 1, 0);
+        operand_a(a, {dG, 2 * b.ldh * e, (int32_t)(2 * b.ldh)});
+        operand_b(a, Xs);
+        a.group.c_stride = matrix;
+        a.f.y = dWg_dev;
+        a.f.ldy = d->d;
+        a.f.y2 = dWu_dev;
+        a.f.ldy2 = d->d;
+        a.f.m_split = (int)b.ldh;
+        a.f.m_valid = d->f;
+        a.f.f32_out = f32_out;
+        a.f.alpha = d->grad_scale;
+        if (launch_experts(d->type, P_GRAD, E_STORE, b.dwgu, a, 0, stream) != hipSuccess) return DN_ERR_DEVICE;
+    }
+    ProductArgs a = product(g, d->d, d->f, 0, 1, 0);
+    operand_a(a, dYs);
+    operand_b(a, {H, b.ldh * e, (int32_t)b.ldh});
+    a.group.c_stride = matrix;
+    a.f.y = dWd_dev;
+    a.f.ldy = f;
+    a.f.f32_out = f32_out;
+    a.f.alpha = d->grad_scale;
+    return device(launch_experts(d->type, P_GRAD, E_STORE, b.dwd, a, 0, stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,11 @@
+// The experts' matrix products on fp32 operands.
+#include "dn_experts_launch.h"
+
+namespace dn {
+
+hipError_t launch_experts_f32(Product p, Epilogue e, ProductKernel kernel, ProductArgs a, int64_t tiles, hipStream_t s)
+{
+    return launch_experts<float>(p, e, kernel, a, tiles, s);
+}
+
+}  // namespace dn

@@ -193,7 +193,8 @@ enum Epilogue : int {
     E_LINEAR = 0,  // P_FWD: + bias, activation, dropout, residual; the net input too
     E_GATED = 1,   // P_FWD of two matrices B: f(g) u; g and u too
     E_DGATED = 2,  // P_DELTA: d(f(g) u) from its derivative: dG, dU, and f(g) u again
-    E_STORE = 3    // alpha times the sum, as T or as fp32
+    E_STORE = 3,   // alpha times the sum, as T or as fp32
+    E_DEXPERT = 4  // as E_DGATED, each row times its weight; and the weight's derivative
 };
 
 struct Finish {
@@ -212,8 +213,25 @@ struct Finish {
     int32_t act = 0;
     int32_t f32_out = 0;        // E_STORE: results are fp32 whatever T is
     float alpha = 1.f;
+    const float *row_scale = nullptr;   // E_DEXPERT: a row's weight
+    float *dots = nullptr;              // E_DEXPERT: parts of the weights' derivatives, [64 columns each][rows], rows dots_ld apart
+    int64_t dots_ld = 0;
     Dropout drop;
 };
+
+// Rows that are pairs of a row and one of several experts, by expert
+struct Group {
+    const int32_t *starts = nullptr, *order = nullptr;   // an expert's first pair, [experts + 1]; the pair at a place
+    int32_t experts = 0, k = 1, pairs = 0, rows = 0;     // k: pairs of a row
+    int64_t b_stride = 0, c_stride = 0;                  // bytes between two experts' matrices; their results (P_GRAD)
+};
+
+__device__ __forceinline__ int bounded(const Group &g, int e) { return min(max(g.starts[e], 0), g.pairs); }
+// the row of X that the pair at place m is of; whatever the lists hold, a row that exists
+__device__ __forceinline__ int token_of(const Group &g, int m)
+{
+    return (int)min((uint32_t)max(g.order[m], 0) / (uint32_t)g.k, (uint32_t)g.rows - 1);
+}
 
 struct ProductArgs {
     const void *a[2], *b[2];    // operands; the second ones: of the second segment of k, or (E_GATED) of the second matrix
@@ -225,6 +243,7 @@ struct ProductArgs {
     int32_t split, steps;       // k steps of each part
     int32_t tiles_m, tiles_n;
     Finish f;
+    Group group;
 };
 
 constexpr int kFewRows = 64;    // most rows of the kernel that stages nothing

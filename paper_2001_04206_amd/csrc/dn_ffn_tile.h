@@ -83,6 +83,7 @@ __device__ __forceinline__ float add_all(const v4u &a, float c, float)
 template <class T, int EPI>
 struct Beside {
     typename Eight<T>::type r, u;    // a row's
+    float by;                        // E_DEXPERT: its weight
     typename Eight<T>::type b, b2;   // its columns'
     template <bool ALL>
     __device__ __forceinline__ void columns(const Finish &e, int n, int left)
@@ -94,10 +95,11 @@ struct Beside {
     __device__ __forceinline__ void get(const Finish &e, int m, int n, int left)
     {
         if (EPI == E_LINEAR && e.r) r = get8<T, ALL>(e.r, m * e.ldr + n, left);
-        if (EPI == E_DGATED) {
+        if (EPI == E_DGATED || EPI == E_DEXPERT) {
             r = get8<T, ALL>(e.r, m * e.ldr + n, left);
             u = get8<T, ALL>(e.r, m * e.ldr + n + e.half, left);
         }
+        if (EPI == E_DEXPERT) by = e.row_scale[m];
     }
 };
 
@@ -157,6 +159,28 @@ __device__ __forceinline__ void finish8(const Finish &e, const Beside<T, EPI> &s
         store8<T, ALL, ALL>(e.y, m * e.ldy + n, v, left + e.zeros);
         store8<T, ALL, ALL>(e.y, m * e.ldy + n + e.half_y, w, left + e.zeros);
         store8<T, ALL, ALL>(e.y2, m * e.ldy2 + n, h, left + e.zeros);
+    } else if constexpr (EPI == E_DEXPERT) {
+        // `v` comes in as dh.  The row's weight goes into dG, dU and H, so that the three products that read them need none; the
+        // weight's own derivative is the row's sum of dh h, of which w[0] takes these columns' part.
+        float g[8], f[8], df[8], h[8], dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = (float)side.r[j];
+        act8<FAST>(e.act, g, f, df);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float u = !ALL && j >= left ? 0.f : (float)side.u[j];
+            if (!ALL && j >= left) v[j] = f[j] = df[j] = 0.f;
+            h[j] = u * f[j];
+            dot = fmaf(v[j], h[j], dot);
+            v[j] *= side.by;
+            h[j] *= side.by;
+            w[j] = v[j] * f[j];
+            v[j] *= u * df[j];
+        }
+        store8<T, ALL, ALL>(e.y, m * e.ldy + n, v, left + e.zeros);
+        store8<T, ALL, ALL>(e.y, m * e.ldy + n + e.half_y, w, left + e.zeros);
+        store8<T, ALL, ALL>(e.y2, m * e.ldy2 + n, h, left + e.zeros);
+        w[0] = dot;
     } else {
         const int row = m < e.m_split ? m : m - e.m_split;
         if (row >= e.m_valid) return;
@@ -188,8 +212,10 @@ __device__ __forceinline__ void finish_sum(const Finish &e, int m, float v)
 // Each spreads what the lanes of one read touch over all banks; the last one's reads have their blocks at constant
 // distances of two addresses, where an exclusive-or of three bits would take an address register for each of eight blocks.
 // PAIR (KC): rows 0..15, 32..47, .. are of the first matrix, the rows between them of the second.
-template <class T, int R, int NW, bool MC, bool PAIR>
+// GATHER (KC): row r of the tile is any row of the matrix, which lies within 2^31 bytes.
+template <class T, int R, int NW, bool MC, bool PAIR, bool GATHER = false>
 struct Operand {
+    static_assert(!GATHER || (!MC && !PAIR), "rows are gathered along k");
     static constexpr bool MC_ = MC;
     static constexpr int Q = R / 8 / NW;             // pieces of a wave
     static constexpr int BK = 128 / (int)sizeof(T);  // k of a stage
@@ -198,7 +224,7 @@ struct Operand {
     static constexpr int PIECE = PAD ? 1056 : 1024, STAGE = R / 8 * PIECE;
     static constexpr int READS = MC ? (sizeof(T) == 2 ? 2 : 4) : 1;   // LDS instructions of a fragment
     static_assert(!MC || RB >= 256, "the exclusive-or of MC needs rows of 256 bytes");
-    static constexpr bool HOP = !MC || sizeof(T) == 2;   // the lane's chunks lie one distance apart
+    static constexpr bool HOP = !GATHER && (!MC || sizeof(T) == 2);   // the lane's chunks lie one distance apart
     uint32_t off[HOP ? 1 : Q], hop;   // byte offsets of the lane's chunks in the first stage of a segment
     uint32_t kbyte;    // KC: its byte within the stage's k
     const char *base, *next;   // first row of the tile, in this segment and the second one
@@ -236,6 +262,20 @@ struct Operand {
         }
     }
 
+    // GATHER: `at` gives the row of the matrix of a row of the tile, of which `total` exist
+    template <class F>
+    __device__ __forceinline__ void init_rows(const void *p, int64_t ld_, F at, int total, int wave, int lane)
+    {
+        ld = ld_;
+        rows = total;
+        base = next = static_cast<const char *>(p);
+        const int r = 8 * (wave & 1) + (lane >> 3);
+        kbyte = (uint32_t)(((lane & 7) ^ ((r >> 1) & 7)) * 16);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) off[q] = (uint32_t)(at(r + 16 * ((wave >> 1) + q * (NW / 2))) * ld) + kbyte;
+        hop = 0;
+    }
+
     // Stage `step` of a segment (K elements long) from memory straight into LDS (zeros if it is not `valid`).  What lies outside
     // the matrix becomes zero or (columns of MC beyond the tile) a number that no result depends on.  Pieces of 16 bytes lie inside
     // or outside whole.  aim() holds the arithmetic, so that it is out of the way when the loads are due.
@@ -250,6 +290,7 @@ struct Operand {
         const char *b = (second ? next : base) + (MC ? (int64_t)k0 * ld : (int64_t)k0 * (int)sizeof(T));
         const int64_t bytes = MC ? (int64_t)(min(kleft, BK) - 1) * ld + rows * (int)sizeof(T) : (int64_t)(rows - 1) * ld + kleft * (int)sizeof(T);
         const bool in = valid && (MC || (int)kbyte < kleft * (int)sizeof(T));
+        if (GATHER) return {b, valid ? (int)bytes : 0, in ? 0 : 0x80000000u};
         return {b, valid ? (int)bytes : 0, in ? off[0] : 0x80000000u};
     }
     __device__ __forceinline__ void fetch(lds_char *lds, const Aim &at, int wave) const
@@ -258,7 +299,7 @@ struct Operand {
 #pragma unroll
         for (int q = 0; q < Q; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * PIECE), 16,
-                                                     (int)(HOP ? at.first + q * hop : offset(q)), 0, 0, 0);
+                                                     (int)(HOP ? at.first + q * hop : GATHER ? at.first + off[q] : offset(q)), 0, 0, 0);
     }
 
     // Fragments: sixteen rows from 16 block on, half kk (64 bytes of k) of the stage.  `at` from start(), block a constant
@@ -378,11 +419,87 @@ typedef Shape<2, 4, 4, 4, 3> Medium;   // 128 x 256, 8 waves; the third stage ma
 typedef Shape<2, 2, 4, 4, 2> Small;    // 128 x 128, 4 waves, two workgroups a compute unit
 typedef Shape<2, 2, 2, 4, 2> Tiny;     // 64 x 128, 4 waves, three
 
-template <class T, int P, int EPI, class S, bool SUMS>
-__global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs a)
+// The experts' products: one kernel's tiles are of all of them.  Rows 0 .. P of the result are pairs of a row and an expert, by expert;
+// expert e has those from starts[e] on.  G_ROWS: row m of A is row m of the matrix.  G_TOKENS: it is the pair's row, order[m] div k.
+// G_TERMS (P_GRAD): an expert's rows are its terms, every expert has a result of its own.
+enum Grouping : int { G_NONE, G_ROWS, G_TOKENS, G_TERMS };
+
+// Expert and first row of tile t of BM rows each, of `tiles` in all; every lane of the wave takes part.  A few loads that the L2 has: 64
+// experts at a time, a lane each.
+struct GroupTile { int expert, first, end; };
+__device__ __forceinline__ int tiles_before(const Group &g, int e0, int bm, int lane, int &from, int &to)
 {
-    constexpr bool PAIR = EPI == E_GATED;
-    typedef Operand<T, S::BM, S::NW, P == P_GRAD, false> OpA;
+    const int e = min(e0 + lane, g.experts - 1);
+    from = bounded(g, e);
+    to = max(bounded(g, e + 1), from);
+    int n = e0 + lane < g.experts ? (to - from + bm - 1) / bm : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(n, o);
+        n += lane >= o ? v : 0;
+    }
+    return n;   // of this lane's expert and those before it from e0 on
+}
+__device__ __forceinline__ int tiles_of_all(const Group &g, int bm, int lane)
+{
+    int n = 0, from, to;
+    for (int e0 = 0; e0 < g.experts; e0 += 64) n += __builtin_amdgcn_readlane(tiles_before(g, e0, bm, lane, from, to), 63);
+    return n;
+}
+__device__ __forceinline__ GroupTile tile_in_group(const Group &g, int t, int bm, int lane)
+{
+    for (int e0 = 0; e0 < g.experts; e0 += 64) {
+        int from, to;
+        const int n = tiles_before(g, e0, bm, lane, from, to), last = __builtin_amdgcn_readlane(n, 63);
+        if (t < last) {
+            const int l = __builtin_ctzll(__ballot(t < n));   // the first expert that has it
+            const int end = __builtin_amdgcn_readlane(to, l), after = __builtin_amdgcn_readlane(n, l), start = __builtin_amdgcn_readlane(from, l);
+            const int all = (end - start + bm - 1) / bm;
+            return {e0 + l, start + (t - (after - all)) * bm, end};
+        }
+        t -= last;
+    }
+    return {0, 0, 0};
+}
+template <class T, int P, int EPI, class S, bool SUMS, int GROUP = G_NONE>
+__global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs arg)
+{
+    constexpr bool PAIR = EPI == E_GATED, GATHER = GROUP == G_TOKENS;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int tm, tn, m0;
+    ProductArgs mine;   // this expert's product; its operands lie so many bytes on
+    int64_t a_on = 0, b_on = 0;
+    if constexpr (GROUP != G_NONE) {
+        mine = arg;
+        const Group &g = arg.group;
+        int e;
+        if constexpr (GROUP == G_TERMS) {
+            e = blockIdx.y;
+            const int from = bounded(g, e), to = bounded(g, e + 1);
+            mine.K = max(to - from, 0);
+            a_on = from * arg.lda;
+            b_on = from * arg.ldb;
+            mine.steps = (mine.K + 128 / (int)sizeof(T) - 1) / (128 / (int)sizeof(T));
+            mine.f.y = static_cast<char *>(arg.f.y) + e * g.c_stride;
+            mine.f.y2 = static_cast<char *>(arg.f.y2) + e * g.c_stride;
+            tile_of(blockIdx.x, arg.tiles_m, arg.tiles_n, tm, tn);
+            m0 = tm * S::BM;
+        } else {
+            const int all = min(tiles_of_all(g, S::BM, lane), arg.tiles_m);   // (whatever the lists hold)
+            if ((int)blockIdx.x >= all * arg.tiles_n) return;
+            tile_of(blockIdx.x, all, arg.tiles_n, tm, tn);
+            const GroupTile t = tile_in_group(g, tm, S::BM, lane);
+            m0 = t.first;
+            mine.M = t.end;
+            b_on = t.expert * g.b_stride;
+        }
+    } else {
+        tile_of(blockIdx.x, arg.tiles_m, arg.tiles_n, tm, tn);
+        m0 = tm * S::BM;
+    }
+    const ProductArgs &a = GROUP != G_NONE ? mine : arg;
+    const int part_of_k = GROUP != G_NONE ? 0 : blockIdx.y;
+    typedef Operand<T, S::BM, S::NW, P == P_GRAD, false, GATHER> OpA;
     typedef Operand<T, S::BN, S::NW, P != P_FWD, PAIR> OpB;
     constexpr int COLS = PAIR ? S::BN / 2 : S::BN;
     constexpr int A_BYTES = OpA::STAGE;
@@ -390,18 +507,22 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     __shared__ __attribute__((aligned(1024))) char stage0[A_BYTES + OpB::STAGE];
     __shared__ __attribute__((aligned(1024))) char stage1[A_BYTES + OpB::STAGE];
     __shared__ __attribute__((aligned(1024))) char stage2[S::NB == 3 ? A_BYTES + OpB::STAGE : 16];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int tm, tn;
-    tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
-    const int m0 = tm * S::BM, n0 = tn * COLS;
+    const int n0 = tn * COLS;
     const int wm = wave / S::WN, wn = wave % S::WN;
 
     OpA oa;
     OpB ob;
-    oa.init(a.a, a.lda, m0, OpA::MC_ ? a.a_ext : a.M, wave, lane);
-    ob.init(a.b, a.ldb, n0, OpB::MC_ ? a.b_ext : a.N, wave, lane);
+    if constexpr (GATHER) oa.init_rows(arg.a[0], a.lda, [&](int r) { return token_of(a.group, min(m0 + r, a.M - 1)); }, a.group.rows, wave, lane);
+    else oa.init(arg.a, a.lda, m0, OpA::MC_ ? a.a_ext : a.M, wave, lane);
+    ob.init(arg.b, a.ldb, n0, OpB::MC_ ? a.b_ext : a.N, wave, lane);
+    if (GROUP != G_NONE) {
+        oa.base += a_on;
+        oa.next += a_on;
+        ob.base += b_on;
+        ob.next += b_on;
+    }
     const int per_seg = (a.K + OpA::BK - 1) / OpA::BK, all = per_seg * a.segments;
-    const int t0 = blockIdx.y * a.steps, t1 = min(all, t0 + a.steps);
+    const int t0 = part_of_k * a.steps, t1 = min(all, t0 + a.steps);
 
     v4f acc[S::TM][S::TN] = {};
     float sum[SUMS ? S::TM : 1] = {};   // the lane's part of A's sums over k
@@ -502,11 +623,11 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             float v = sum[i] + __shfl_xor(sum[i], 16);
             v += __shfl_xor(v, 32);
             if (h == 0 && m < a.M) {
-                if (a.split > 1) a.ws[a.split * plane + (int64_t)blockIdx.y * a.M + m] = v;
+                if (a.split > 1) a.ws[a.split * plane + (int64_t)part_of_k * a.M + m] = v;
                 else finish_sum<T>(a.f, m, v);
             }
         }
-    float *part = a.ws + blockIdx.y * plane * (PAIR ? 2 : 1);
+    float *part = a.ws + part_of_k * plane * (PAIR ? 2 : 1);
     constexpr int EACH_STAGE = (S::NW + S::NB - 1) / S::NB;   // waves
     constexpr int BLOCKS = S::TM < 4 ? S::TM : 4, ROWS = BLOCKS * 16;   // at a time
     static_assert(EACH_STAGE * ROWS * 256 <= A_BYTES + OpB::STAGE, "a wave's own part of a stage");
@@ -571,7 +692,14 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
                     const int m = first + r + q * STEP;
                     float v[8], w[8];
                     sums_of(r + q * STEP, v, w);
+                    if (EPI == E_DEXPERT) w[0] = 0.f;
                     if (ALL || (m < a.M && n < a.N)) finish8<T, EPI, ALL>(a.f, side[q], m, n, left, v, w);
+                    if constexpr (EPI == E_DEXPERT) {   // the eight lanes of a row
+                        float dot = w[0] + __shfl_xor(w[0], 1);
+                        dot += __shfl_xor(dot, 2);
+                        dot += __shfl_xor(dot, 4);
+                        if (c == 0 && m < a.M) a.f.dots[(int64_t)(tn * S::WN + wn) * a.f.dots_ld + m] = dot;
+                    }
                 }
             }
             exchanged();

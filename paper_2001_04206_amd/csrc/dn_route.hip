@@ -1,0 +1,536 @@
+// Routing of rows to experts: choices and weights from logits, the lists of rows by expert, and the logits' gradient.
+#include <type_traits>
+
+#include "dn_ffn_host.h"
+#include "dn_wave.h"
+
+namespace dn {
+namespace {
+
+constexpr int kMostExperts = 1024, kMostChoices = 32, kWaves = 4;
+constexpr int64_t kMostRows = (int64_t)1 << 26, kMostPairs = (int64_t)1 << 30;
+
+struct RouteArgs {
+    const void *l;
+    const float *bias;
+    int32_t *expert;
+    float *weight;
+    const int32_t *chosen;    // backward: expert
+    const float *dweight;
+    void *dl;
+    int64_t ldl;
+    int32_t rows, experts, k;
+    int32_t groups, each, top_groups, best;   // each: experts of a group
+    int32_t score, renorm;
+    float scale;
+};
+
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ double dpp_move64(double v, double identity)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v), i = __builtin_bit_cast(uint64_t, identity);
+    const uint32_t lo = __builtin_amdgcn_update_dpp((int)(uint32_t)i, (int)(uint32_t)b, CTRL, ROW_MASK, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp((int)(uint32_t)(i >> 32), (int)(uint32_t)(b >> 32), CTRL, ROW_MASK, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double last_lane(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, 63), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ float highest(float v) { return wave_max(v); }
+__device__ __forceinline__ double highest(double v)
+{
+    const double ninf = -INFINITY;
+    v = fmax(v, dpp_move64<0xB1, 0xf>(v, ninf));
+    v = fmax(v, dpp_move64<0x4E, 0xf>(v, ninf));
+    v = fmax(v, dpp_move64<0x141, 0xf>(v, ninf));
+    v = fmax(v, dpp_move64<0x140, 0xf>(v, ninf));
+    v = fmax(v, dpp_move64<0x142, 0xa>(v, ninf));
+    v = fmax(v, dpp_move64<0x143, 0xc>(v, ninf));
+    return last_lane(v);
+}
+__device__ __forceinline__ double total(double v)
+{
+    v += dpp_move64<0xB1, 0xf>(v, 0.);
+    v += dpp_move64<0x4E, 0xf>(v, 0.);
+    v += dpp_move64<0x141, 0xf>(v, 0.);
+    v += dpp_move64<0x140, 0xf>(v, 0.);
+    v += dpp_move64<0x142, 0xa>(v, 0.);
+    v += dpp_move64<0x143, 0xc>(v, 0.);
+    return last_lane(v);
+}
+
+// sigmoid(l) e^-low, low <= 0 and not below the largest of the logits that are compared (or 0): ratios of small scores keep their bits
+__device__ __forceinline__ float sigmoid_above(float l, float low)
+{
+    const float e = expf(-fabsf(l)), q = 1.f / (1.f + e);
+    return l >= 0.f ? q : l == l ? expf(l - low) * q : l;
+}
+
+// The weights of choices, lane j the one of logit l where it is `mine`: m, sum are the row's (softmax without renorm).
+__device__ __forceinline__ float weight_of(const RouteArgs &a, float l, bool mine, float m, float sum)
+{
+    float x;
+    if (a.score == DN_SCORE_SOFTMAX) {
+        if (a.renorm) m = wave_max(mine ? l : -INFINITY);
+        x = expf(l - m);
+    } else {
+        x = sigmoid_above(l, a.renorm ? fminf(0.f, wave_max(mine ? l : -INFINITY)) : 0.f);
+    }
+    if (a.renorm) sum = wave_sum(mine ? x : 0.f);
+    if (a.renorm || a.score == DN_SCORE_SOFTMAX) x /= sum;
+    return x * a.scale;
+}
+
+// A wave takes a row, a lane V neighbouring experts of it.  The highest of all lanes, k times: of equal ones the lowest lane holds the
+// lowest expert.  WIDE: ranks are scores in 64 bits plus the bias; otherwise the logits themselves.
+template <class T, int V, bool WIDE>
+__global__ __launch_bounds__(kWaves * 64) void route_kernel(const RouteArgs a)
+{
+    typedef typename std::conditional<WIDE, double, float>::type Rank;
+    const int lane = threadIdx.x & 63, row = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = lane * V;
+    if (row >= a.rows) return;
+    const Rank ninf = -INFINITY;
+    const T *p = static_cast<const T *>(a.l) + row * a.ldl;
+    float l[V], high = -INFINITY;
+    Rank c[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        l[i] = first + i < a.experts ? (float)p[first + i] : -INFINITY;
+        high = fmaxf(high, l[i]);
+    }
+    float m = -INFINITY, sum = 1.f;
+    if (a.score == DN_SCORE_SOFTMAX) m = wave_max(high);
+    if constexpr (WIDE) {
+        if (a.score == DN_SCORE_SOFTMAX) {
+            double s = 0.;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                c[i] = l[i] == -INFINITY ? 0. : exp((double)l[i] - (double)m);
+                s += c[i];
+            }
+            s = total(s);
+            sum = (float)s;
+#pragma unroll
+            for (int i = 0; i < V; ++i) c[i] /= s;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) c[i] = 1. / (1. + exp(-(double)l[i]));
+        }
+        if (a.bias)
+#pragma unroll
+            for (int i = 0; i < V; ++i) c[i] += first + i < a.experts ? (double)a.bias[first + i] : 0.;
+    } else {
+        if (a.score == DN_SCORE_SOFTMAX && !a.renorm) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) s += l[i] == -INFINITY ? 0.f : expf(l[i] - m);
+            sum = wave_sum(s);
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) c[i] = l[i];
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) c[i] = l[i] == -INFINITY ? ninf : c[i] == c[i] ? c[i] : (Rank)INFINITY;
+    if (a.top_groups < a.groups) {
+        Rank score = ninf;   // lane g: group g's
+        for (int g = 0; g < a.groups; ++g) {
+            const int from = g * a.each, to = from + a.each;
+            Rank b = ninf;
+#pragma unroll
+            for (int i = 0; i < V; ++i) b = first + i >= from && first + i < to && c[i] > b ? c[i] : b;
+            Rank best = highest(b);
+            if (a.best == 2 && best > ninf) {
+                const int f = __builtin_ctzll(__ballot(b == best));
+                bool skip = lane == f;
+                b = ninf;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (first + i >= from && first + i < to) {
+                        if (skip && c[i] == best) skip = false;   // once
+                        else b = c[i] > b ? c[i] : b;
+                    }
+                const Rank second = highest(b);
+                if (second > ninf) best += second;
+            }
+            if (lane == g) score = best;
+        }
+        uint64_t stay = 0;
+        for (int n = 0; n < a.top_groups; ++n) {
+            const Rank best = highest(score);
+            if (!(best > ninf)) break;
+            const int f = __builtin_ctzll(__ballot(score == best));
+            stay |= (uint64_t)1 << f;
+            if (lane == f) score = ninf;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (!(stay >> min((first + i) / a.each, 63) & 1)) c[i] = ninf;
+    }
+    int chosen = -1;
+    float logit = -INFINITY;   // lane j: of choice j
+    Rank b = ninf;
+#pragma unroll
+    for (int i = 0; i < V; ++i) b = c[i] > b ? c[i] : b;
+    for (int j = 0; j < a.k; ++j) {
+        const Rank best = highest(b);
+        if (!(best > ninf)) break;
+        const int f = __builtin_ctzll(__ballot(b == best));
+        int at = 0;
+        float mine = l[0];
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i)
+            if (c[i] == best) {
+                at = i;
+                mine = l[i];
+            }
+        const int e = f * V + __builtin_amdgcn_readlane(at, f);
+        const float le = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), f));
+        if (lane == j) {
+            chosen = e;
+            logit = le;
+        }
+        b = ninf;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (first + i == e) c[i] = ninf;
+            b = c[i] > b ? c[i] : b;
+        }
+    }
+    float w = weight_of(a, logit, chosen >= 0, m, sum);
+    if (!(sum == sum)) w = sum;   // a softmax of NaN or +inf, whose ranks name any expert
+    if (lane < a.k) {
+        a.expert[(int64_t)row * a.k + lane] = chosen;
+        a.weight[(int64_t)row * a.k + lane] = chosen >= 0 ? w : 0.f;
+    }
+}
+
+// With u = w / scale the weights without their scale and g = scale dw:
+//   softmax, renorm: dl_j = u_j (g_j - sum g u);  sigmoid, renorm: the same times 1 - s_j (chosen experts only, as every s drops out of
+//   the others' ratio);  sigmoid: dl_j = g_j s_j (1 - s_j);  softmax: dl = s (g - sum g s) over all of a row, g 0 but where chosen.
+template <class T, int V>
+__global__ __launch_bounds__(kWaves * 64) void route_back_kernel(const RouteArgs a)
+{
+    const int lane = threadIdx.x & 63, row = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = lane * V;
+    if (row >= a.rows) return;
+    const T *p = static_cast<const T *>(a.l) + row * a.ldl;
+    const int e = lane < a.k ? a.chosen[(int64_t)row * a.k + lane] : -1;
+    const bool mine = (uint32_t)e < (uint32_t)a.experts;
+    const float g = mine ? a.dweight[(int64_t)row * a.k + lane] * a.scale : 0.f, l = mine ? (float)p[e] : -INFINITY;
+    const bool dense = a.score == DN_SCORE_SOFTMAX && !a.renorm;
+    float s[V], m = 0.f, sum = 1.f, d;
+    if (dense) {
+        float high = -INFINITY, t = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            s[i] = first + i < a.experts ? (float)p[first + i] : -INFINITY;
+            high = fmaxf(high, s[i]);
+        }
+        m = wave_max(high);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            s[i] = s[i] == -INFINITY ? 0.f : expf(s[i] - m);
+            t += s[i];
+        }
+        sum = 1.f / wave_sum(t);
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] = t == 0.f && m == -INFINITY ? 0.f : s[i] * sum;
+        d = g;
+    } else {
+        RouteArgs one = a;
+        one.scale = 1.f;
+        float u = weight_of(one, l, mine, m, sum);   // (every lane takes part)
+        if (!mine) u = 0.f;
+        d = a.renorm ? u * (g - wave_sum(g * u)) : g * u;
+        if (a.score == DN_SCORE_SIGMOID) d *= sigmoid_above(-l, 0.f);   // 1 - s
+        if (!mine) d = 0.f;
+    }
+    float v[V] = {};
+    for (int j = 0; j < a.k; ++j) {
+        const int ej = __builtin_amdgcn_readlane(e, j);
+        const float dj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, d), j));
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += first + i == ej ? dj : 0.f;
+    }
+    if (dense) {
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) dot = fmaf(v[i], s[i], dot);
+        dot = wave_sum(dot);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = s[i] * (v[i] - dot);
+    }
+    T *q = static_cast<T *>(a.dl) + (int64_t)row * a.experts + first;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (first + i < a.experts) q[i] = (T)v[i];
+}
+
+// ---- lists -----------------------------------------------------------------------------------------------------------
+// A stable counting sort of the pairs by expert: workgroups count chunks, and then each adds up what lies before its own (every expert
+// before, and its own expert's pairs in earlier chunks) and gives its pairs their places in order.  Counts are whole numbers: the LDS
+// atomics that make them leave no order behind.
+struct ListArgs {
+    const int32_t *expert;
+    int32_t *starts, *order, *place, *counts;   // counts [chunks][experts]
+    int32_t pairs, experts, chunk, chunks;      // pairs of a chunk, a multiple of 1024
+};
+
+__global__ __launch_bounds__(256) void count_kernel(const ListArgs a)
+{
+    __shared__ int32_t count[kMostExperts];
+    for (int e = threadIdx.x; e < a.experts; e += 256) count[e] = 0;
+    __syncthreads();
+    const int from = blockIdx.x * a.chunk, to = min(a.pairs - from, a.chunk);
+    for (int i = threadIdx.x; i < to; i += 256) {
+        const int e = a.expert[from + i];
+        if ((uint32_t)e < (uint32_t)a.experts) atomicAdd(&count[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += 256) a.counts[blockIdx.x * a.experts + e] = count[e];
+}
+
+// one chunk: it counts itself
+__global__ __launch_bounds__(256) void place_kernel(const ListArgs a)
+{
+    __shared__ int32_t next[4][kMostExperts], all[kMostExperts], sums[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int from = blockIdx.x * a.chunk + wave * (a.chunk / 4), to = min(from + a.chunk / 4, a.pairs);   // the wave's pairs
+    for (int e = threadIdx.x; e < 4 * kMostExperts; e += 256) next[0][e] = 0;
+    __syncthreads();
+    for (int i = from + lane; i < to; i += 64) {
+        const int e = a.expert[i];
+        if ((uint32_t)e < (uint32_t)a.experts) atomicAdd(&next[wave][e], 1);
+    }
+    __syncthreads();
+    // `all`: an expert's pairs; next[w]: those of earlier chunks and of earlier waves of this one
+    for (int e = threadIdx.x; e < kMostExperts; e += 256) {
+        int own = 0, before = 0, sum = 0;
+        int32_t c[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            c[w] = own;
+            own += next[w][e];
+        }
+        if (e < a.experts) {
+            if (a.chunks == 1) sum = own;
+            else
+                for (int b = 0; b < a.chunks; ++b) {
+                    const int n = a.counts[b * a.experts + e];
+                    before += b < (int)blockIdx.x ? n : 0;
+                    sum += n;
+                }
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) next[w][e] = before + c[w];
+        all[e] = sum;
+    }
+    __syncthreads();
+    // where each expert's pairs begin: four experts a thread
+    int n[4], mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        n[i] = mine;
+        mine += all[threadIdx.x * 4 + i];
+    }
+    int until = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(until, o);
+        until += lane >= o ? v : 0;
+    }
+    if (lane == 63) sums[wave] = until;
+    __syncthreads();
+    int before = until - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        before += w < wave ? sums[w] : 0;
+        total += sums[w];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = threadIdx.x * 4 + i;
+        if (e >= a.experts) break;
+        const int start = before + n[i];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) next[w][e] += start;
+        if (blockIdx.x == 0) a.starts[e] = start;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.starts[a.experts] = total;
+    __syncthreads();
+    // sixty-four pairs at a time: a pair's place is its expert's next one and how many lanes below have the same expert
+    for (int i = from; i < to; i += 64) {
+        const int q = i + lane;
+        const int e = q < to ? a.expert[q] : -1;
+        const bool has = (uint32_t)e < (uint32_t)a.experts;
+        uint64_t same = __ballot(has);
+#pragma unroll
+        for (int b = 0; b < 10; ++b) {
+            const uint64_t set = __ballot(has && (e >> b & 1));
+            same &= e >> b & 1 ? set : ~set;
+        }
+        const int below = __popcll(same & (((uint64_t)1 << lane) - 1));
+        int p = -1;
+        if (has) {
+            p = next[wave][e] + below;
+            a.order[p] = q;
+        }
+        if (q < to) a.place[q] = p;
+        // every lane has read before one of each expert writes
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+        if (has && below == 0) next[wave][e] = p + __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    }
+    for (int p = max(from, total) + lane; p < to; p += 64) a.order[p] = -1;
+}
+
+constexpr int kMostChunks = 128;   // each workgroup reads all counts
+int chunk_of(int pairs) { return (pairs + 1024 * kMostChunks - 1) / (1024 * kMostChunks) * 1024; }
+
+dn_status sizes(int32_t rows, int32_t experts, int32_t k)
+{
+    return rows < 1 || experts < 1 || k < 1 || experts > kMostExperts || k > kMostChoices || rows >= kMostRows || (int64_t)rows * k >= kMostPairs
+               ? DN_ERR_SHAPE
+               : DN_OK;
+}
+
+size_t lists_bytes(int32_t rows, int32_t experts, int32_t k)
+{
+    const int pairs = rows * k, chunk = chunk_of(pairs), chunks = (pairs + chunk - 1) / chunk;
+    return chunks == 1 ? 0 : up256((size_t)chunks * experts * sizeof(int32_t));
+}
+
+hipError_t launch_lists(ListArgs a, hipStream_t s)
+{
+    a.chunk = chunk_of(a.pairs);
+    a.chunks = (a.pairs + a.chunk - 1) / a.chunk;
+    if (a.chunks > 1) launch_kernel(count_kernel, dim3(a.chunks), dim3(256), 0, s, a);
+    launch_kernel(place_kernel, dim3(a.chunks), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+dn_status route_of(const dn_route_desc *d, RouteArgs &a)
+{
+    a = RouteArgs{};
+    if (!d || !type_ok(d->type) || (d->score != DN_SCORE_SOFTMAX && d->score != DN_SCORE_SIGMOID)) return DN_ERR_INVALID_ARG;
+    if (!isfinite(d->scale) || (d->group_best != 1 && d->group_best != 2) || (d->renorm != 0 && d->renorm != 1)) return DN_ERR_INVALID_ARG;
+    const dn_status s = sizes(d->rows, d->experts, d->k);
+    if (s != DN_OK) return s;
+    if (d->groups < 1 || d->groups > 64 || d->experts % d->groups || d->top_groups < 1 || d->top_groups > d->groups) return DN_ERR_SHAPE;
+    a.each = d->experts / d->groups;
+    if (d->k > a.each * d->top_groups || (d->groups > 1 && d->group_best > a.each)) return DN_ERR_SHAPE;
+    a.ldl = d->ldl;
+    const dn_status r = row_length(d->type, a.ldl, d->experts);
+    if (r != DN_OK) return r;
+    a.rows = d->rows;
+    a.experts = d->experts;
+    a.k = d->k;
+    a.groups = d->groups;
+    a.top_groups = d->top_groups;
+    a.best = d->group_best;
+    a.score = d->score;
+    a.renorm = d->renorm;
+    a.scale = d->scale;
+    return DN_OK;
+}
+
+template <class T, int V>
+void forward_as(const RouteArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.rows + kWaves - 1) / kWaves)), block(kWaves * 64);
+    if (a.bias || (a.top_groups < a.groups && a.best == 2)) launch_kernel(route_kernel<T, V, true>, grid, block, 0, s, a);
+    else launch_kernel(route_kernel<T, V, false>, grid, block, 0, s, a);
+}
+template <class T, int V>
+void backward_as(const RouteArgs &a, hipStream_t s)
+{
+    launch_kernel(route_back_kernel<T, V>, dim3((unsigned)((a.rows + kWaves - 1) / kWaves)), dim3(kWaves * 64), 0, s, a);
+}
+template <class T>
+hipError_t run(const RouteArgs &a, bool back, hipStream_t s)
+{
+    if (a.experts <= 64) back ? backward_as<T, 1>(a, s) : forward_as<T, 1>(a, s);
+    else if (a.experts <= 128) back ? backward_as<T, 2>(a, s) : forward_as<T, 2>(a, s);
+    else if (a.experts <= 256) back ? backward_as<T, 4>(a, s) : forward_as<T, 4>(a, s);
+    else if (a.experts <= 512) back ? backward_as<T, 8>(a, s) : forward_as<T, 8>(a, s);
+    else back ? backward_as<T, 16>(a, s) : forward_as<T, 16>(a, s);
+    return hipGetLastError();
+}
+hipError_t launch_route(int type, const RouteArgs &a, bool back, hipStream_t s)
+{
+    return type == DN_F32 ? run<float>(a, back, s) : type == DN_F16 ? run<f16>(a, back, s) : run<bf16>(a, back, s);
+}
+
+template <class... P>
+bool words(const P *...p)
+{
+    return multiples(DN_F32, p...);
+}
+
+}  // namespace
+}  // namespace dn
+
+using namespace dn;
+
+extern "C" {
+
+size_t dn_route_workspace_bytes(int32_t rows, int32_t experts, int32_t k)
+{
+    return sizes(rows, experts, k) == DN_OK ? lists_bytes(rows, experts, k) : kBad;
+}
+
+dn_status dn_route_lists(const int32_t *expert_dev, int32_t rows, int32_t experts, int32_t k, int32_t *starts_dev, int32_t *order_dev,
+                         int32_t *place_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    if (!expert_dev || !starts_dev || !order_dev || !place_dev || !words(expert_dev, starts_dev, order_dev, place_dev)) return DN_ERR_INVALID_ARG;
+    dn_status s = sizes(rows, experts, k);
+    if (s != DN_OK) return s;
+    if ((s = workspace(lists_bytes(rows, experts, k), workspace_dev, workspace_bytes)) != DN_OK) return s;
+    return device(launch_lists({expert_dev, starts_dev, order_dev, place_dev, static_cast<int32_t *>(workspace_dev), rows * k, experts, 0, 0},
+                               (hipStream_t)hip_stream));
+}
+
+dn_status dn_route_forward(const dn_route_desc *d, const void *L_dev, const float *bias_dev, int32_t *expert_dev, float *weight_dev,
+                           int32_t *starts_dev, int32_t *order_dev, int32_t *place_dev, void *workspace_dev,
+                           size_t workspace_bytes, void *hip_stream)
+{
+    RouteArgs a;
+    dn_status s = route_of(d, a);
+    if (s != DN_OK) return s;
+    const bool lists = starts_dev || order_dev || place_dev;
+    if (!L_dev || !expert_dev || !weight_dev || (lists && !(starts_dev && order_dev && place_dev))) return DN_ERR_INVALID_ARG;
+    if (!multiples(d->type, L_dev) || !words(bias_dev, expert_dev, weight_dev, starts_dev, order_dev, place_dev)) return DN_ERR_INVALID_ARG;
+    if (lists && (s = workspace(lists_bytes(d->rows, d->experts, d->k), workspace_dev, workspace_bytes)) != DN_OK) return s;
+    a.l = L_dev;
+    a.bias = bias_dev;
+    a.expert = expert_dev;
+    a.weight = weight_dev;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (launch_route(d->type, a, false, stream) != hipSuccess) return DN_ERR_DEVICE;
+    if (!lists) return DN_OK;
+    return device(launch_lists({expert_dev, starts_dev, order_dev, place_dev, static_cast<int32_t *>(workspace_dev), d->rows * d->k, d->experts, 0, 0},
+                               stream));
+}
+
+dn_status dn_route_backward(const dn_route_desc *d, const void *L_dev, const int32_t *expert_dev, const float *dweight_dev,
+                            void *dL_dev, void *hip_stream)
+{
+    RouteArgs a;
+    const dn_status s = route_of(d, a);
+    if (s != DN_OK) return s;
+    if (!L_dev || !expert_dev || !dweight_dev || !dL_dev) return DN_ERR_INVALID_ARG;
+    if (!multiples(d->type, L_dev, dL_dev) || !words(expert_dev, dweight_dev)) return DN_ERR_INVALID_ARG;
+    a.l = L_dev;
+    a.chosen = expert_dev;
+    a.dweight = dweight_dev;
+    a.dl = dL_dev;
+    return device(launch_route(d->type, a, true, (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

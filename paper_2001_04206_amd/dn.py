@@ -22,6 +22,7 @@ DN_ACT_SILU, DN_ACT_GELU = 5, 6
 DN_LOSS_MSE, DN_LOSS_CROSS_ENTROPY = 0, 1
 DN_F32, DN_F16, DN_BF16 = range(3)
 DN_NORM_NONE, DN_NORM_RMS, DN_NORM_LAYER = range(3)
+DN_SCORE_SOFTMAX, DN_SCORE_SIGMOID = range(2)
 DN_K_FORWARD, DN_K_DELTA, DN_K_GRAD_UPDATE, DN_K_OUTPUT, DN_K_ONLINE = range(5)
 KERNEL_CLASS_NAMES = ["forward", "delta", "grad_update", "output", "online"]
 (DN_SCHED_NONE, DN_SCHED_LAUNCHES, DN_SCHED_PER_SAMPLE, DN_SCHED_TWO_COPY, DN_SCHED_MINIBATCH,
@@ -48,6 +49,9 @@ EXPORTS = [
     "dn_linear_forward_workspace_bytes", "dn_linear_backward_workspace_bytes", "dn_linear_forward", "dn_linear_backward",
     "dn_ffn_forward_workspace_bytes", "dn_ffn_backward_workspace_bytes", "dn_ffn_forward", "dn_ffn_backward",
     "dn_norm_backward_workspace_bytes", "dn_norm_forward", "dn_norm_backward", "dn_dropout",
+    "dn_route_workspace_bytes", "dn_route_forward", "dn_route_lists", "dn_route_backward",
+    "dn_experts_forward_workspace_bytes", "dn_experts_backward_workspace_bytes", "dn_experts_forward", "dn_experts_backward",
+    "dn_clip_workspace_bytes", "dn_clip",
 ]
 
 
@@ -71,6 +75,26 @@ class NormDesc(C.Structure):
     _fields_ = [("type", C.c_int32), ("grad_type", C.c_int32), ("rows", C.c_int32), ("d", C.c_int32),
                 ("post", C.c_int32), ("pre", C.c_int32), ("rows_per_gate", C.c_int32), ("scale", C.c_float),
                 ("eps", C.c_float)]
+
+
+class RouteDesc(C.Structure):
+    """dn_route_desc"""
+    _fields_ = [("type", C.c_int32), ("score", C.c_int32), ("rows", C.c_int32), ("experts", C.c_int32), ("k", C.c_int32),
+                ("groups", C.c_int32), ("top_groups", C.c_int32), ("group_best", C.c_int32), ("renorm", C.c_int32),
+                ("scale", C.c_float), ("ldl", C.c_int64)]
+
+
+class ExpertsDesc(C.Structure):
+    """dn_experts_desc"""
+    _fields_ = [("type", C.c_int32), ("grad_type", C.c_int32), ("act", C.c_int32), ("rows", C.c_int32), ("d", C.c_int32),
+                ("f", C.c_int32), ("experts", C.c_int32), ("k", C.c_int32), ("ldx", C.c_int64), ("ldr", C.c_int64),
+                ("ldy", C.c_int64), ("grad_scale", C.c_float)]
+
+
+class Span(C.Structure):
+    """dn_span"""
+    _fields_ = [("grad_dev", C.c_void_p), ("out_dev", C.c_void_p), ("count", C.c_int64), ("type", C.c_int32),
+                ("out_type", C.c_int32)]
 
 
 _lib = None
@@ -140,6 +164,16 @@ def lib():
         l.dn_norm_forward.argtypes = [vp] * 11
         l.dn_norm_backward.argtypes = [vp] * 17 + [sz, vp]
         l.dn_dropout.argtypes = [i32, vp, vp, i32, i32, i64, i64, f32, u64, u64, vp]
+        l.dn_route_workspace_bytes.argtypes = [i32, i32, i32]
+        l.dn_route_forward.argtypes = [vp] * 9 + [sz, vp]
+        l.dn_route_lists.argtypes = [vp, i32, i32, i32] + [vp] * 4 + [sz, vp]
+        l.dn_route_backward.argtypes = [vp] * 6
+        for f in (l.dn_experts_forward_workspace_bytes, l.dn_experts_backward_workspace_bytes):
+            f.argtypes = [vp]
+        l.dn_experts_forward.argtypes = [vp] * 13 + [sz, vp]
+        l.dn_experts_backward.argtypes = [vp] * 17 + [sz, vp]
+        l.dn_clip_workspace_bytes.argtypes = [vp, i32]
+        l.dn_clip.argtypes = [vp, i32, f32, vp, vp, sz, vp]
         for name in EXPORTS[2:]:
             if name.endswith("_workspace_bytes") or name.endswith("_static_limit") or name.endswith("_arena_bytes"):
                 getattr(l, name).restype = C.c_size_t
@@ -349,12 +383,17 @@ _TYPES = {}     # torch.dtype -> dn_type
 _torch = _raw_stream = None
 
 
-def _type_of(t, what: str) -> int:
+def _setup():
     global _torch, _raw_stream
     if _torch is None:
         import torch
         _torch, _raw_stream = torch, getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _TYPES.update({torch.float32: DN_F32, torch.float16: DN_F16, torch.bfloat16: DN_BF16})
+
+
+def _type_of(t, what: str) -> int:
+    if _torch is None:
+        _setup()
     kind = _TYPES.get(getattr(t, "dtype", None))
     if kind is None or not t.is_cuda:
         raise TypeError("%s must be a device tensor of float32, float16 or bfloat16" % what)
@@ -578,6 +617,146 @@ def dn_dropout(X, Y, drop: float, seed: int, offset: int = 0):
     y, ldy = _matrix(Y, X.dtype, dev, shape, "Y")
     with _on(dev):
         _check(lib().dn_dropout(kind, x, y, shape[0], shape[1], ldx, ldy, drop, seed, offset, _stream(dev)), "dn_dropout")
+
+
+# ---- a block of experts ------------------------------------------------------------------------------------------
+
+def _route_desc(L, k, score, groups, top_groups, group_best, renorm, scale):
+    kind = _type_of(L, "L")
+    rows, experts = _two(L, "L")
+    l, ldl = _matrix(L, L.dtype, L.get_device(), (rows, experts), "L")
+    return RouteDesc(kind, score, rows, experts, k, groups, top_groups, group_best, bool(renorm), scale, ldl), l, rows, experts
+
+
+def _choices(t, what: str):
+    """[rows][k] of a table of choices."""
+    if t.dim() != 2:
+        raise TypeError("%s must be a matrix" % what)
+    return _two(t, what)
+
+
+def dn_route_forward(L, bias, expert, weight, starts=None, order=None, place=None, score: int = DN_SCORE_SOFTMAX, groups: int = 1,
+                     top_groups: int = 1, group_best: int = 1, renorm: bool = True, scale: float = 1.0, workspace=None):
+    """Each row's k experts by the scores of its logits L, expert [rows][k] int32 (highest first, -1 for none), and their weights
+    [rows][k] float32; with starts [experts + 1], order and place [rows * k] (int32) the lists of pairs by expert too.  bias: float32
+    [experts] or None."""
+    l = lib()
+    rows, k = _choices(expert, "expert")
+    d, at_l, _, experts = _route_desc(L, k, score, groups, top_groups, group_best, renorm, scale)
+    i32, f32, dev = _torch.int32, _torch.float32, L.get_device()
+    b, e, w = _dense(bias, f32, dev, (experts,), "bias"), _dense(expert, i32, dev, (d.rows, k), "expert"), _dense(weight, f32, dev, (d.rows, k), "weight")
+    lists = (_dense(starts, i32, dev, (experts + 1,), "starts"), _dense(order, i32, dev, (rows * k,), "order"), _dense(place, i32, dev, (rows * k,), "place"))
+    with _on(dev):
+        need = l.dn_route_workspace_bytes(rows, experts, k) if starts is not None else 0
+        _keep, ws, n = _workspace(need, workspace, L)
+        _check(l.dn_route_forward(C.addressof(d), at_l, b, e, w, *lists, ws, n, _stream(dev)), "dn_route_forward")
+
+
+def dn_route_lists(expert, starts, order, place, workspace=None):
+    """The lists of a table of choices, expert [rows][k] int32 (numbers that are no expert's: none): starts [experts + 1], order and
+    place [rows * k]."""
+    l = lib()
+    _setup()
+    if not expert.is_cuda:
+        raise TypeError("expert must be a device tensor")
+    rows, k = _choices(expert, "expert")
+    i32, dev, experts = _torch.int32, expert.get_device(), starts.numel() - 1
+    p = (_dense(expert, i32, dev, (rows, k), "expert"), _dense(starts, i32, dev, (experts + 1,), "starts"),
+         _dense(order, i32, dev, (rows * k,), "order"), _dense(place, i32, dev, (rows * k,), "place"))
+    with _on(dev):
+        _keep, ws, n = _workspace(l.dn_route_workspace_bytes(rows, experts, k), workspace, expert)
+        _check(l.dn_route_lists(p[0], rows, experts, k, *p[1:], ws, n, _stream(dev)), "dn_route_lists")
+
+
+def dn_route_backward(L, expert, dweight, dL, score: int = DN_SCORE_SOFTMAX, renorm: bool = True, scale: float = 1.0):
+    """dL from the weights' gradient, for the choices in expert."""
+    l = lib()
+    rows, k = _choices(expert, "expert")
+    d, at_l, _, experts = _route_desc(L, k, score, 1, 1, 1, renorm, scale)
+    dev = L.get_device()
+    e, w = _dense(expert, _torch.int32, dev, (d.rows, k), "expert"), _dense(dweight, _torch.float32, dev, (d.rows, k), "dweight")
+    dl = _dense(dL, L.dtype, dev, (d.rows, experts), "dL")
+    with _on(dev):
+        _check(l.dn_route_backward(C.addressof(d), at_l, e, w, dl, _stream(dev)), "dn_route_backward")
+
+
+def _experts_desc(X, Wg, Wu, Wd, weight, starts, order, place, R, Y, Yname, act, grad_type, grad_scale):
+    kind = _type_of(X, "X")
+    rows, d = _two(X, "X")
+    if Wg.dim() != 3 or max(Wg.shape) >> 31:
+        raise TypeError("Wg must be [experts][f][d]")
+    experts, f, _ = Wg.shape
+    k = _choices(weight, "weight")[1]
+    dtype, dev, i32 = X.dtype, X.get_device(), _torch.int32
+    x, ldx = _matrix(X, dtype, dev, (rows, d), "X")
+    r, ldr = _matrix(R, dtype, dev, (rows, d), "R")
+    y, ldy = _matrix(Y, dtype, dev, (rows, d), Yname)
+    desc = ExpertsDesc(kind, kind if grad_type is None else grad_type, act, rows, d, f, experts, k, ldx, ldr, ldy, grad_scale)
+    w = (_dense(Wg, dtype, dev, (experts, f, d), "Wg"), _dense(Wu, dtype, dev, (experts, f, d), "Wu"), _dense(Wd, dtype, dev, (experts, d, f), "Wd"))
+    lists = (_dense(weight, _torch.float32, dev, (rows, k), "weight"), _dense(starts, i32, dev, (experts + 1,), "starts"),
+             _dense(order, i32, dev, (rows * k,), "order"), _dense(place, i32, dev, (rows * k,), "place"))
+    return desc, x, r, y, w, lists, (rows, d, f, experts, k), dtype, dev
+
+
+def dn_experts_forward(X, Wg, Wu, Wd, weight, starts, order, place, R, Y, GU=None, act: int = DN_ACT_SILU, workspace=None):
+    """Y_t = R_t + the sum over row t's choices of weight ((f(X Wg[e]^T) * (X Wu[e]^T)) Wd[e]^T), the choices by dn_route_forward's
+    weight and lists.  GU [rows * k][2 f] receives both net inputs by place.  R and GU may be None."""
+    l = lib()
+    desc, x, r, y, w, lists, (rows, d, f, experts, k), dtype, dev = _experts_desc(X, Wg, Wu, Wd, weight, starts, order, place, R, Y, "Y", act,
+                                                                                 None, 1.0)
+    gu = _dense(GU, dtype, dev, (rows * k, 2 * f), "GU")
+    with _on(dev):
+        at = C.addressof(desc)
+        _keep, ws, n = _workspace(l.dn_experts_forward_workspace_bytes(at), workspace, X)
+        _check(l.dn_experts_forward(at, x, *w, *lists, r, y, gu, ws, n, _stream(dev)), "dn_experts_forward")
+
+
+def dn_experts_backward(X, Wg, Wu, Wd, weight, starts, order, place, GU, dY, dX, dWg, dWu, dWd, dweight, act: int = DN_ACT_SILU,
+                        grad_scale: float = 1.0, workspace=None):
+    """The block's gradients; dX and dweight may be None, the matrices' are all of X's type or all float32."""
+    l = lib()
+    gt, gdtype = _grad_type(dWg, X)
+    desc, x, _, y, w, lists, (rows, d, f, experts, k), dtype, dev = _experts_desc(X, Wg, Wu, Wd, weight, starts, order, place, None, dY, "dY",
+                                                                                 act, gt, grad_scale)
+    gu, dx = _dense(GU, dtype, dev, (rows * k, 2 * f), "GU"), _dense(dX, dtype, dev, (rows, d), "dX")
+    dw = (_dense(dWg, gdtype, dev, (experts, f, d), "dWg"), _dense(dWu, gdtype, dev, (experts, f, d), "dWu"),
+          _dense(dWd, gdtype, dev, (experts, d, f), "dWd"))
+    dwt = _dense(dweight, _torch.float32, dev, (rows, k), "dweight")
+    with _on(dev):
+        at = C.addressof(desc)
+        _keep, ws, n = _workspace(l.dn_experts_backward_workspace_bytes(at), workspace, X)
+        _check(l.dn_experts_backward(at, x, *w, *lists, gu, y, dx, *dw, dwt, ws, n, _stream(dev)), "dn_experts_backward")
+
+
+def dn_clip(grads, max_norm: float, norm, outs=None, workspace=None):
+    """grads (tensors of any of the three types, each contiguous) times min(1, max_norm / n), n the norm of all of them together, which
+    norm [1] float32 receives.  outs: where the results go, tensor by tensor: the gradient itself, another tensor of its type or of
+    float32, or None (takes part in the norm only); outs None: into the gradients themselves."""
+    l = lib()
+    _type_of(norm, "norm")
+    dev = norm.get_device()
+    at_norm = _dense(norm, _torch.float32, dev, (1,), "norm")
+    outs = grads if outs is None else outs
+    if len(outs) != len(grads):
+        raise TypeError("outs must be as many as grads")
+    spans = (Span * max(len(grads), 1))()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        kind = _type_of(g, "a gradient")
+        if g.get_device() != dev or not g.is_contiguous():
+            raise TypeError("gradients must be contiguous tensors on device %d" % dev)
+        s = spans[i]
+        s.grad_dev, s.count, s.type, s.out_type = g.data_ptr(), g.numel(), kind, kind
+        if o is g:
+            s.out_dev = s.grad_dev
+        elif o is not None:
+            s.out_type = _type_of(o, "a result")
+            if o.get_device() != dev or not o.is_contiguous() or o.shape != g.shape:
+                raise TypeError("results must be contiguous tensors of their gradients' shapes on device %d" % dev)
+            s.out_dev = o.data_ptr()
+    with _on(dev):
+        at = C.addressof(spans)
+        _keep, ws, n = _workspace(l.dn_clip_workspace_bytes(at, len(grads)), workspace, norm)
+        _check(l.dn_clip(at, len(grads), max_norm, at_norm, ws, n, _stream(dev)), "dn_clip")
 
 
 class Net:

@@ -1,0 +1,149 @@
+"""Host-side checks of the calls of a block of experts that need no GPU: workspace queries and refusals, all before anything is launched."""
+import ctypes as C
+import math
+
+import pytest
+
+from paper_2001_04206_amd import dn
+
+A = 0x10000           # an aligned address that no call below gets to
+BAD = C.c_size_t(-1).value
+ARG, SHAPE, UNSUPPORTED = dn.DN_ERR_INVALID_ARG, dn.DN_ERR_SHAPE, dn.DN_ERR_UNSUPPORTED
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return dn.lib()
+
+
+def route(**kw):
+    d = dict(type=dn.DN_BF16, score=dn.DN_SCORE_SIGMOID, rows=1000, experts=64, k=8, groups=8, top_groups=4, group_best=2, renorm=1, scale=2.5, ldl=0)
+    d.update(kw)
+    return dn.RouteDesc(**d)
+
+
+def experts(**kw):
+    d = dict(type=dn.DN_BF16, grad_type=dn.DN_F32, act=dn.DN_ACT_SILU, rows=100, d=64, f=48, experts=8, k=2, ldx=0, ldr=0, ldy=0, grad_scale=1.0)
+    d.update(kw)
+    return dn.ExpertsDesc(**d)
+
+
+def swap(args, k, v):
+    return [v if i == k else w for i, w in enumerate(args)]
+
+
+def test_route_refuses(lib):
+    at = C.addressof
+    ok = route()
+    need = lib.dn_route_workspace_bytes(1000, 64, 8)
+    assert 0 < need < BAD and need % 256 == 0
+    assert lib.dn_route_workspace_bytes(128, 1024, 8) == 0
+    fwd, back = [A] * 7, [A] * 4
+    assert lib.dn_route_forward(None, *fwd, A, need, None) == ARG and lib.dn_route_backward(None, *back, None) == ARG
+    for kw, status in [({"type": 3}, ARG), ({"score": 2}, ARG), ({"score": -1}, ARG), ({"group_best": 0}, ARG), ({"group_best": 3}, ARG),
+                       ({"renorm": 2}, ARG), ({"scale": math.nan}, ARG), ({"scale": math.inf}, ARG), ({"rows": 0}, SHAPE), ({"rows": 1 << 26}, SHAPE),
+                       ({"experts": 0}, SHAPE), ({"experts": 1032}, SHAPE), ({"k": 0}, SHAPE), ({"k": 33}, SHAPE), ({"groups": 0}, SHAPE),
+                       ({"groups": 7}, SHAPE), ({"groups": 128, "experts": 128}, SHAPE), ({"top_groups": 0}, SHAPE), ({"top_groups": 9}, SHAPE),
+                       ({"top_groups": 1, "k": 9}, SHAPE), ({"groups": 64, "top_groups": 8}, SHAPE), ({"ldl": 63}, SHAPE), ({"ldl": -64}, SHAPE),
+                       ({"rows": (1 << 26) - 1, "k": 32}, SHAPE)]:
+        d = route(**kw)
+        assert lib.dn_route_forward(at(d), *fwd, A, 1 << 40, None) == status, kw
+        assert lib.dn_route_backward(at(d), *back, None) == status, kw
+    for k in (0, 2, 3, 4, 5, 6):
+        assert lib.dn_route_forward(at(ok), *swap(fwd, k, None), A, need, None) == ARG, k
+    for k in range(7):
+        assert lib.dn_route_forward(at(ok), *swap(fwd, k, A + 1), A, need, None) == ARG, k
+    for k in range(4):
+        assert lib.dn_route_backward(at(ok), *swap(back, k, None), None) == ARG and lib.dn_route_backward(at(ok), *swap(back, k, A + 1), None) == ARG
+    assert lib.dn_route_forward(at(ok), *fwd, A, need - 1, None) == SHAPE
+    assert lib.dn_route_forward(at(ok), *fwd, None, need, None) == ARG
+    assert lib.dn_route_forward(at(ok), *fwd, A + 8, need, None) == ARG
+
+
+def test_lists_refuse(lib):
+    for rows, n, k in ((0, 4, 2), (5, 0, 2), (5, 4, 0), (5, 1025, 2), (5, 4, 33), (1 << 26, 4, 1), (1 << 25, 4, 32), (-1, 4, 2), (5, -4, 2)):
+        assert lib.dn_route_workspace_bytes(rows, n, k) == BAD
+        assert lib.dn_route_lists(A, rows, n, k, A, A, A, A, 1 << 40, None) == SHAPE, (rows, n, k)
+    need = lib.dn_route_workspace_bytes(5000, 64, 8)
+    for i in range(4):
+        for v in (None, A + 2):
+            p = swap([A] * 4, i, v)
+            assert lib.dn_route_lists(p[0], 5000, 64, 8, *p[1:], A, need, None) == ARG
+    assert lib.dn_route_lists(A, 5000, 64, 8, A, A, A, A, need - 1, None) == SHAPE
+    assert lib.dn_route_lists(A, 5000, 64, 8, A, A, A, None, need, None) == ARG
+
+
+def test_experts_refuse(lib):
+    at = C.addressof
+    ok = experts()
+    need = [lib.dn_experts_forward_workspace_bytes(at(ok)), lib.dn_experts_backward_workspace_bytes(at(ok))]
+    assert all(0 < n < BAD and n % 256 == 0 for n in need) and need[0] >= 200 * (48 + 64) * 2 and need[1] >= 200 * (3 * 48 + 3 * 64) * 2
+    fwd, back = [A] * 11, [A] * 15
+    assert lib.dn_experts_forward_workspace_bytes(None) == BAD and lib.dn_experts_forward(None, *fwd, A, 1 << 40, None) == ARG
+    for kw, status in [({"type": 3}, ARG), ({"type": dn.DN_F16, "grad_type": dn.DN_BF16}, ARG), ({"act": -1}, ARG), ({"act": 7}, ARG),
+                       ({"act": dn.DN_ACT_SOFTMAX}, UNSUPPORTED), ({"rows": 0}, SHAPE), ({"d": 0}, SHAPE), ({"f": -1}, SHAPE), ({"f": 1 << 22}, SHAPE),
+                       ({"experts": 0}, SHAPE), ({"experts": 1025}, SHAPE), ({"k": 0}, SHAPE), ({"k": 33}, SHAPE), ({"ldx": 63}, SHAPE),
+                       ({"ldr": 1}, SHAPE), ({"ldy": -64}, SHAPE), ({"rows": 1 << 24, "k": 1, "d": 8, "f": 8}, SHAPE), ({"rows": 1 << 26, "k": 1}, SHAPE),
+                       ({"rows": 1 << 23, "k": 1, "d": 128}, SHAPE), ({"rows": 1 << 20, "ldx": 1024, "k": 1}, SHAPE), ({"rows": 1 << 20, "ldy": 1024, "k": 1}, SHAPE),
+                       ({"experts": 1024, "f": 1 << 21, "d": 64}, SHAPE), ({"grad_scale": math.inf}, ARG)]:
+        d = experts(**kw)
+        assert lib.dn_experts_forward_workspace_bytes(at(d)) == BAD and lib.dn_experts_backward_workspace_bytes(at(d)) == BAD, kw
+        assert lib.dn_experts_forward(at(d), *fwd, A, 1 << 50, None) == status, kw
+        assert lib.dn_experts_backward(at(d), *back, A, 1 << 50, None) == status, kw
+    for k in (0, 1, 2, 3, 4, 5, 6, 7, 9):
+        assert lib.dn_experts_forward(at(ok), *swap(fwd, k, None), A, need[0], None) == ARG, k
+    for k in range(11):
+        assert lib.dn_experts_forward(at(ok), *swap(fwd, k, A + 1), A, need[0], None) == ARG, k
+    for k in (0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 11, 12, 13):
+        assert lib.dn_experts_backward(at(ok), *swap(back, k, None), A, need[1], None) == ARG, k
+    for k in range(15):
+        assert lib.dn_experts_backward(at(ok), *swap(back, k, A + 1), A, need[1], None) == ARG, k
+    # matrices of whole 16-byte rows begin at 16 bytes; others may begin anywhere
+    for k in (1, 2, 3):
+        assert lib.dn_experts_forward(at(ok), *swap(fwd, k, A + 2), A, need[0], None) == ARG
+        assert lib.dn_experts_backward(at(ok), *swap(back, k, A + 2), A, need[1], None) == ARG
+    assert lib.dn_experts_forward(at(ok), *fwd, A, need[0] - 1, None) == SHAPE and lib.dn_experts_backward(at(ok), *back, A, need[1] - 1, None) == SHAPE
+    assert lib.dn_experts_forward(at(ok), *fwd, None, need[0], None) == ARG and lib.dn_experts_backward(at(ok), *back, A + 128, need[1], None) == ARG
+
+
+def spans(*rows):
+    s = (dn.Span * max(len(rows), 1))()
+    for i, r in enumerate(rows):
+        s[i] = dn.Span(*r)
+    return s
+
+
+def test_clip_refuses(lib):
+    f32, f16, bf16 = dn.DN_F32, dn.DN_F16, dn.DN_BF16
+    at = C.addressof
+    ok = (A, A, 100, f32, f32)
+    good = spans(ok, (A + 4096, 2 * A, 50, bf16, f32), (None, None, 0, f16, f16))
+    need = lib.dn_clip_workspace_bytes(at(good), 3)
+    assert 0 < need < BAD and need % 256 == 0 and 0 < lib.dn_clip_workspace_bytes(None, 0) < BAD
+    for bound in (-1.0, math.nan, -math.inf):
+        assert lib.dn_clip(at(good), 3, bound, A, A, need, None) == ARG
+    assert lib.dn_clip(at(good), 3, 1.0, None, A, need, None) == ARG and lib.dn_clip(at(good), 3, 1.0, A + 2, A, need, None) == ARG
+    assert lib.dn_clip(at(good), 3, 1.0, A, A, need - 1, None) == SHAPE and lib.dn_clip(at(good), 3, 1.0, A, None, need, None) == ARG
+    assert lib.dn_clip(at(good), -1, 1.0, A, A, need, None) == ARG and lib.dn_clip(None, 1, 1.0, A, A, need, None) == ARG
+    for row, status in [((A, A, 100, 3, 3), ARG), ((A, A, 100, f32, f16), ARG), ((A, A, 100, f16, bf16), ARG), ((A, A, -1, f32, f32), SHAPE),
+                        ((A, A, 1 << 44, f32, f32), SHAPE), ((None, A, 1, f32, f32), ARG), ((A + 2, A + 2, 1, f32, f32), ARG), ((A, A + 1, 1, f16, f16), ARG),
+                        ((A + 1, None, 1, bf16, bf16), ARG), ((A, 2 * A + 2, 1, f16, f32), ARG)]:
+        s = spans(ok[:1] + (None,) + ok[2:], row)
+        assert lib.dn_clip_workspace_bytes(at(s), 2) == BAD, row
+        assert lib.dn_clip(at(s), 2, 1.0, A, A, 1 << 30, None) == status, row
+    # results over other gradients or results; over their own gradient in another type, or a little further on
+    for rows in ([ok, ok], [ok, (A + 396, A + 396, 1, f32, f32)], [ok, (A + 4096, A + 200, 10, f32, f32)], [(A, 2 * A, 100, f32, f32), (A + 4096, 2 * A + 4, 9, f32, f32)],
+                 [(A, A, 100, f16, f32)], [(A, A + 4, 100, f32, f32)], [(A, 2 * A, 9, f32, f32), (2 * A + 16, None, 9, f32, f32)]):
+        s = spans(*rows)
+        assert lib.dn_clip(at(s), len(rows), 1.0, A, A, 1 << 30, None) == ARG, rows
+
+
+def test_workspaces_follow_the_spans(lib):
+    """One number for each workgroup of each launch: at most 80 tensors and 1024 workgroups a launch."""
+    at = C.addressof
+    for n, count in ((1, 1), (80, 1), (81, 1), (500, 300), (2, 1 << 33), (3, 1 << 43)):
+        s = (dn.Span * n)()
+        for i in range(n):
+            s[i] = dn.Span(A + i * 16 * count, None, count, dn.DN_F32, dn.DN_F32)
+        need = lib.dn_clip_workspace_bytes(at(s), n)
+        assert need % 256 == 0 and 8 <= need <= (-(-n // 80) + n) * 1024 * 8
