@@ -11,34 +11,19 @@ constexpr int64_t kMostRows = (int64_t)1 << 26, kMostPairs = (int64_t)1 << 24, k
 
 // ---- rows ------------------------------------------------------------------------------------------------------------
 
-// Rows of up to two matrices of the same width into the experts' order and 16-byte rows, zeros following; and the pairs' weights.
-struct SortArgs {
-    const void *x[2];
-    void *y[2];
-    int64_t ldx[2];
-    const float *weight;
-    float *sorted;
-    Group group;
-    int32_t cols;
-};
-template <class T>
-__global__ __launch_bounds__(256) void sort_rows_kernel(const SortArgs a)
+// The pairs' weights in the experts' order.
+__global__ __launch_bounds__(256) void sort_weights_kernel(const Group g, const float *weight, float *sorted)
 {
-    const uint32_t eights = ((uint32_t)a.cols + 7) / 8;
-    const uint64_t first = (uint64_t)blockIdx.x * 256;
-    const uint32_t row0 = (uint32_t)(first / eights), c0 = (uint32_t)(first % eights) + threadIdx.x, more = c0 / eights;
-    const int64_t p = (int64_t)row0 + more;
-    const uint32_t c = c0 - more * eights;
-    if (p >= min(a.group.starts[a.group.experts], a.group.pairs)) return;
-    const int t = token_of(a.group, (int)p), k = blockIdx.y, left = a.cols - (int)c * 8;
-    const auto v = get8<T>(a.x[k], t * a.ldx[k] + c * 8, left);
-    *reinterpret_cast<typename Eight<T>::type *>(static_cast<T *>(a.y[k]) + (p * eights + c) * 8) = v;
-    if (k == 0 && c == 0) a.sorted[p] = a.weight[min((uint32_t)max(a.group.order[p], 0), (uint32_t)a.group.pairs - 1)];
+    const int p = blockIdx.x * 256 + threadIdx.x;
+    if (p < min(g.starts[g.experts], g.pairs)) sorted[p] = weight[min((uint32_t)max(g.order[p], 0), (uint32_t)g.pairs - 1)];
 }
 
-// Y_t = R_t + the sum over its pairs of (weight) z, in the order of the choices, in fp32.  A thread: eight columns of a row.
+// Y_t = R_t + the sum over its pairs of (weight) z, in the order of the choices.  A thread: eight columns of a row.  z is fp32, so that what is
+// added is rounded once, as a sum: in 16 bits each z would be rounded by itself, and results without a residual be off by 0.0029 where
+// they are by 0.0024 (bf16; of which H has a rounding, and the result).
 struct JoinArgs {
-    const void *z, *r;
+    const float *z;
+    const void *r;
     void *y;
     int64_t ldz, ldr, ldy;
     const float *weight;       // NULL: ones
@@ -57,19 +42,18 @@ __global__ __launch_bounds__(256) void join_pairs_kernel(const JoinArgs a)
     float v[8] = {};
     if (a.r) load8<T>(v, a.r, t * a.ldr + n, left);
     for (int j0 = 0; j0 < a.k; j0 += 4) {
-        typename Eight<T>::type z[4];
-        float w[4];
+        float z[4][8], w[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int j = min(j0 + q, a.k - 1), p = a.place[t * a.k + j];
             const bool has = j0 + q < a.k && (uint32_t)p < (uint32_t)a.pairs;
             w[q] = !has ? 0.f : a.weight ? a.weight[t * a.k + j] : 1.f;
-            z[q] = has ? get8<T>(a.z, p * a.ldz + n, left) : typename Eight<T>::type{};
+            load8<float>(z[q], a.z, has ? p * a.ldz + n : 0, has ? left : 0);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = fmaf(w[q], (float)z[q][j], v[j]);
+            for (int j = 0; j < 8; ++j) v[j] = fmaf(w[q], z[q][j], v[j]);
     }
     store8<T>(a.y, t * a.ldy + n, v, left);
 }
@@ -99,22 +83,11 @@ hipError_t launch_join(int type, const JoinArgs &a, hipStream_t s)
 {
     return type == DN_F32 ? join_as<float>(a, s) : type == DN_F16 ? join_as<f16>(a, s) : join_as<bf16>(a, s);
 }
-template <class T>
-hipError_t sort_as(const SortArgs &a, hipStream_t s)
+hipError_t launch_experts(int type, Product p, Epilogue e, ProductKernel kernel, const ProductArgs &a, int64_t tiles, hipStream_t s, int gathered = 0)
 {
-    const uint64_t threads = (uint64_t)a.group.pairs * (((uint32_t)a.cols + 7) / 8);
-    launch_kernel(sort_rows_kernel<T>, dim3((unsigned)((threads + 255) / 256), 2), dim3(256), 0, s, a);
-    return hipGetLastError();
-}
-hipError_t launch_sort(int type, const SortArgs &a, hipStream_t s)
-{
-    return type == DN_F32 ? sort_as<float>(a, s) : type == DN_F16 ? sort_as<f16>(a, s) : sort_as<bf16>(a, s);
-}
-hipError_t launch_experts(int type, Product p, Epilogue e, ProductKernel kernel, const ProductArgs &a, int64_t tiles, hipStream_t s)
-{
-    return type == DN_F32   ? launch_experts_f32(p, e, kernel, a, tiles, s)
-           : type == DN_F16 ? launch_experts_f16(p, e, kernel, a, tiles, s)
-                            : launch_experts_bf16(p, e, kernel, a, tiles, s);
+    return type == DN_F32   ? launch_experts_f32(p, e, kernel, gathered, a, tiles, s)
+           : type == DN_F16 ? launch_experts_f16(p, e, kernel, gathered, a, tiles, s)
+                            : launch_experts_bf16(p, e, kernel, gathered, a, tiles, s);
 }
 
 // ---- plans -----------------------------------------------------------------------------------------------------------
@@ -203,7 +176,7 @@ dn_status block_of(const dn_experts_desc *d, Block &b)
     b.pack_w = d->d * e % 16 || d->f * e % 16;
     const size_t wgu = b.pack_w ? packed_bytes(d->type, n * d->f, d->d) : 0, wd = b.pack_w ? packed_bytes(d->type, n * d->d, d->f) : 0;
     b.h = up256((size_t)(b.pairs * b.ldh * e));
-    b.z = up256((size_t)(b.pairs * b.ldz * e));
+    b.z = up256((size_t)(b.pairs * b.ldz) * sizeof(float));
     b.x = packed_bytes(d->type, d->rows, d->d);
     b.w1 = wgu;
     b.w2 = wd;
@@ -212,7 +185,7 @@ dn_status block_of(const dn_experts_desc *d, Block &b)
     b.sorted = up256((size_t)b.pairs * sizeof(float));
     b.dots = up256((size_t)b.pairs * b.parts * sizeof(float));
     b.dgu = up256((size_t)(b.pairs * 2 * b.ldh * e));
-    b.bwd_bytes = 2 * b.z + b.sorted + b.dots + b.h + b.dgu + b.z + 2 * wgu + wd;
+    b.bwd_bytes = b.sorted + b.dots + b.h + b.dgu + b.z + 2 * b.x + 2 * wgu + wd;
     return DN_OK;
 }
 
@@ -294,8 +267,9 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
     c.group.b_stride = c.ldb * d->d;
     c.f.y = z;
     c.f.ldy = b.ldz;
+    c.f.f32_out = 1;
     if (launch_experts(d->type, P_FWD, E_STORE, b.down, c, most_tiles(b.pairs, d->experts, rows_of_tile(b.down)), stream) != hipSuccess) return DN_ERR_DEVICE;
-    return device(launch_join(d->type, {z, R_dev, Y_dev, b.ldz, b.d.ldr, b.d.ldy, weight_dev, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream));
+    return device(launch_join(d->type, {reinterpret_cast<const float *>(z), R_dev, Y_dev, b.ldz, b.d.ldr, b.d.ldy, weight_dev, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream));
 }
 
 dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
@@ -316,21 +290,23 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
     if ((s = workspace(b.bwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const int64_t e = size_of(d->type), n = d->experts, f = d->f;
-    char *xs = static_cast<char *>(workspace_dev), *dys = xs + b.z, *sorted = dys + b.z, *dots = sorted + b.sorted, *H = dots + b.dots;
+    char *sorted = static_cast<char *>(workspace_dev), *dots = sorted + b.sorted, *H = dots + b.dots;
     char *dG = H + b.h, *dU = dG + b.ldh * e, *dx = dG + b.dgu;
     const Group g{starts_dev, order_dev, d->experts, d->k, (int32_t)b.pairs, d->rows, 0, 0};
     Packer pack{d->type, dx + b.z};
+    const Packer::Rows X = pack.take(X_dev, b.d.ldx, d->rows, d->d), dY = pack.take(dY_dev, b.d.ldy, d->rows, d->d);
+    if (b.pack_w && pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;   // (four matrices a launch)
+    if (b.pack_w) pack.a = {};
     const Packer::Rows Wd = pack.take(Wd_dev, f, n * d->d, f, b.pack_w);
     const Packer::Rows Wg = dX_dev ? pack.take(Wg_dev, d->d, n * f, d->d, b.pack_w) : Packer::Rows{};
     const Packer::Rows Wu = dX_dev ? pack.take(Wu_dev, d->d, n * f, d->d, b.pack_w) : Packer::Rows{};
     if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
-    if (launch_sort(d->type, {{X_dev, dY_dev}, {xs, dys}, {b.d.ldx, b.d.ldy}, weight_dev, reinterpret_cast<float *>(sorted), g, d->d}, stream) != hipSuccess)
-        return DN_ERR_DEVICE;
+    launch_kernel(sort_weights_kernel, dim3((unsigned)((b.pairs + 255) / 256)), dim3(256), 0, stream, g, weight_dev, reinterpret_cast<float *>(sorted));
+    if (hipGetLastError() != hipSuccess) return DN_ERR_DEVICE;
     auto tiles = [&](ProductKernel k) { return most_tiles(b.pairs, d->experts, rows_of_tile(k)); };
-    const Packer::Rows Xs{xs, b.ldz * e, (int32_t)b.ldz}, dYs{dys, b.ldz * e, (int32_t)b.ldz};
     {   // dh, and from it dG, dU, w H and the weights' derivatives
         ProductArgs a = product(g, 0, d->f, d->d, 1, Wd.ld * d->d);
-        operand_a(a, dYs);
+        operand_a(a, dY);
         operand_b(a, Wd);
         a.f.y = dG;
         a.f.ldy = 2 * b.ldh;
@@ -361,8 +337,9 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
         a.b[1] = Wu.p;
         a.f.y = dx;
         a.f.ldy = b.ldz;
+        a.f.f32_out = 1;
         if (launch_experts(d->type, P_DELTA, E_STORE, b.dx, a, tiles(b.dx), stream) != hipSuccess) return DN_ERR_DEVICE;
-        if (launch_join(d->type, {dx, nullptr, dX_dev, b.ldz, 0, d->d, nullptr, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream) != hipSuccess)
+        if (launch_join(d->type, {reinterpret_cast<const float *>(dx), nullptr, dX_dev, b.ldz, 0, d->d, nullptr, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream) != hipSuccess)
             return DN_ERR_DEVICE;
     }
     const bool f32_out = d->grad_type == DN_F32;
@@ -370,7 +347,7 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
     {   // dWg and dWu: the columns of dG (and of the zeros up to ldh), then those of dU
         ProductArgs a = product(g, (int)(2 * b.ldh), d->d, 0, 1, 0);
         operand_a(a, {dG, 2 * b.ldh * e, (int32_t)(2 * b.ldh)});
-        operand_b(a, Xs);
+        operand_b(a, X);
         a.group.c_stride = matrix;
         a.f.y = dWg_dev;
         a.f.ldy = d->d;
@@ -380,10 +357,10 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
         a.f.m_valid = d->f;
         a.f.f32_out = f32_out;
         a.f.alpha = d->grad_scale;
-        if (launch_experts(d->type, P_GRAD, E_STORE, b.dwgu, a, 0, stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_experts(d->type, P_GRAD, E_STORE, b.dwgu, a, 0, stream, 1) != hipSuccess) return DN_ERR_DEVICE;
     }
     ProductArgs a = product(g, d->d, d->f, 0, 1, 0);
-    operand_a(a, dYs);
+    operand_a(a, dY);
     operand_b(a, {H, b.ldh * e, (int32_t)b.ldh});
     a.group.c_stride = matrix;
     a.f.y = dWd_dev;

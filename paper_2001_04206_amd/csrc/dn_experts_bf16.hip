@@ -3,9 +3,9 @@
 
 namespace dn {
 
-hipError_t launch_experts_bf16(Product p, Epilogue e, ProductKernel kernel, ProductArgs a, int64_t tiles, hipStream_t s)
+hipError_t launch_experts_bf16(Product p, Epilogue e, ProductKernel kernel, int gathered, ProductArgs a, int64_t tiles, hipStream_t s)
 {
-    return launch_experts<bf16>(p, e, kernel, a, tiles, s);
+    return launch_experts<bf16>(p, e, kernel, gathered, a, tiles, s);
 }
 
 }  // namespace dn

@@ -14,7 +14,7 @@ __global__ __launch_bounds__(WAVES * 64) void experts_few_kernel(const ProductAr
     __shared__ v4f part[WAVES][PLANES][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, h = lane >> 4;
     const uint32_t columns = ((uint32_t)a.N + 15) / 16;
-    const GroupTile tile = tile_in_group(a.group, (int)(blockIdx.x / columns), 16, lane);
+    const GroupTile tile = tile_in_group(a.group, tiles_of(a.group, 0, 16, lane), (int)(blockIdx.x / columns), 16, lane);
     if (tile.first >= tile.end) return;
     const int n0 = (int)(blockIdx.x % columns) * 16, row = min(tile.first + i, tile.end - 1);
     const int64_t from = GROUP == G_TOKENS ? token_of(a.group, row) : row;

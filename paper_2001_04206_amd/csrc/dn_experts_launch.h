@@ -12,8 +12,9 @@ hipError_t expert_tiles(ProductArgs &a, int64_t tiles, hipStream_t s)
 {
     const int cols = EPI == E_GATED ? S::BN / 2 : S::BN;
     a.tiles_n = (a.N + cols - 1) / cols;
-    a.tiles_m = GROUP == G_TERMS ? (a.M + S::BM - 1) / S::BM : (int32_t)tiles;
-    launch_kernel(product_kernel<T, P, EPI, S, false, GROUP>, dim3((unsigned)a.tiles_m * (unsigned)a.tiles_n, GROUP == G_TERMS ? (unsigned)a.group.experts : 1u),
+    constexpr bool TERMS = GROUP == G_TERMS_A || GROUP == G_TERMS_B;
+    a.tiles_m = TERMS ? (a.M + S::BM - 1) / S::BM : (int32_t)tiles;
+    launch_kernel(product_kernel<T, P, EPI, S, false, GROUP>, dim3((unsigned)a.tiles_m * (unsigned)a.tiles_n, TERMS ? (unsigned)a.group.experts : 1u),
                   dim3(S::NW * 64), 0, s, a);
     return hipGetLastError();
 }
@@ -49,13 +50,14 @@ hipError_t expert_run(ProductKernel kernel, ProductArgs &a, int64_t tiles, hipSt
 }  // namespace
 
 template <class T>
-hipError_t launch_experts(Product p, Epilogue e, ProductKernel kernel, ProductArgs &a, int64_t tiles, hipStream_t s)
+hipError_t launch_experts(Product p, Epilogue e, ProductKernel kernel, int gathered, ProductArgs &a, int64_t tiles, hipStream_t s)
 {
     if (p == P_FWD && e == E_GATED) return expert_run<T, P_FWD, E_GATED, G_TOKENS>(kernel, a, tiles, s);
     if (p == P_FWD && e == E_STORE) return expert_run<T, P_FWD, E_STORE, G_ROWS>(kernel, a, tiles, s);
-    if (p == P_DELTA && e == E_DEXPERT) return expert_run<T, P_DELTA, E_DEXPERT, G_ROWS>(kernel, a, tiles, s);
+    if (p == P_DELTA && e == E_DEXPERT) return expert_run<T, P_DELTA, E_DEXPERT, G_TOKENS>(kernel, a, tiles, s);
     if (p == P_DELTA && e == E_STORE) return expert_run<T, P_DELTA, E_STORE, G_ROWS>(kernel, a, tiles, s);
-    if (p == P_GRAD && e == E_STORE) return expert_run<T, P_GRAD, E_STORE, G_TERMS>(kernel, a, tiles, s);
+    if (p == P_GRAD && e == E_STORE)
+        return gathered == 0 ? expert_run<T, P_GRAD, E_STORE, G_TERMS_A>(kernel, a, tiles, s) : expert_run<T, P_GRAD, E_STORE, G_TERMS_B>(kernel, a, tiles, s);
     return hipErrorInvalidValue;
 }
 

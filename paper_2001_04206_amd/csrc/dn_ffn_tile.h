@@ -212,10 +212,10 @@ __device__ __forceinline__ void finish_sum(const Finish &e, int m, float v)
 // Each spreads what the lanes of one read touch over all banks; the last one's reads have their blocks at constant
 // distances of two addresses, where an exclusive-or of three bits would take an address register for each of eight blocks.
 // PAIR (KC): rows 0..15, 32..47, .. are of the first matrix, the rows between them of the second.
-// GATHER (KC): row r of the tile is any row of the matrix, which lies within 2^31 bytes.
+// GATHER: KC: row r of the tile, MC: term k of the product is any row of the matrix, which lies within 2^31 bytes.
 template <class T, int R, int NW, bool MC, bool PAIR, bool GATHER = false>
 struct Operand {
-    static_assert(!GATHER || (!MC && !PAIR), "rows are gathered along k");
+    static_assert(!GATHER || !PAIR, "one matrix");
     static constexpr bool MC_ = MC;
     static constexpr int Q = R / 8 / NW;             // pieces of a wave
     static constexpr int BK = 128 / (int)sizeof(T);  // k of a stage
@@ -224,7 +224,7 @@ struct Operand {
     static constexpr int PIECE = PAD ? 1056 : 1024, STAGE = R / 8 * PIECE;
     static constexpr int READS = MC ? (sizeof(T) == 2 ? 2 : 4) : 1;   // LDS instructions of a fragment
     static_assert(!MC || RB >= 256, "the exclusive-or of MC needs rows of 256 bytes");
-    static constexpr bool HOP = !GATHER && (!MC || sizeof(T) == 2);   // the lane's chunks lie one distance apart
+    static constexpr bool HOP = MC ? sizeof(T) == 2 : !GATHER;   // the lane's chunks lie one distance apart
     uint32_t off[HOP ? 1 : Q], hop;   // byte offsets of the lane's chunks in the first stage of a segment
     uint32_t kbyte;    // KC: its byte within the stage's k
     const char *base, *next;   // first row of the tile, in this segment and the second one
@@ -248,7 +248,7 @@ struct Operand {
                 const int byte = (wave + q * NW) * 1024 + lane * 16, k = byte / RB;
                 int x = byte % RB;
                 x ^= PAD ? (k & 1) << 6 : sizeof(T) == 2 ? ((k & 3) + 4 * ((k >> 3) & 1)) << 5 : ((k >> 2) & 3) << 6;
-                off[q] = (uint32_t)(k * ld) + (uint32_t)x;
+                off[q] = (GATHER ? 0 : (uint32_t)(k * ld)) + (uint32_t)x;
             }
             static_assert(!MC || !HOP || NW * 1024 / RB % 16 == 0, "the exclusive-or repeats after sixteen k");
             hop = (uint32_t)(NW * 1024 / RB * ld);
@@ -262,7 +262,7 @@ struct Operand {
         }
     }
 
-    // GATHER: `at` gives the row of the matrix of a row of the tile, of which `total` exist
+    // GATHER, KC: `at` gives the row of the matrix, of `total`, of a row of the tile
     template <class F>
     __device__ __forceinline__ void init_rows(const void *p, int64_t ld_, F at, int total, int wave, int lane)
     {
@@ -283,15 +283,25 @@ struct Operand {
         const char *from;
         int bytes;
         uint32_t first;   // offset of the lane's first chunk, past every resource if it is not to be read
+        uint32_t row[MC && GATHER ? Q : 1];   // bytes before the row of each chunk
     };
+    // GATHER, MC: the matrix has `total` rows; `in_lds` holds what lies before each term's row in bytes (2^31 for none)
+    typedef const __attribute__((address_space(3))) uint32_t *Rows;
+    __device__ __forceinline__ Aim aim_rows(bool valid, int step, Rows in_lds, int total, int wave, int lane) const
+    {
+        Aim a{base, valid ? (int)((int64_t)(total - 1) * ld + rows * (int)sizeof(T)) : 0, 0, {}};
+#pragma unroll
+        for (int q = 0; q < Q; ++q) a.row[MC && GATHER ? q : 0] = in_lds[step * BK + ((wave + q * NW) * 1024 + lane * 16) / RB];
+        return a;
+    }
     __device__ __forceinline__ Aim aim(bool valid, bool second, int step, int K) const
     {
         const int k0 = step * BK, kleft = K - k0;
         const char *b = (second ? next : base) + (MC ? (int64_t)k0 * ld : (int64_t)k0 * (int)sizeof(T));
         const int64_t bytes = MC ? (int64_t)(min(kleft, BK) - 1) * ld + rows * (int)sizeof(T) : (int64_t)(rows - 1) * ld + kleft * (int)sizeof(T);
         const bool in = valid && (MC || (int)kbyte < kleft * (int)sizeof(T));
-        if (GATHER) return {b, valid ? (int)bytes : 0, in ? 0 : 0x80000000u};
-        return {b, valid ? (int)bytes : 0, in ? off[0] : 0x80000000u};
+        if (GATHER) return {b, valid ? (int)bytes : 0, in ? 0 : 0x80000000u, {}};
+        return {b, valid ? (int)bytes : 0, in ? off[0] : 0x80000000u, {}};
     }
     __device__ __forceinline__ void fetch(lds_char *lds, const Aim &at, int wave) const
     {
@@ -299,7 +309,11 @@ struct Operand {
 #pragma unroll
         for (int q = 0; q < Q; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * PIECE), 16,
-                                                     (int)(HOP ? at.first + q * hop : GATHER ? at.first + off[q] : offset(q)), 0, 0, 0);
+                                                     (int)(GATHER && MC ? at.row[MC && GATHER ? q : 0] + off[HOP ? 0 : q]
+                                                           : HOP    ? at.first + q * hop
+                                                           : GATHER ? at.first + off[q]
+                                                                    : offset(q)),
+                                                     0, 0, 0);
     }
 
     // Fragments: sixteen rows from 16 block on, half kk (64 bytes of k) of the stage.  `at` from start(), block a constant
@@ -421,74 +435,80 @@ typedef Shape<2, 2, 2, 4, 2> Tiny;     // 64 x 128, 4 waves, three
 
 // The experts' products: one kernel's tiles are of all of them.  Rows 0 .. P of the result are pairs of a row and an expert, by expert;
 // expert e has those from starts[e] on.  G_ROWS: row m of A is row m of the matrix.  G_TOKENS: it is the pair's row, order[m] div k.
-// G_TERMS (P_GRAD): an expert's rows are its terms, every expert has a result of its own.
-enum Grouping : int { G_NONE, G_ROWS, G_TOKENS, G_TERMS };
+// G_TERMS_A, G_TERMS_B (P_GRAD): an expert's rows are its terms, and it has a result of its own; the operand that is named has the
+// pair's row where the other has its place.
+enum Grouping : int { G_NONE, G_ROWS, G_TOKENS, G_TERMS_A, G_TERMS_B };
+// terms whose rows a workgroup keeps in LDS at a time: what the stages leave room for
+template <class T> constexpr int terms_of() { return sizeof(T) == 4 ? 960 : 1920; }
 
 // Expert and first row of tile t of BM rows each, of `tiles` in all; every lane of the wave takes part.  A few loads that the L2 has: 64
 // experts at a time, a lane each.
 struct GroupTile { int expert, first, end; };
-__device__ __forceinline__ int tiles_before(const Group &g, int e0, int bm, int lane, int &from, int &to)
+struct GroupTiles { int from, to, until; };   // of a lane's expert: its pairs, and its last tile's number, counted from the 64 experts' first
+__device__ __forceinline__ GroupTiles tiles_of(const Group &g, int e0, int bm, int lane)
 {
-    const int e = min(e0 + lane, g.experts - 1);
-    from = bounded(g, e);
-    to = max(bounded(g, e + 1), from);
+    const int e = min(e0 + lane, g.experts - 1), from = bounded(g, e), to = max(bounded(g, e + 1), from);
     int n = e0 + lane < g.experts ? (to - from + bm - 1) / bm : 0;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(n, o);
-        n += lane >= o ? v : 0;
-    }
-    return n;   // of this lane's expert and those before it from e0 on
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4 and 8: sums along each sixteen lanes
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);   // row_bcast:15 and 31
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
+    return {from, to, n};
 }
-__device__ __forceinline__ int tiles_of_all(const Group &g, int bm, int lane)
+// of all experts, `first` those of the first 64
+__device__ __forceinline__ int count_tiles(const Group &g, const GroupTiles &first, int bm, int lane)
 {
-    int n = 0, from, to;
-    for (int e0 = 0; e0 < g.experts; e0 += 64) n += __builtin_amdgcn_readlane(tiles_before(g, e0, bm, lane, from, to), 63);
+    int n = __builtin_amdgcn_readlane(first.until, 63);
+    for (int e0 = 64; e0 < g.experts; e0 += 64) n += __builtin_amdgcn_readlane(tiles_of(g, e0, bm, lane).until, 63);
     return n;
 }
-__device__ __forceinline__ GroupTile tile_in_group(const Group &g, int t, int bm, int lane)
+__device__ __forceinline__ GroupTile tile_in_group(const Group &g, const GroupTiles &first, int t, int bm, int lane)
 {
-    for (int e0 = 0; e0 < g.experts; e0 += 64) {
-        int from, to;
-        const int n = tiles_before(g, e0, bm, lane, from, to), last = __builtin_amdgcn_readlane(n, 63);
+    GroupTiles in = first;
+    for (int e0 = 0;;) {
+        const int last = __builtin_amdgcn_readlane(in.until, 63);
         if (t < last) {
-            const int l = __builtin_ctzll(__ballot(t < n));   // the first expert that has it
-            const int end = __builtin_amdgcn_readlane(to, l), after = __builtin_amdgcn_readlane(n, l), start = __builtin_amdgcn_readlane(from, l);
-            const int all = (end - start + bm - 1) / bm;
-            return {e0 + l, start + (t - (after - all)) * bm, end};
+            const int l = __builtin_ctzll(__ballot(t < in.until));   // the first expert that has it
+            const int end = __builtin_amdgcn_readlane(in.to, l), after = __builtin_amdgcn_readlane(in.until, l), start = __builtin_amdgcn_readlane(in.from, l);
+            return {e0 + l, start + (t - (after - (end - start + bm - 1) / bm)) * bm, end};
         }
         t -= last;
+        e0 += 64;
+        if (e0 >= g.experts) return {0, 0, 0};
+        in = tiles_of(g, e0, bm, lane);
     }
-    return {0, 0, 0};
 }
+
 template <class T, int P, int EPI, class S, bool SUMS, int GROUP = G_NONE>
 __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs arg)
 {
-    constexpr bool PAIR = EPI == E_GATED, GATHER = GROUP == G_TOKENS;
+    constexpr bool PAIR = EPI == E_GATED, GATHER = GROUP == G_TOKENS, TERMS = GROUP == G_TERMS_A || GROUP == G_TERMS_B;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int tm, tn, m0;
     ProductArgs mine;   // this expert's product; its operands lie so many bytes on
     int64_t a_on = 0, b_on = 0;
+    int from = 0;      // TERMS: the expert's first pair
     if constexpr (GROUP != G_NONE) {
         mine = arg;
         const Group &g = arg.group;
-        int e;
-        if constexpr (GROUP == G_TERMS) {
-            e = blockIdx.y;
-            const int from = bounded(g, e), to = bounded(g, e + 1);
-            mine.K = max(to - from, 0);
-            a_on = from * arg.lda;
-            b_on = from * arg.ldb;
-            mine.steps = (mine.K + 128 / (int)sizeof(T) - 1) / (128 / (int)sizeof(T));
+        if constexpr (TERMS) {
+            const int e = blockIdx.y;
+            from = bounded(g, e);
+            mine.K = max(bounded(g, e + 1) - from, 0);
+            if (GROUP == G_TERMS_B) a_on = from * arg.lda;
+            else b_on = from * arg.ldb;
             mine.f.y = static_cast<char *>(arg.f.y) + e * g.c_stride;
             mine.f.y2 = static_cast<char *>(arg.f.y2) + e * g.c_stride;
             tile_of(blockIdx.x, arg.tiles_m, arg.tiles_n, tm, tn);
             m0 = tm * S::BM;
         } else {
-            const int all = min(tiles_of_all(g, S::BM, lane), arg.tiles_m);   // (whatever the lists hold)
+            const GroupTiles first = tiles_of(g, 0, S::BM, lane);
+            const int all = min(count_tiles(g, first, S::BM, lane), arg.tiles_m);   // (whatever the lists hold)
             if ((int)blockIdx.x >= all * arg.tiles_n) return;
             tile_of(blockIdx.x, all, arg.tiles_n, tm, tn);
-            const GroupTile t = tile_in_group(g, tm, S::BM, lane);
+            const GroupTile t = tile_in_group(g, first, tm, S::BM, lane);
             m0 = t.first;
             mine.M = t.end;
             b_on = t.expert * g.b_stride;
@@ -499,14 +519,15 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     }
     const ProductArgs &a = GROUP != G_NONE ? mine : arg;
     const int part_of_k = GROUP != G_NONE ? 0 : blockIdx.y;
-    typedef Operand<T, S::BM, S::NW, P == P_GRAD, false, GATHER> OpA;
-    typedef Operand<T, S::BN, S::NW, P != P_FWD, PAIR> OpB;
+    typedef Operand<T, S::BM, S::NW, P == P_GRAD, false, GATHER || GROUP == G_TERMS_A> OpA;
+    typedef Operand<T, S::BN, S::NW, P != P_FWD, PAIR, GROUP == G_TERMS_B> OpB;
     constexpr int COLS = PAIR ? S::BN / 2 : S::BN;
     constexpr int A_BYTES = OpA::STAGE;
     constexpr int LOADS = OpA::Q + OpB::Q;   // of a wave and stage
     __shared__ __attribute__((aligned(1024))) char stage0[A_BYTES + OpB::STAGE];
     __shared__ __attribute__((aligned(1024))) char stage1[A_BYTES + OpB::STAGE];
     __shared__ __attribute__((aligned(1024))) char stage2[S::NB == 3 ? A_BYTES + OpB::STAGE : 16];
+    __shared__ uint32_t rows_at[TERMS ? terms_of<T>() + (S::NB + 1) * 128 / (int)sizeof(T) : 1];   // bytes before the terms' rows; the stages past the last ones
     const int n0 = tn * COLS;
     const int wm = wave / S::WN, wn = wave % S::WN;
 
@@ -522,7 +543,7 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
         ob.next += b_on;
     }
     const int per_seg = (a.K + OpA::BK - 1) / OpA::BK, all = per_seg * a.segments;
-    const int t0 = part_of_k * a.steps, t1 = min(all, t0 + a.steps);
+    int t0 = part_of_k * a.steps, t1 = min(all, t0 + a.steps);
 
     v4f acc[S::TM][S::TN] = {};
     float sum[SUMS ? S::TM : 1] = {};   // the lane's part of A's sums over k
@@ -557,10 +578,13 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     Half f0, f1;
     typename OpA::Aim aim_a;
     typename OpB::Aim aim_b;
+    int terms = 0;   // TERMS: the terms before those in rows_at
     auto prepare = [&](int t) {
-        const bool second = t >= per_seg;
-        aim_a = oa.aim(t < t1, second, second ? t - per_seg : t, OpA::MC_ ? a.K : a.a_ext);
-        aim_b = ob.aim(t < t1, second, second ? t - per_seg : t, OpB::MC_ ? a.K : a.b_ext);
+        const bool second = !TERMS && t >= per_seg;
+        if constexpr (GROUP == G_TERMS_A) aim_a = oa.aim_rows(t < t1, t - terms / OpA::BK, (typename OpA::Rows)rows_at, a.group.rows, wave, lane);
+        else aim_a = oa.aim(t < t1, second, second ? t - per_seg : t, OpA::MC_ ? a.K : a.a_ext);
+        if constexpr (GROUP == G_TERMS_B) aim_b = ob.aim_rows(t < t1, t - terms / OpB::BK, (typename OpB::Rows)rows_at, a.group.rows, wave, lane);
+        else aim_b = ob.aim(t < t1, second, second ? t - per_seg : t, OpB::MC_ ? a.K : a.b_ext);
     };
     auto fetch = [&](char *stage) {
         oa.fetch((lds_char *)stage, aim_a, wave);
@@ -581,34 +605,47 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
         multiply(f1, AHEAD, S::TM);
         order_second<OpB::READS, OpA::READS, LOADS, S::TN, S::TM, EACH, AHEAD>();
     };
-    prepare(t0);
-    fetch(stage0);
-    prepare(t0 + 1);
-    fetch(stage1);
-    if (S::NB == 3) {
-        prepare(t0 + 2);
-        fetch(stage2);
-    }
-    arrived<(S::NB - 1) * LOADS>();
-    read(f0, stage0, 0);
-    int t = t0;
-    if constexpr (S::NB == 3) {
-        for (; t + 2 < t1; t += 3) {
-            stage(stage0, stage1, t);
-            stage(stage1, stage2, t + 1);
-            stage(stage2, stage0, t + 2);
+    do {
+        if constexpr (TERMS) {   // a run of terms at a time, whose rows the workgroup looks up first
+            constexpr int TERMS_NOW = terms_of<T>();
+            static_assert(TERMS_NOW % (2 * OpA::BK) == 0, "whole pairs of stages");
+            const int now = min(a.K - terms, TERMS_NOW);
+            for (int i = threadIdx.x; i < TERMS_NOW + (S::NB + 1) * OpA::BK; i += S::NW * 64)
+                rows_at[i] = i < now ? (uint32_t)token_of(a.group, from + terms + i) * (uint32_t)(GROUP == G_TERMS_A ? a.lda : a.ldb) : 0x80000000u;
+            __syncthreads();
+            t0 = terms / OpA::BK;
+            t1 = t0 + (now + OpA::BK - 1) / OpA::BK;
         }
-        if (t < t1) stage(stage0, stage1, t);
-        if (t + 1 < t1) stage(stage1, stage2, t + 1);
-    } else {
-        // Large tiles: a stage past the last one is zeros.  (A loop's tail of its own costs registers that they do not have.)
-        for (; t + (S::TM == 8 ? 0 : 1) < t1; t += 2) {
-            stage(stage0, stage1, t);
-            stage(stage1, stage0, t + 1);
+        prepare(t0);
+        fetch(stage0);
+        prepare(t0 + 1);
+        fetch(stage1);
+        if (S::NB == 3) {
+            prepare(t0 + 2);
+            fetch(stage2);
         }
-        if (S::TM != 8 && t < t1) stage(stage0, stage1, t);
-    }
-    arrived<0>();
+        arrived<(S::NB - 1) * LOADS>();
+        read(f0, stage0, 0);
+        int t = t0;
+        if constexpr (S::NB == 3) {
+            for (; t + 2 < t1; t += 3) {
+                stage(stage0, stage1, t);
+                stage(stage1, stage2, t + 1);
+                stage(stage2, stage0, t + 2);
+            }
+            if (t < t1) stage(stage0, stage1, t);
+            if (t + 1 < t1) stage(stage1, stage2, t + 1);
+        } else {
+            // Large tiles: a stage past the last one is zeros.  (A loop's tail of its own costs registers that they do not have.)
+            for (; t + (S::TM == 8 ? 0 : 1) < t1; t += 2) {
+                stage(stage0, stage1, t);
+                stage(stage1, stage0, t + 1);
+            }
+            if (S::TM != 8 && t < t1) stage(stage0, stage1, t);
+        }
+        arrived<0>();
+        terms += terms_of<T>();
+    } while (TERMS && terms < a.K);
 
     // Epilogue.  A wave turns its sums through its own 16 KB of LDS, sixty-four rows (or all it has) at a time, so that a lane gets eight
     // neighbouring columns of a row: rows of 256 bytes, their 16-byte units u at u ^ (row mod 16).  No bank conflicts but a pair's: sixteen of its

@@ -118,6 +118,13 @@ def test_tiles(name, rows, experts, k, d, f):
 
 
 @pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("rows", [959, 960, 961, 1919, 1920, 1921, 3841, 5000])
+def test_long_runs(name, rows):
+    """Experts with more rows than a workgroup of the matrices' gradients looks up at a time (960 in fp32, 1920 in 16 bits), to a row."""
+    Case(TYPES[name], rows, 2, 2, 24, 40, seed=rows, pad=rows % 3).check()
+
+
+@pytest.mark.parametrize("name", TYPES)
 @pytest.mark.parametrize("act", ACTS)
 def test_activations(name, act):
     Case(TYPES[name], 50, 4, 2, 96, 80, act=act, seed=7).check()
