@@ -62,6 +62,15 @@ __device__ __forceinline__ double total(double v)
     return last_lane(v);
 }
 
+// 1 / x of an x from 1 on: the hardware's estimate and two Newton steps; 0 of infinity, NaN of NaN
+__device__ __forceinline__ double inverse64(double x)
+{
+    double r = __builtin_amdgcn_rcp(x);
+    r = fma(fma(-x, r, 1.), r, r);
+    r = fma(fma(-x, r, 1.), r, r);
+    return x < 1e300 ? r : x == x ? 0. : x;
+}
+
 // sigmoid(l) e^-low, low <= 0 and not below the largest of the logits that are compared (or 0): ratios of small scores keep their bits
 __device__ __forceinline__ float sigmoid_above(float l, float low)
 {
@@ -84,14 +93,39 @@ __device__ __forceinline__ float weight_of(const RouteArgs &a, float l, bool min
     return x * a.scale;
 }
 
+// The two highest of p and q (p >= q) and of another lane's, whose lane the move names
+template <int CTRL>
+__device__ __forceinline__ void best_two(double &p, double &q)
+{
+    const double x = dpp_move64<CTRL, 0xf>(p, p), y = dpp_move64<CTRL, 0xf>(q, q);
+    q = fmax(fmin(p, x), fmax(q, y));
+    p = fmax(p, x);
+}
+template <int CTRL>
+__device__ __forceinline__ void best_two(float &p, float &q)
+{
+    const float x = dpp_move<CTRL, 0xf>(p, p), y = dpp_move<CTRL, 0xf>(q, q);
+    q = fmaxf(fminf(p, x), fmaxf(q, y));
+    p = fmaxf(p, x);
+}
+__device__ __forceinline__ double from_lane(double v, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ float from_lane(float v, int lane)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+
 // A wave takes a row, a lane V neighbouring experts of it.  The highest of all lanes, k times: of equal ones the lowest lane holds the
 // lowest expert.  WIDE: ranks are scores in 64 bits plus the bias; otherwise the logits themselves.
 template <class T, int V, bool WIDE>
-__global__ __launch_bounds__(kWaves * 64) void route_kernel(const RouteArgs a)
+__device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
 {
     typedef typename std::conditional<WIDE, double, float>::type Rank;
-    const int lane = threadIdx.x & 63, row = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = lane * V;
-    if (row >= a.rows) return;
+    const int first = lane * V;
     const Rank ninf = -INFINITY;
     const T *p = static_cast<const T *>(a.l) + row * a.ldl;
     float l[V], high = -INFINITY;
@@ -117,7 +151,7 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(const RouteArgs a)
             for (int i = 0; i < V; ++i) c[i] /= s;
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) c[i] = 1. / (1. + exp(-(double)l[i]));
+            for (int i = 0; i < V; ++i) c[i] = inverse64(1. + exp(-(double)l[i]));
         }
         if (a.bias)
 #pragma unroll
@@ -134,7 +168,35 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(const RouteArgs a)
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) c[i] = l[i] == -INFINITY ? ninf : c[i] == c[i] ? c[i] : (Rank)INFINITY;
-    if (a.top_groups < a.groups) {
+    const int lanes = a.each / V;   // of a group, where it is whole lanes and a power of two of them
+    if (a.top_groups < a.groups && a.each % V == 0 && (lanes & (lanes - 1)) == 0) {
+        // every lane forms its group's score with the others, and then counts the groups before its own
+        Rank p = ninf, q = ninf;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            q = c[i] > p ? p : c[i] > q ? c[i] : q;
+            p = c[i] > p ? c[i] : p;
+        }
+        if (lanes > 1) best_two<0xB1>(p, q);     // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
+        if (lanes > 2) best_two<0x4E>(p, q);
+        if (lanes > 4) best_two<0x141>(p, q);
+        if (lanes > 8) best_two<0x140>(p, q);
+        for (int o = 16; o < lanes; o <<= 1) {
+            const Rank x = __shfl_xor(p, o), y = __shfl_xor(q, o), low = x < p ? x : p, high = y > q ? y : q;
+            p = x > p ? x : p;
+            q = low > high ? low : high;
+        }
+        if (a.best == 2 && q > ninf) p += q;
+        int before = 0;
+        const int mine = lane / lanes;
+        for (int g = 0; g < a.groups; ++g) {
+            const Rank other = from_lane(p, g * lanes);
+            before += other > p || (other == p && g < mine);
+        }
+        if (before >= a.top_groups)
+#pragma unroll
+            for (int i = 0; i < V; ++i) c[i] = ninf;
+    } else if (a.top_groups < a.groups) {
         Rank score = ninf;   // lane g: group g's
         for (int g = 0; g < a.groups; ++g) {
             const int from = g * a.each, to = from + a.each;
@@ -175,9 +237,21 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(const RouteArgs a)
 #pragma unroll
     for (int i = 0; i < V; ++i) b = c[i] > b ? c[i] : b;
     for (int j = 0; j < a.k; ++j) {
-        const Rank best = highest(b);
-        if (!(best > ninf)) break;
-        const int f = __builtin_ctzll(__ballot(b == best));
+        // Rounding keeps the order: a lane that alone has the highest of the ranks rounded to 32 bits has the highest.
+        const float top = wave_max((float)b);
+        if (!(top > -INFINITY)) break;
+        uint64_t have = __ballot((float)b == top);
+        Rank best;
+        if constexpr (WIDE) {
+            if (have & (have - 1)) {   // (every lane takes part)
+                const Rank of_those = highest((float)b == top ? b : ninf);
+                have = __ballot(b == of_those);
+            }
+            best = b;   // (of the lane that has it)
+        } else {
+            best = top;
+        }
+        const int f = __builtin_ctzll(have);
         int at = 0;
         float mine = l[0];
 #pragma unroll
@@ -210,6 +284,13 @@ __global__ __launch_bounds__(kWaves * 64) void route_kernel(const RouteArgs a)
 // With u = w / scale the weights without their scale and g = scale dw:
 //   softmax, renorm: dl_j = u_j (g_j - sum g u);  sigmoid, renorm: the same times 1 - s_j (chosen experts only, as every s drops out of
 //   the others' ratio);  sigmoid: dl_j = g_j s_j (1 - s_j);  softmax: dl = s (g - sum g s) over all of a row, g 0 but where chosen.
+template <class T, int V, bool WIDE>
+__global__ __launch_bounds__(kWaves * 64) void route_kernel(const RouteArgs a)
+{
+    const int row = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row < a.rows) route_row<T, V, WIDE>(a, row, threadIdx.x & 63);
+}
+
 template <class T, int V>
 __global__ __launch_bounds__(kWaves * 64) void route_back_kernel(const RouteArgs a)
 {
@@ -293,12 +374,14 @@ __global__ __launch_bounds__(256) void count_kernel(const ListArgs a)
 }
 
 // one chunk: it counts itself
-__global__ __launch_bounds__(256) void place_kernel(const ListArgs a)
+__device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
 {
     __shared__ int32_t next[4][kMostExperts], all[kMostExperts], sums[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int from = blockIdx.x * a.chunk + wave * (a.chunk / 4), to = min(from + a.chunk / 4, a.pairs);   // the wave's pairs
-    for (int e = threadIdx.x; e < 4 * kMostExperts; e += 256) next[0][e] = 0;
+    const int from = block * a.chunk + wave * (a.chunk / 4), to = min(from + a.chunk / 4, a.pairs);   // the wave's pairs
+    #pragma unroll
+    for (int w = 0; w < 4; ++w)
+        for (int e = threadIdx.x; e < a.experts; e += 256) next[w][e] = 0;
     __syncthreads();
     for (int i = from + lane; i < to; i += 64) {
         const int e = a.expert[i];
@@ -308,23 +391,28 @@ __global__ __launch_bounds__(256) void place_kernel(const ListArgs a)
     // `all`: an expert's pairs; next[w]: those of earlier chunks and of earlier waves of this one
     for (int e = threadIdx.x; e < kMostExperts; e += 256) {
         int own = 0, before = 0, sum = 0;
-        int32_t c[4];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            c[w] = own;
-            own += next[w][e];
-        }
         if (e < a.experts) {
+            int32_t c[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                c[w] = own;
+                own += next[w][e];
+            }
             if (a.chunks == 1) sum = own;
             else
-                for (int b = 0; b < a.chunks; ++b) {
-                    const int n = a.counts[b * a.experts + e];
-                    before += b < (int)blockIdx.x ? n : 0;
-                    sum += n;
-                }
-        }
+                for (int b0 = 0; b0 < a.chunks; b0 += 16) {   // sixteen loads under way
+                    int n[16];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) next[w][e] = before + c[w];
+                    for (int q = 0; q < 16; ++q) n[q] = a.counts[min(b0 + q, a.chunks - 1) * a.experts + e];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        before += b0 + q < block ? n[q] : 0;
+                        sum += b0 + q < a.chunks ? n[q] : 0;
+                    }
+                }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) next[w][e] = before + c[w];
+        }
         all[e] = sum;
     }
     __syncthreads();
@@ -356,9 +444,9 @@ __global__ __launch_bounds__(256) void place_kernel(const ListArgs a)
         const int start = before + n[i];
 #pragma unroll
         for (int w = 0; w < 4; ++w) next[w][e] += start;
-        if (blockIdx.x == 0) a.starts[e] = start;
+        if (block == 0) a.starts[e] = start;
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.starts[a.experts] = total;
+    if (block == 0 && threadIdx.x == 0) a.starts[a.experts] = total;
     __syncthreads();
     // sixty-four pairs at a time: a pair's place is its expert's next one and how many lanes below have the same expert
     for (int i = from; i < to; i += 64) {
@@ -388,6 +476,21 @@ __global__ __launch_bounds__(256) void place_kernel(const ListArgs a)
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
     }
     for (int p = max(from, total) + lane; p < to; p += 64) a.order[p] = -1;
+}
+
+__global__ __launch_bounds__(256) void place_kernel(const ListArgs a)
+{
+    place_chunk(a, blockIdx.x);
+}
+
+// Few rows: choices and lists in one launch of one workgroup, a wave a row at a time.
+template <class T, int V, bool WIDE>
+__global__ __launch_bounds__(256) void route_few_kernel(const RouteArgs a, const ListArgs lists)
+{
+    for (int row = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); row < a.rows; row += 4) route_row<T, V, WIDE>(a, row, threadIdx.x & 63);
+    __threadfence_block();
+    __syncthreads();
+    place_chunk(lists, 0);
 }
 
 constexpr int kMostChunks = 128;   // each workgroup reads all counts
@@ -440,12 +543,19 @@ dn_status route_of(const dn_route_desc *d, RouteArgs &a)
     return DN_OK;
 }
 
-template <class T, int V>
-void forward_as(const RouteArgs &a, hipStream_t s)
+constexpr int kOneLaunchRows = 8;   // of one workgroup
+
+template <class T, int V, bool WIDE>
+void choose_as(const RouteArgs &a, const ListArgs *lists, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.rows + kWaves - 1) / kWaves)), block(kWaves * 64);
-    if (a.bias || (a.top_groups < a.groups && a.best == 2)) launch_kernel(route_kernel<T, V, true>, grid, block, 0, s, a);
-    else launch_kernel(route_kernel<T, V, false>, grid, block, 0, s, a);
+    if (lists) launch_kernel(route_few_kernel<T, V, WIDE>, dim3(1), dim3(256), 0, s, a, *lists);
+    else launch_kernel(route_kernel<T, V, WIDE>, dim3((unsigned)((a.rows + kWaves - 1) / kWaves)), dim3(kWaves * 64), 0, s, a);
+}
+template <class T, int V>
+void forward_as(const RouteArgs &a, const ListArgs *lists, hipStream_t s)
+{
+    if (a.bias || (a.top_groups < a.groups && a.best == 2)) choose_as<T, V, true>(a, lists, s);
+    else choose_as<T, V, false>(a, lists, s);
 }
 template <class T, int V>
 void backward_as(const RouteArgs &a, hipStream_t s)
@@ -453,18 +563,18 @@ void backward_as(const RouteArgs &a, hipStream_t s)
     launch_kernel(route_back_kernel<T, V>, dim3((unsigned)((a.rows + kWaves - 1) / kWaves)), dim3(kWaves * 64), 0, s, a);
 }
 template <class T>
-hipError_t run(const RouteArgs &a, bool back, hipStream_t s)
+hipError_t run(const RouteArgs &a, bool back, const ListArgs *lists, hipStream_t s)
 {
-    if (a.experts <= 64) back ? backward_as<T, 1>(a, s) : forward_as<T, 1>(a, s);
-    else if (a.experts <= 128) back ? backward_as<T, 2>(a, s) : forward_as<T, 2>(a, s);
-    else if (a.experts <= 256) back ? backward_as<T, 4>(a, s) : forward_as<T, 4>(a, s);
-    else if (a.experts <= 512) back ? backward_as<T, 8>(a, s) : forward_as<T, 8>(a, s);
-    else back ? backward_as<T, 16>(a, s) : forward_as<T, 16>(a, s);
+    if (a.experts <= 64) back ? backward_as<T, 1>(a, s) : forward_as<T, 1>(a, lists, s);
+    else if (a.experts <= 128) back ? backward_as<T, 2>(a, s) : forward_as<T, 2>(a, lists, s);
+    else if (a.experts <= 256) back ? backward_as<T, 4>(a, s) : forward_as<T, 4>(a, lists, s);
+    else if (a.experts <= 512) back ? backward_as<T, 8>(a, s) : forward_as<T, 8>(a, lists, s);
+    else back ? backward_as<T, 16>(a, s) : forward_as<T, 16>(a, lists, s);
     return hipGetLastError();
 }
-hipError_t launch_route(int type, const RouteArgs &a, bool back, hipStream_t s)
+hipError_t launch_route(int type, const RouteArgs &a, bool back, const ListArgs *lists, hipStream_t s)
 {
-    return type == DN_F32 ? run<float>(a, back, s) : type == DN_F16 ? run<f16>(a, back, s) : run<bf16>(a, back, s);
+    return type == DN_F32 ? run<float>(a, back, lists, s) : type == DN_F16 ? run<f16>(a, back, lists, s) : run<bf16>(a, back, lists, s);
 }
 
 template <class... P>
@@ -512,10 +622,14 @@ dn_status dn_route_forward(const dn_route_desc *d, const void *L_dev, const floa
     a.expert = expert_dev;
     a.weight = weight_dev;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    if (launch_route(d->type, a, false, stream) != hipSuccess) return DN_ERR_DEVICE;
-    if (!lists) return DN_OK;
-    return device(launch_lists({expert_dev, starts_dev, order_dev, place_dev, static_cast<int32_t *>(workspace_dev), d->rows * d->k, d->experts, 0, 0},
-                               stream));
+    ListArgs l{expert_dev, starts_dev, order_dev, place_dev, static_cast<int32_t *>(workspace_dev), d->rows * d->k, d->experts, 0, 0};
+    if (lists && d->rows <= kOneLaunchRows) {
+        l.chunk = chunk_of(l.pairs);
+        l.chunks = 1;
+        return device(launch_route(d->type, a, false, &l, stream));
+    }
+    if (launch_route(d->type, a, false, nullptr, stream) != hipSuccess) return DN_ERR_DEVICE;
+    return lists ? device(launch_lists(l, stream)) : DN_OK;
 }
 
 dn_status dn_route_backward(const dn_route_desc *d, const void *L_dev, const int32_t *expert_dev, const float *dweight_dev,
@@ -530,7 +644,7 @@ dn_status dn_route_backward(const dn_route_desc *d, const void *L_dev, const int
     a.chosen = expert_dev;
     a.dweight = dweight_dev;
     a.dl = dL_dev;
-    return device(launch_route(d->type, a, true, (hipStream_t)hip_stream));
+    return device(launch_route(d->type, a, true, nullptr, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"
