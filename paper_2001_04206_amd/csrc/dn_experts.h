@@ -12,4 +12,18 @@ hipError_t launch_experts_f16(Product p, Epilogue e, ProductKernel kernel, int g
 hipError_t launch_experts_bf16(Product p, Epilogue e, ProductKernel kernel, int gathered, ProductArgs a, int64_t tiles, hipStream_t s);
 int rows_of_tile(ProductKernel kernel);
 
+// Few tokens: the last product and the sum over a row's choices in one launch
+struct FewDown {
+    const void *h, *w, *r;
+    void *y;
+    const float *weight;
+    const int32_t *starts, *place;
+    int64_t ldh, ldw, w_stride;   // bytes
+    int64_t ldr, ldy;             // elements
+    int32_t N, K, k, experts, pairs;
+};
+hipError_t launch_few_down_f32(const FewDown &a, int rows, hipStream_t s);
+hipError_t launch_few_down_f16(const FewDown &a, int rows, hipStream_t s);
+hipError_t launch_few_down_bf16(const FewDown &a, int rows, hipStream_t s);
+
 }  // namespace dn

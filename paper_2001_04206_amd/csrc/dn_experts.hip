@@ -6,7 +6,7 @@
 namespace dn {
 namespace {
 
-constexpr int kMostExperts = 1024, kMostChoices = 32;
+constexpr int kFewTokens = 4, kMostExperts = 1024, kMostChoices = 32;
 constexpr int64_t kMostRows = (int64_t)1 << 26, kMostPairs = (int64_t)1 << 24, kMostBytes = ((int64_t)1 << 31) - 1;
 
 // ---- rows ------------------------------------------------------------------------------------------------------------
@@ -109,7 +109,7 @@ ProductKernel plan_experts(int type, Product p, Epilogue e, int64_t pairs, int e
         return t > met ? t : met;
     };
     if (p == P_FWD && (int64_t)K * size_of(type) >= 32 && most_tiles(pairs, experts, 16) * ((N + 15) / 16) < 1 << 23) {   // 2^32 threads
-        best = 6 + es * tiles_of(16) * planes * N * K / 4.6e6;
+        best = 6 + es * tiles_of(16) * planes * N * K / 5e6;
         kernel = K_FEW;
     }
     struct Way { ProductKernel kernel; int rows, cols, together; double stage, least, round; };
@@ -142,6 +142,7 @@ struct Block {
     dn_experts_desc d;
     int64_t pairs, ldh, ldz;     // between rows of H, of z
     ProductKernel up, down, dh, dx, dwgu, dwd;
+    bool few;                    // the last product forms the sums over choices itself
     bool pack_w;                 // the matrices are copied to 16-byte rows
     int parts;                   // of the weights' derivatives
     size_t h, z, x, w1, w2, fwd_bytes;                        // bytes of H, z, X, Wg (and Wu), Wd; workspace
@@ -173,6 +174,7 @@ dn_status block_of(const dn_experts_desc *d, Block &b)
     b.dx = plan_experts(d->type, P_DELTA, E_STORE, b.pairs, d->experts, d->d, d->f, 2);
     b.dwgu = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->d, (int)(2 * b.ldh), 1);
     b.dwd = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->f, d->d, 1);
+    b.few = b.down == K_FEW && d->rows <= kFewTokens;
     b.pack_w = d->d * e % 16 || d->f * e % 16;
     const size_t wgu = b.pack_w ? packed_bytes(d->type, n * d->f, d->d) : 0, wd = b.pack_w ? packed_bytes(d->type, n * d->d, d->f) : 0;
     b.h = up256((size_t)(b.pairs * b.ldh * e));
@@ -237,7 +239,7 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
     if (!b.pack_w && ((uintptr_t)Wg_dev | (uintptr_t)Wu_dev | (uintptr_t)Wd_dev) % 16) return DN_ERR_INVALID_ARG;
     if ((s = workspace(b.fwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const int64_t e = size_of(d->type), n = d->experts;
+    const int64_t e = size_of(d->type), n = d->experts, f = d->f;
     char *H = static_cast<char *>(workspace_dev), *z = H + b.h;
     const Group g{starts_dev, order_dev, d->experts, d->k, (int32_t)b.pairs, d->rows, 0, 0};
     ProductArgs a = product(g, 0, d->f, d->d, 1, 0), c = product(g, 0, d->d, d->f, 1, 0);
@@ -265,6 +267,13 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
     if (launch_experts(d->type, P_FWD, E_GATED, b.up, a, most_tiles(b.pairs, d->experts, rows_of_tile(b.up)), stream) != hipSuccess) return DN_ERR_DEVICE;
     operand_a(c, {H, b.ldh * e, (int32_t)b.ldh});
     c.group.b_stride = c.ldb * d->d;
+    if (b.few) {
+        const FewDown few{H, Wd_dev, R_dev, Y_dev, weight_dev, starts_dev, place_dev, b.ldh * e, f * e, f * e * d->d, b.d.ldr, b.d.ldy,
+                          d->d, d->f, d->k, d->experts, (int32_t)b.pairs};
+        return device(d->type == DN_F32   ? launch_few_down_f32(few, d->rows, stream)
+                      : d->type == DN_F16 ? launch_few_down_f16(few, d->rows, stream)
+                                          : launch_few_down_bf16(few, d->rows, stream));
+    }
     c.f.y = z;
     c.f.ldy = b.ldz;
     c.f.f32_out = 1;

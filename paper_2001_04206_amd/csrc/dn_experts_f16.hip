@@ -8,4 +8,6 @@ hipError_t launch_experts_f16(Product p, Epilogue e, ProductKernel kernel, int g
     return launch_experts<f16>(p, e, kernel, gathered, a, tiles, s);
 }
 
+hipError_t launch_few_down_f16(const FewDown &a, int rows, hipStream_t s) { return few_down<f16>(a, rows, s); }
+
 }  // namespace dn

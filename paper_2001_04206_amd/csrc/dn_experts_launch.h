@@ -24,9 +24,16 @@ hipError_t expert_few(const ProductArgs &a, int64_t tiles, hipStream_t s)
 {
     const uintptr_t all = (uintptr_t)a.a[0] | (uintptr_t)a.b[0] | (uintptr_t)a.b[1] | (uintptr_t)a.lda | (uintptr_t)a.ldb | (uintptr_t)a.group.b_stride |
                           (uintptr_t)a.K * sizeof(T);
-    const dim3 grid((unsigned)((a.N + 15) / 16) * (unsigned)tiles), block(512);
-    if (all % 16 == 0) launch_kernel(experts_few_kernel<T, EPI, 8, true, GROUP>, grid, block, 0, s, a);
-    else launch_kernel(experts_few_kernel<T, EPI, 8, false, GROUP>, grid, block, 0, s, a);
+    const dim3 grid((unsigned)((a.N + 15) / 16) * (unsigned)tiles);
+    // four waves have all of a short k under way, and more workgroups run at once
+    const bool shorter = (int64_t)a.K * (int)sizeof(T) <= 4 * 4 * 128;
+    if (all % 16 == 0) {
+        if (shorter) launch_kernel(experts_few_kernel<T, EPI, 4, true, GROUP>, grid, dim3(256), 0, s, a);
+        else launch_kernel(experts_few_kernel<T, EPI, 8, true, GROUP>, grid, dim3(512), 0, s, a);
+    } else {
+        if (shorter) launch_kernel(experts_few_kernel<T, EPI, 4, false, GROUP>, grid, dim3(256), 0, s, a);
+        else launch_kernel(experts_few_kernel<T, EPI, 8, false, GROUP>, grid, dim3(512), 0, s, a);
+    }
     return hipGetLastError();
 }
 
@@ -48,6 +55,16 @@ hipError_t expert_run(ProductKernel kernel, ProductArgs &a, int64_t tiles, hipSt
 }
 
 }  // namespace
+
+template <class T>
+hipError_t few_down(const FewDown &a, int rows, hipStream_t s)
+{
+    const uintptr_t all = (uintptr_t)a.h | (uintptr_t)a.w | (uintptr_t)a.ldh | (uintptr_t)a.ldw | (uintptr_t)a.w_stride | (uintptr_t)a.K * sizeof(T);
+    const dim3 grid((unsigned)((a.N + 7) / 8) * (unsigned)rows);
+    if (all % 16 == 0) launch_kernel(few_down_kernel<T, true>, grid, dim3(512), 0, s, a);
+    else launch_kernel(few_down_kernel<T, false>, grid, dim3(512), 0, s, a);
+    return hipGetLastError();
+}
 
 template <class T>
 hipError_t launch_experts(Product p, Epilogue e, ProductKernel kernel, int gathered, ProductArgs &a, int64_t tiles, hipStream_t s)
