@@ -28,7 +28,8 @@ struct JoinArgs {
     int64_t ldz, ldr, ldy;
     const float *weight;       // NULL: ones
     const int32_t *place;
-    int32_t rows, cols, k, pairs;
+    int32_t rows, cols, k, pairs, parts;
+    int64_t plane;             // elements between two parts of z
 };
 template <class T>
 __global__ __launch_bounds__(256) void join_pairs_kernel(const JoinArgs a)
@@ -49,6 +50,12 @@ __global__ __launch_bounds__(256) void join_pairs_kernel(const JoinArgs a)
             const bool has = j0 + q < a.k && (uint32_t)p < (uint32_t)a.pairs;
             w[q] = !has ? 0.f : a.weight ? a.weight[t * a.k + j] : 1.f;
             load8<float>(z[q], a.z, has ? p * a.ldz + n : 0, has ? left : 0);
+            for (int s = 1; s < a.parts; ++s) {
+                float more[8];
+                load8<float>(more, a.z, has ? s * a.plane + p * a.ldz + n : 0, has ? left : 0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[q][i] += more[i];
+            }
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
@@ -95,28 +102,35 @@ hipError_t launch_experts(int type, Product p, Epilogue e, ProductKernel kernel,
 // Tiles of rows: at most, whatever the lists hold.
 int64_t most_tiles(int64_t pairs, int experts, int rows) { return pairs / rows + (pairs < experts ? pairs : experts); }
 
-// Which kernel a product of the experts takes: the one expected to take least, by the times that plan_product goes by.  How the pairs
-// are spread is not known here: each expert's last tile is taken to be half full.
-ProductKernel plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, int N, int K, int segments)
+// Which kernel a product of the experts takes, and its k in how many parts: what is expected to take least, by the times that plan_product
+// goes by.  How the pairs are spread is not known here: each expert's last tile is taken to be half full.  Weights come at 4.6 TB/s (large
+// tiles: 3.8; the kernel for few rows: 5): 64 tokens through 8 of 64 experts, 2048 wide with 1024 hidden, take 108 us for the gated product
+// on the kernel for few rows (large tiles 141), 1024 tokens 249 on medium tiles (large ones 313), 128 191 on small ones (few rows 224).  The
+// product with the activation's derivative moves ten bytes an element beside it, and large tiles have no registers for that: 415 us on
+// medium ones at 8192 tokens, 442 on large ones.  Parts are for the products whose results the pairs' sums read: these add them too.
+struct Plan { ProductKernel kernel = K_SMALL; int parts = 1; };
+Plan plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, int N, int K, int segments)
 {
     const int planes = e == E_GATED ? 2 : 1, bk = type == DN_F32 ? 32 : 64;
     const double es = (double)size_of(type), met = (double)(pairs < experts ? pairs : experts);
+    const bool packed = p == P_FWD && (N * size_of(type) % 16 || K * size_of(type) % 16);   // tiles copy the matrices first
     const double weights = p == P_GRAD ? 0 : es * met * planes * N * K * segments / 4.6e6;
     double best = 1e300;
-    ProductKernel kernel = K_SMALL;
+    Plan plan;
     auto tiles_of = [&](int rows) {
         const double t = (double)pairs / rows + met / 2;
         return t > met ? t : met;
     };
     if (p == P_FWD && (int64_t)K * size_of(type) >= 32 && most_tiles(pairs, experts, 16) * ((N + 15) / 16) < 1 << 23) {   // 2^32 threads
         best = 6 + es * tiles_of(16) * planes * N * K / 5e6;
-        kernel = K_FEW;
+        plan.kernel = K_FEW;
     }
-    struct Way { ProductKernel kernel; int rows, cols, together; double stage, least, round; };
-    const Way tiny{K_TINY, 64, 128, 3, 0.95, 0.95, 6}, large{K_LARGE, 256, 256, 1, 1.5, 1.5, 8}, medium{K_MEDIUM, 128, 256, 1, 0.8, 0.8, 6};
-    const Way small = type == DN_F32 ? Way{K_SMALL, 128, 128, 2, 1.8, 1.8, 6} : Way{K_SMALL, 128, 128, 2, 0.5, 0.9, 4};
+    struct Way { ProductKernel kernel; int rows, cols, together; double stage, least, round, behind; };
+    const Way tiny{K_TINY, 64, 128, 3, 0.9, 0.9, 3, 1}, large{K_LARGE, 256, 256, 1, 1.5, 1.5, 8, 4.6 / 3.8}, medium{K_MEDIUM, 128, 256, 1, 0.8, 0.8, 6, 1};
+    const Way small = type == DN_F32 ? Way{K_SMALL, 128, 128, 2, 1.8, 1.8, 6, 1} : Way{K_SMALL, 128, 128, 2, 0.5, 0.9, 4, 1};
     for (const Way &w : {large, medium, small, tiny}) {
         if (type == DN_F32 ? w.kernel > K_SMALL : w.kernel == K_TINY) continue;
+        if (w.kernel == K_LARGE && e == E_DEXPERT) continue;
         const int64_t cols = w.cols / planes;
         double tiles = (double)((N + cols - 1) / cols), steps;
         if (p == P_GRAD) {   // K: the result's rows; its terms are the pairs
@@ -126,27 +140,30 @@ ProductKernel plan_experts(int type, Product p, Epilogue e, int64_t pairs, int e
             tiles *= tiles_of(w.rows);
             steps = (double)((K + bk - 1) / bk * segments);
         }
-        const double deep = ceil(tiles / 256), rounds = ceil(deep / w.together);
-        const double stage = deep * w.stage > rounds * w.least ? deep * w.stage : rounds * w.least;
-        double us = steps * stage + rounds * w.round;
-        if (us < weights) us = weights;
-        if (us < best) {
-            best = us;
-            kernel = w.kernel;
+        for (int parts = 1; parts <= (e == E_STORE && p != P_GRAD ? 4 : 1) && parts * 4 <= steps; ++parts) {
+            const double deep = ceil(tiles * parts / 256), rounds = ceil(deep / w.together);
+            const double stage = deep * w.stage > rounds * w.least ? deep * w.stage : rounds * w.least;
+            double us = ceil(steps / parts) * stage + rounds * w.round;
+            if (us < weights * w.behind) us = weights * w.behind;
+            us += (parts - 1) * 8. * pairs * N / 4.5e6 + (packed ? 4 + 2 * es * experts * planes * N * K / 4.6e6 : 0);
+            if (us < best) {
+                best = us;
+                plan = {w.kernel, parts};
+            }
         }
     }
-    return kernel;
+    return plan;
 }
 
 struct Block {
     dn_experts_desc d;
     int64_t pairs, ldh, ldz;     // between rows of H, of z
-    ProductKernel up, down, dh, dx, dwgu, dwd;
+    Plan up, down, dh, dx, dwgu, dwd;
     bool few;                    // the last product forms the sums over choices itself
     bool pack_w;                 // the matrices are copied to 16-byte rows
     int parts;                   // of the weights' derivatives
     size_t h, z, x, w1, w2, fwd_bytes;                        // bytes of H, z, X, Wg (and Wu), Wd; workspace
-    size_t sorted, dots, dgu, bwd_bytes;
+    size_t sorted, dots, dgu, dx_parts, bwd_bytes;            // the pairs' dX
 };
 
 dn_status block_of(const dn_experts_desc *d, Block &b)
@@ -174,20 +191,21 @@ dn_status block_of(const dn_experts_desc *d, Block &b)
     b.dx = plan_experts(d->type, P_DELTA, E_STORE, b.pairs, d->experts, d->d, d->f, 2);
     b.dwgu = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->d, (int)(2 * b.ldh), 1);
     b.dwd = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->f, d->d, 1);
-    b.few = b.down == K_FEW && d->rows <= kFewTokens;
+    b.few = b.down.kernel == K_FEW && d->rows <= kFewTokens;
     b.pack_w = d->d * e % 16 || d->f * e % 16;
     const size_t wgu = b.pack_w ? packed_bytes(d->type, n * d->f, d->d) : 0, wd = b.pack_w ? packed_bytes(d->type, n * d->d, d->f) : 0;
     b.h = up256((size_t)(b.pairs * b.ldh * e));
-    b.z = up256((size_t)(b.pairs * b.ldz) * sizeof(float));
+    b.z = up256((size_t)(b.pairs * b.ldz * b.down.parts) * sizeof(float));
+    b.dx_parts = up256((size_t)(b.pairs * b.ldz * b.dx.parts) * sizeof(float));
     b.x = packed_bytes(d->type, d->rows, d->d);
     b.w1 = wgu;
     b.w2 = wd;
-    b.fwd_bytes = b.h + b.z + (b.up == K_FEW ? 0 : b.x + 2 * wgu) + (b.down == K_FEW ? 0 : wd);
+    b.fwd_bytes = b.h + b.z + (b.up.kernel == K_FEW ? 0 : b.x + 2 * wgu) + (b.down.kernel == K_FEW ? 0 : wd);
     b.parts = (int)((d->f + 255) / 256 * 4);   // of 64 columns, whole tiles
     b.sorted = up256((size_t)b.pairs * sizeof(float));
     b.dots = up256((size_t)b.pairs * b.parts * sizeof(float));
     b.dgu = up256((size_t)(b.pairs * 2 * b.ldh * e));
-    b.bwd_bytes = b.sorted + b.dots + b.h + b.dgu + b.z + 2 * b.x + 2 * wgu + wd;
+    b.bwd_bytes = b.sorted + b.dots + b.h + b.dgu + b.dx_parts + 2 * b.x + 2 * wgu + wd;
     return DN_OK;
 }
 
@@ -198,6 +216,7 @@ ProductArgs product(const Group &g, int M, int N, int K, int segments, int64_t b
     a.N = N;
     a.K = K;
     a.segments = segments;
+    a.split = 1;
     a.group = g;
     a.group.b_stride = b_stride;
     return a;
@@ -244,7 +263,7 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
     const Group g{starts_dev, order_dev, d->experts, d->k, (int32_t)b.pairs, d->rows, 0, 0};
     ProductArgs a = product(g, 0, d->f, d->d, 1, 0), c = product(g, 0, d->d, d->f, 1, 0);
     Packer pack{d->type, z + b.z};
-    if (b.up == K_FEW) {
+    if (b.up.kernel == K_FEW) {
         operand_a(a, {X_dev, b.d.ldx * e, d->d});
         operand_b(a, {Wg_dev, d->d * e, d->d});
         a.b[1] = Wu_dev;
@@ -253,7 +272,7 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
         operand_b(a, pack.take(Wg_dev, d->d, n * d->f, d->d, b.pack_w));
         a.b[1] = pack.take(Wu_dev, d->d, n * d->f, d->d, b.pack_w).p;
     }
-    if (b.down == K_FEW) operand_b(c, {Wd_dev, d->f * e, d->f});
+    if (b.down.kernel == K_FEW) operand_b(c, {Wd_dev, d->f * e, d->f});
     else operand_b(c, pack.take(Wd_dev, d->f, n * d->d, d->f, b.pack_w));
     if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
     a.group.b_stride = a.ldb * d->f;
@@ -264,7 +283,8 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
     a.f.ldy2 = 2 * (int64_t)d->f;
     a.f.half = d->f;
     a.f.act = d->act;
-    if (launch_experts(d->type, P_FWD, E_GATED, b.up, a, most_tiles(b.pairs, d->experts, rows_of_tile(b.up)), stream) != hipSuccess) return DN_ERR_DEVICE;
+    auto tiles = [&](const Plan &p) { return most_tiles(b.pairs, d->experts, rows_of_tile(p.kernel)); };
+    if (launch_experts(d->type, P_FWD, E_GATED, b.up.kernel, a, tiles(b.up), stream) != hipSuccess) return DN_ERR_DEVICE;
     operand_a(c, {H, b.ldh * e, (int32_t)b.ldh});
     c.group.b_stride = c.ldb * d->d;
     if (b.few) {
@@ -277,8 +297,10 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
     c.f.y = z;
     c.f.ldy = b.ldz;
     c.f.f32_out = 1;
-    if (launch_experts(d->type, P_FWD, E_STORE, b.down, c, most_tiles(b.pairs, d->experts, rows_of_tile(b.down)), stream) != hipSuccess) return DN_ERR_DEVICE;
-    return device(launch_join(d->type, {reinterpret_cast<const float *>(z), R_dev, Y_dev, b.ldz, b.d.ldr, b.d.ldy, weight_dev, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream));
+    c.split = b.down.parts;
+    c.group.c_stride = b.pairs * b.ldz * (int64_t)sizeof(float);
+    if (launch_experts(d->type, P_FWD, E_STORE, b.down.kernel, c, tiles(b.down), stream) != hipSuccess) return DN_ERR_DEVICE;
+    return device(launch_join(d->type, {reinterpret_cast<const float *>(z), R_dev, Y_dev, b.ldz, b.d.ldr, b.d.ldy, weight_dev, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs, b.down.parts, b.pairs * b.ldz}, stream));
 }
 
 dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
@@ -302,7 +324,7 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
     char *sorted = static_cast<char *>(workspace_dev), *dots = sorted + b.sorted, *H = dots + b.dots;
     char *dG = H + b.h, *dU = dG + b.ldh * e, *dx = dG + b.dgu;
     const Group g{starts_dev, order_dev, d->experts, d->k, (int32_t)b.pairs, d->rows, 0, 0};
-    Packer pack{d->type, dx + b.z};
+    Packer pack{d->type, dx + b.dx_parts};
     const Packer::Rows X = pack.take(X_dev, b.d.ldx, d->rows, d->d), dY = pack.take(dY_dev, b.d.ldy, d->rows, d->d);
     if (b.pack_w && pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;   // (four matrices a launch)
     if (b.pack_w) pack.a = {};
@@ -312,7 +334,7 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
     if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
     launch_kernel(sort_weights_kernel, dim3((unsigned)((b.pairs + 255) / 256)), dim3(256), 0, stream, g, weight_dev, reinterpret_cast<float *>(sorted));
     if (hipGetLastError() != hipSuccess) return DN_ERR_DEVICE;
-    auto tiles = [&](ProductKernel k) { return most_tiles(b.pairs, d->experts, rows_of_tile(k)); };
+    auto tiles = [&](const Plan &p) { return most_tiles(b.pairs, d->experts, rows_of_tile(p.kernel)); };
     {   // dh, and from it dG, dU, w H and the weights' derivatives
         ProductArgs a = product(g, 0, d->f, d->d, 1, Wd.ld * d->d);
         operand_a(a, dY);
@@ -330,10 +352,10 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
         a.f.row_scale = reinterpret_cast<const float *>(sorted);
         a.f.dots = reinterpret_cast<float *>(dots);
         a.f.dots_ld = b.pairs;
-        if (launch_experts(d->type, P_DELTA, E_DEXPERT, b.dh, a, tiles(b.dh), stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_experts(d->type, P_DELTA, E_DEXPERT, b.dh.kernel, a, tiles(b.dh), stream) != hipSuccess) return DN_ERR_DEVICE;
     }
     if (dweight_dev) {
-        const int cols = b.dh == K_SMALL || b.dh == K_TINY ? 128 : 256, parts = (int)((f + cols - 1) / cols * (cols / 64));
+        const int cols = b.dh.kernel == K_SMALL || b.dh.kernel == K_TINY ? 128 : 256, parts = (int)((f + cols - 1) / cols * (cols / 64));
         launch_kernel(dots_kernel, dim3((unsigned)((b.pairs + 255) / 256)), dim3(256), 0, stream, reinterpret_cast<const float *>(dots), parts, g, place_dev,
                       dweight_dev);
         if (hipGetLastError() != hipSuccess) return DN_ERR_DEVICE;
@@ -347,8 +369,12 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
         a.f.y = dx;
         a.f.ldy = b.ldz;
         a.f.f32_out = 1;
-        if (launch_experts(d->type, P_DELTA, E_STORE, b.dx, a, tiles(b.dx), stream) != hipSuccess) return DN_ERR_DEVICE;
-        if (launch_join(d->type, {reinterpret_cast<const float *>(dx), nullptr, dX_dev, b.ldz, 0, d->d, nullptr, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs}, stream) != hipSuccess)
+        a.split = b.dx.parts;
+        a.group.c_stride = b.pairs * b.ldz * (int64_t)sizeof(float);
+        if (launch_experts(d->type, P_DELTA, E_STORE, b.dx.kernel, a, tiles(b.dx), stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_join(d->type, {reinterpret_cast<const float *>(dx), nullptr, dX_dev, b.ldz, 0, d->d, nullptr, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs, b.dx.parts,
+                                  b.pairs * b.ldz},
+                        stream) != hipSuccess)
             return DN_ERR_DEVICE;
     }
     const bool f32_out = d->grad_type == DN_F32;
@@ -366,7 +392,7 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
         a.f.m_valid = d->f;
         a.f.f32_out = f32_out;
         a.f.alpha = d->grad_scale;
-        if (launch_experts(d->type, P_GRAD, E_STORE, b.dwgu, a, 0, stream, 1) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_experts(d->type, P_GRAD, E_STORE, b.dwgu.kernel, a, 0, stream, 1) != hipSuccess) return DN_ERR_DEVICE;
     }
     ProductArgs a = product(g, d->d, d->f, 0, 1, 0);
     operand_a(a, dY);
@@ -376,7 +402,7 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
     a.f.ldy = f;
     a.f.f32_out = f32_out;
     a.f.alpha = d->grad_scale;
-    return device(launch_experts(d->type, P_GRAD, E_STORE, b.dwd, a, 0, stream));
+    return device(launch_experts(d->type, P_GRAD, E_STORE, b.dwd.kernel, a, 0, stream));
 }
 
 }  // extern "C"

@@ -10,11 +10,16 @@ namespace {
 template <class T, int P, int EPI, int GROUP, class S>
 hipError_t expert_tiles(ProductArgs &a, int64_t tiles, hipStream_t s)
 {
+    int parts = a.split;
+    const int all = (a.K + 128 / (int)sizeof(T) - 1) / (128 / (int)sizeof(T)) * a.segments;
+    a.steps = (all + parts - 1) / parts;
+    if (S::TM == 8) a.steps = (a.steps + 1) / 2 * 2;   // (its loop takes two at a time)
+    a.split = 1;
     const int cols = EPI == E_GATED ? S::BN / 2 : S::BN;
     a.tiles_n = (a.N + cols - 1) / cols;
     constexpr bool TERMS = GROUP == G_TERMS_A || GROUP == G_TERMS_B;
     a.tiles_m = TERMS ? (a.M + S::BM - 1) / S::BM : (int32_t)tiles;
-    launch_kernel(product_kernel<T, P, EPI, S, false, GROUP>, dim3((unsigned)a.tiles_m * (unsigned)a.tiles_n, TERMS ? (unsigned)a.group.experts : 1u),
+    launch_kernel(product_kernel<T, P, EPI, S, false, GROUP>, dim3((unsigned)a.tiles_m * (unsigned)a.tiles_n, TERMS ? (unsigned)a.group.experts : (unsigned)parts),
                   dim3(S::NW * 64), 0, s, a);
     return hipGetLastError();
 }
@@ -40,8 +45,6 @@ hipError_t expert_few(const ProductArgs &a, int64_t tiles, hipStream_t s)
 template <class T, int P, int EPI, int GROUP>
 hipError_t expert_run(ProductKernel kernel, ProductArgs &a, int64_t tiles, hipStream_t s)
 {
-    a.steps = (a.K + 128 / (int)sizeof(T) - 1) / (128 / (int)sizeof(T)) * a.segments;
-    a.split = 1;
     if constexpr (P == P_FWD)
         if (kernel == K_FEW) return expert_few<T, EPI, GROUP>(a, tiles, s);
     if (kernel == K_SMALL) return expert_tiles<T, P, EPI, GROUP, Small>(a, tiles, s);

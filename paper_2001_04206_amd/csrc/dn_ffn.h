@@ -223,7 +223,7 @@ struct Finish {
 struct Group {
     const int32_t *starts = nullptr, *order = nullptr;   // an expert's first pair, [experts + 1]; the pair at a place
     int32_t experts = 0, k = 1, pairs = 0, rows = 0;     // k: pairs of a row
-    int64_t b_stride = 0, c_stride = 0;                  // bytes between two experts' matrices; their results (P_GRAD)
+    int64_t b_stride = 0, c_stride = 0;                  // bytes between two experts' matrices; between their results (P_GRAD), those of parts of k
 };
 
 __device__ __forceinline__ int bounded(const Group &g, int e) { return min(max(g.starts[e], 0), g.pairs); }

@@ -512,13 +512,14 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             m0 = t.first;
             mine.M = t.end;
             b_on = t.expert * g.b_stride;
+            if (EPI == E_STORE) mine.f.y = static_cast<char *>(arg.f.y) + blockIdx.y * g.c_stride;   // a part of k has a result of its own
         }
     } else {
         tile_of(blockIdx.x, arg.tiles_m, arg.tiles_n, tm, tn);
         m0 = tm * S::BM;
     }
     const ProductArgs &a = GROUP != G_NONE ? mine : arg;
-    const int part_of_k = GROUP != G_NONE ? 0 : blockIdx.y;
+    const int part_of_k = TERMS ? 0 : blockIdx.y;
     typedef Operand<T, S::BM, S::NW, P == P_GRAD, false, GATHER || GROUP == G_TERMS_A> OpA;
     typedef Operand<T, S::BN, S::NW, P != P_FWD, PAIR, GROUP == G_TERMS_B> OpB;
     constexpr int COLS = PAIR ? S::BN / 2 : S::BN;
