@@ -76,7 +76,7 @@ hipError_t run(const MaskArgs *a, const PackArgs &p, hipStream_t s)
         return hipGetLastError();
     }
     if (masks) launch_kernel(mask_kernel<T>, dim3(masks), dim3(256), 0, s, *a, eights);
-    // four matrices together may take more threads than a launch can have
+    // the matrices together may take more threads than a launch can have
     constexpr unsigned most = 1u << 23;
     for (unsigned first = 0; first < packs; first += most)
         launch_kernel(pack_kernel<T>, dim3(packs - first < most ? packs - first : most), dim3(256), 0, s, p, first);

@@ -5,7 +5,8 @@
 
 namespace dn {
 
-// The experts' products, one source per type: E_GATED of gathered rows, E_STORE forward (Wd), E_DEXPERT, E_STORE backward (dX; two
+// The experts' products, one source per type: E_GATED of gathered rows, E_STORE or E_PAIR
+// forward (Wd), E_DEXPERT, E_STORE or E_PAIR backward (dX; two
 // segments) and E_STORE of an expert's terms (P_GRAD; operand `gathered`, 0 or 1, has rows of X or dY).  `tiles`: most tiles of rows that the lists can give (K_FEW: of sixteen).
 hipError_t launch_experts_f32(Product p, Epilogue e, ProductKernel kernel, int gathered, ProductArgs a, int64_t tiles, hipStream_t s);
 hipError_t launch_experts_f16(Product p, Epilogue e, ProductKernel kernel, int gathered, ProductArgs a, int64_t tiles, hipStream_t s);

@@ -11,18 +11,11 @@ constexpr int64_t kMostRows = (int64_t)1 << 26, kMostPairs = (int64_t)1 << 24, k
 
 // ---- rows ------------------------------------------------------------------------------------------------------------
 
-// The pairs' weights in the experts' order.
-__global__ __launch_bounds__(256) void sort_weights_kernel(const Group g, const float *weight, float *sorted)
-{
-    const int p = blockIdx.x * 256 + threadIdx.x;
-    if (p < min(g.starts[g.experts], g.pairs)) sorted[p] = weight[min((uint32_t)max(g.order[p], 0), (uint32_t)g.pairs - 1)];
-}
-
-// Y_t = R_t + the sum over its pairs of (weight) z, in the order of the choices.  A thread: eight columns of a row.  z is fp32, so that what is
-// added is rounded once, as a sum: in 16 bits each z would be rounded by itself, and results without a residual be off by 0.0029 where
-// they are by 0.0024 (bf16; of which H has a rounding, and the result).
+// Y_t = R_t + the sum over its pairs of (weight) z, in the order of the choices.  A thread: eight columns of a row.  z is fp32, or for results of
+// 16 bits (and k in one part) in 24, so that what is rounded is the sum: with z in 16 bits each would be rounded by itself, and results
+// without a residual be off by 0.0029 where they are by 0.0024 (bf16; of which H has a rounding, and the result).
 struct JoinArgs {
-    const float *z;
+    const void *z, *low;       // low: the low bytes of 24 bits, NULL: fp32
     const void *r;
     void *y;
     int64_t ldz, ldr, ldy;
@@ -31,7 +24,7 @@ struct JoinArgs {
     int32_t rows, cols, k, pairs, parts;
     int64_t plane;             // elements between two parts of z
 };
-template <class T>
+template <class T, bool SHORT>
 __global__ __launch_bounds__(256) void join_pairs_kernel(const JoinArgs a)
 {
     const uint32_t eights = ((uint32_t)a.cols + 7) / 8;
@@ -49,6 +42,13 @@ __global__ __launch_bounds__(256) void join_pairs_kernel(const JoinArgs a)
             const int j = min(j0 + q, a.k - 1), p = a.place[t * a.k + j];
             const bool has = j0 + q < a.k && (uint32_t)p < (uint32_t)a.pairs;
             w[q] = !has ? 0.f : a.weight ? a.weight[t * a.k + j] : 1.f;
+            if constexpr (SHORT) {
+                load24(z[q], a.z, a.low, has ? p * a.ldz + n : n);   // (any pair's row: its weight is 0)
+                if (!has)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[q][i] = 0.f;
+                continue;
+            }
             load8<float>(z[q], a.z, has ? p * a.ldz + n : 0, has ? left : 0);
             for (int s = 1; s < a.parts; ++s) {
                 float more[8];
@@ -83,7 +83,8 @@ template <class T>
 hipError_t join_as(const JoinArgs &a, hipStream_t s)
 {
     const uint64_t threads = (uint64_t)a.rows * (((uint32_t)a.cols + 7) / 8);
-    launch_kernel(join_pairs_kernel<T>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+    if (a.low) launch_kernel(join_pairs_kernel<T, true>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+    else launch_kernel(join_pairs_kernel<T, false>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 hipError_t launch_join(int type, const JoinArgs &a, hipStream_t s)
@@ -159,11 +160,12 @@ struct Block {
     dn_experts_desc d;
     int64_t pairs, ldh, ldz;     // between rows of H, of z
     Plan up, down, dh, dx, dwgu, dwd;
+    bool short_z, short_dx;      // pairs' results in 24 bits
     bool few;                    // the last product forms the sums over choices itself
     bool pack_w;                 // the matrices are copied to 16-byte rows
     int parts;                   // of the weights' derivatives
     size_t h, z, x, w1, w2, fwd_bytes;                        // bytes of H, z, X, Wg (and Wu), Wd; workspace
-    size_t sorted, dots, dgu, dx_parts, bwd_bytes;            // the pairs' dX
+    size_t dots, dgu, dx_parts, bwd_bytes;            // the pairs' dX
 };
 
 dn_status block_of(const dn_experts_desc *d, Block &b)
@@ -191,6 +193,8 @@ dn_status block_of(const dn_experts_desc *d, Block &b)
     b.dx = plan_experts(d->type, P_DELTA, E_STORE, b.pairs, d->experts, d->d, d->f, 2);
     b.dwgu = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->d, (int)(2 * b.ldh), 1);
     b.dwd = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->f, d->d, 1);
+    b.short_z = e == 2 && b.down.parts == 1 && b.down.kernel != K_FEW;
+    b.short_dx = e == 2 && b.dx.parts == 1;
     b.few = b.down.kernel == K_FEW && d->rows <= kFewTokens;
     b.pack_w = d->d * e % 16 || d->f * e % 16;
     const size_t wgu = b.pack_w ? packed_bytes(d->type, n * d->f, d->d) : 0, wd = b.pack_w ? packed_bytes(d->type, n * d->d, d->f) : 0;
@@ -202,10 +206,9 @@ dn_status block_of(const dn_experts_desc *d, Block &b)
     b.w2 = wd;
     b.fwd_bytes = b.h + b.z + (b.up.kernel == K_FEW ? 0 : b.x + 2 * wgu) + (b.down.kernel == K_FEW ? 0 : wd);
     b.parts = (int)((d->f + 255) / 256 * 4);   // of 64 columns, whole tiles
-    b.sorted = up256((size_t)b.pairs * sizeof(float));
     b.dots = up256((size_t)b.pairs * b.parts * sizeof(float));
     b.dgu = up256((size_t)(b.pairs * 2 * b.ldh * e));
-    b.bwd_bytes = b.sorted + b.dots + b.h + b.dgu + b.dx_parts + 2 * b.x + 2 * wgu + wd;
+    b.bwd_bytes = b.dots + b.h + b.dgu + b.dx_parts + 2 * b.x + 2 * wgu + wd;
     return DN_OK;
 }
 
@@ -297,10 +300,12 @@ dn_status dn_experts_forward(const dn_experts_desc *d, const void *X_dev, const 
     c.f.y = z;
     c.f.ldy = b.ldz;
     c.f.f32_out = 1;
+    char *low = b.short_z ? z + (size_t)(b.pairs * b.ldz) * 2 : nullptr;
+    c.f.y2 = low;
     c.split = b.down.parts;
     c.group.c_stride = b.pairs * b.ldz * (int64_t)sizeof(float);
-    if (launch_experts(d->type, P_FWD, E_STORE, b.down.kernel, c, tiles(b.down), stream) != hipSuccess) return DN_ERR_DEVICE;
-    return device(launch_join(d->type, {reinterpret_cast<const float *>(z), R_dev, Y_dev, b.ldz, b.d.ldr, b.d.ldy, weight_dev, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs, b.down.parts, b.pairs * b.ldz}, stream));
+    if (launch_experts(d->type, P_FWD, low ? E_PAIR : E_STORE, b.down.kernel, c, tiles(b.down), stream) != hipSuccess) return DN_ERR_DEVICE;
+    return device(launch_join(d->type, {z, low, R_dev, Y_dev, b.ldz, b.d.ldr, b.d.ldy, weight_dev, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs, b.down.parts, b.pairs * b.ldz}, stream));
 }
 
 dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const void *Wg_dev, const void *Wu_dev, const void *Wd_dev,
@@ -321,19 +326,15 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
     if ((s = workspace(b.bwd_bytes, workspace_dev, workspace_bytes)) != DN_OK) return s;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const int64_t e = size_of(d->type), n = d->experts, f = d->f;
-    char *sorted = static_cast<char *>(workspace_dev), *dots = sorted + b.sorted, *H = dots + b.dots;
+    char *dots = static_cast<char *>(workspace_dev), *H = dots + b.dots;
     char *dG = H + b.h, *dU = dG + b.ldh * e, *dx = dG + b.dgu;
     const Group g{starts_dev, order_dev, d->experts, d->k, (int32_t)b.pairs, d->rows, 0, 0};
     Packer pack{d->type, dx + b.dx_parts};
     const Packer::Rows X = pack.take(X_dev, b.d.ldx, d->rows, d->d), dY = pack.take(dY_dev, b.d.ldy, d->rows, d->d);
-    if (b.pack_w && pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;   // (four matrices a launch)
-    if (b.pack_w) pack.a = {};
     const Packer::Rows Wd = pack.take(Wd_dev, f, n * d->d, f, b.pack_w);
     const Packer::Rows Wg = dX_dev ? pack.take(Wg_dev, d->d, n * f, d->d, b.pack_w) : Packer::Rows{};
     const Packer::Rows Wu = dX_dev ? pack.take(Wu_dev, d->d, n * f, d->d, b.pack_w) : Packer::Rows{};
     if (pack.run(stream) != hipSuccess) return DN_ERR_DEVICE;
-    launch_kernel(sort_weights_kernel, dim3((unsigned)((b.pairs + 255) / 256)), dim3(256), 0, stream, g, weight_dev, reinterpret_cast<float *>(sorted));
-    if (hipGetLastError() != hipSuccess) return DN_ERR_DEVICE;
     auto tiles = [&](const Plan &p) { return most_tiles(b.pairs, d->experts, rows_of_tile(p.kernel)); };
     {   // dh, and from it dG, dU, w H and the weights' derivatives
         ProductArgs a = product(g, 0, d->f, d->d, 1, Wd.ld * d->d);
@@ -349,7 +350,9 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
         a.f.ldr = 2 * f;
         a.f.half = f;
         a.f.act = d->act;
-        a.f.row_scale = reinterpret_cast<const float *>(sorted);
+        a.f.weight = weight_dev;
+        a.f.order = order_dev;
+        a.f.pairs = (uint32_t)b.pairs;
         a.f.dots = reinterpret_cast<float *>(dots);
         a.f.dots_ld = b.pairs;
         if (launch_experts(d->type, P_DELTA, E_DEXPERT, b.dh.kernel, a, tiles(b.dh), stream) != hipSuccess) return DN_ERR_DEVICE;
@@ -369,10 +372,12 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
         a.f.y = dx;
         a.f.ldy = b.ldz;
         a.f.f32_out = 1;
+        char *low = b.short_dx ? dx + (size_t)(b.pairs * b.ldz) * 2 : nullptr;
+        a.f.y2 = low;
         a.split = b.dx.parts;
         a.group.c_stride = b.pairs * b.ldz * (int64_t)sizeof(float);
-        if (launch_experts(d->type, P_DELTA, E_STORE, b.dx.kernel, a, tiles(b.dx), stream) != hipSuccess) return DN_ERR_DEVICE;
-        if (launch_join(d->type, {reinterpret_cast<const float *>(dx), nullptr, dX_dev, b.ldz, 0, d->d, nullptr, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs, b.dx.parts,
+        if (launch_experts(d->type, P_DELTA, low ? E_PAIR : E_STORE, b.dx.kernel, a, tiles(b.dx), stream) != hipSuccess) return DN_ERR_DEVICE;
+        if (launch_join(d->type, {dx, low, nullptr, dX_dev, b.ldz, 0, d->d, nullptr, place_dev, d->rows, d->d, d->k, (int32_t)b.pairs, b.dx.parts,
                                   b.pairs * b.ldz},
                         stream) != hipSuccess)
             return DN_ERR_DEVICE;

@@ -73,6 +73,10 @@ template <class T>
 hipError_t launch_experts(Product p, Epilogue e, ProductKernel kernel, int gathered, ProductArgs &a, int64_t tiles, hipStream_t s)
 {
     if (p == P_FWD && e == E_GATED) return expert_run<T, P_FWD, E_GATED, G_TOKENS>(kernel, a, tiles, s);
+    if constexpr (sizeof(T) == 2) {
+        if (p == P_FWD && e == E_PAIR) return expert_run<T, P_FWD, E_PAIR, G_ROWS>(kernel, a, tiles, s);
+        if (p == P_DELTA && e == E_PAIR) return expert_run<T, P_DELTA, E_PAIR, G_ROWS>(kernel, a, tiles, s);
+    }
     if (p == P_FWD && e == E_STORE) return expert_run<T, P_FWD, E_STORE, G_ROWS>(kernel, a, tiles, s);
     if (p == P_DELTA && e == E_DEXPERT) return expert_run<T, P_DELTA, E_DEXPERT, G_TOKENS>(kernel, a, tiles, s);
     if (p == P_DELTA && e == E_STORE) return expert_run<T, P_DELTA, E_STORE, G_ROWS>(kernel, a, tiles, s);

@@ -50,6 +50,40 @@ __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8],
     }
 }
 
+// fp32 numbers in 24 bits, the upper 16 and the next 8 apart: rounded to 16 significant bits, which is 2^-17 of a number.  For what is
+// added up and then rounded to 16 bits: a third less to write and read.
+__device__ __forceinline__ uint32_t upper24(float v)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    return v == v ? u + 0x80 : u & 0xffffff00u | 0x400000u;   // (a carry of NaN's would make a number of it)
+}
+template <bool ALL>
+__device__ __forceinline__ void store24(void *high, void *low, int64_t at, const float (&v)[8], int left)
+{
+    typedef uint16_t v8s __attribute__((ext_vector_type(8), aligned(16)));
+    typedef uint8_t v8b __attribute__((ext_vector_type(8), aligned(8)));
+    v8s h;
+    v8b l;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t u = ALL || j < left ? upper24(v[j]) : 0;
+        h[j] = (uint16_t)(u >> 16);
+        l[j] = (uint8_t)(u >> 8);
+    }
+    // rows are padded to multiples of eight
+    __builtin_nontemporal_store(h, reinterpret_cast<v8s *>(static_cast<uint16_t *>(high) + at));
+    __builtin_nontemporal_store(l, reinterpret_cast<v8b *>(static_cast<uint8_t *>(low) + at));
+}
+__device__ __forceinline__ void load24(float (&v)[8], const void *high, const void *low, int64_t at)
+{
+    typedef uint16_t v8s __attribute__((ext_vector_type(8), aligned(16)));
+    typedef uint8_t v8b __attribute__((ext_vector_type(8), aligned(8)));
+    const v8s h = *reinterpret_cast<const v8s *>(static_cast<const uint16_t *>(high) + at);
+    const v8b l = *reinterpret_cast<const v8b *>(static_cast<const uint8_t *>(low) + at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __builtin_bit_cast(float, (uint32_t)h[j] << 16 | (uint32_t)l[j] << 8);
+}
+
 // ---- dropout --------------------------------------------------------------------------------------------------
 // Philox 4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): ten rounds of two
 // 32 x 32 -> 64 bit products over a 128-bit counter.  One call gives the eight 16-bit numbers of eight neighbouring columns
@@ -194,13 +228,14 @@ enum Epilogue : int {
     E_GATED = 1,   // P_FWD of two matrices B: f(g) u; g and u too
     E_DGATED = 2,  // P_DELTA: d(f(g) u) from its derivative: dG, dU, and f(g) u again
     E_STORE = 3,   // alpha times the sum, as T or as fp32
-    E_DEXPERT = 4  // as E_DGATED, each row times its weight; and the weight's derivative
+    E_DEXPERT = 4, // as E_DGATED, each row times its weight; and the weight's derivative
+    E_PAIR = 5     // the sum, in 24 bits
 };
 
 struct Finish {
     void *y = nullptr;          // result [M][ldy]; E_DGATED: dG [M][ldy] with dU `half_y` columns further on
     int64_t ldy = 0;
-    void *y2 = nullptr;         // E_LINEAR: net inputs; E_GATED: G and U; E_DGATED: f(g) u; E_STORE: rows from m_split on
+    void *y2 = nullptr;         // E_LINEAR: net inputs; E_GATED: G and U; E_DGATED: f(g) u; E_STORE: rows from m_split on; E_PAIR: low bytes
     int64_t ldy2 = 0;
     const void *r = nullptr;    // E_LINEAR: residual; E_DGATED: G and U
     int64_t ldr = 0;
@@ -213,7 +248,9 @@ struct Finish {
     int32_t act = 0;
     int32_t f32_out = 0;        // E_STORE: results are fp32 whatever T is
     float alpha = 1.f;
-    const float *row_scale = nullptr;   // E_DEXPERT: a row's weight
+    const float *weight = nullptr;      // E_DEXPERT: of row m, weight[order[m]] of `pairs`
+    const int32_t *order = nullptr;
+    uint32_t pairs = 1;
     float *dots = nullptr;              // E_DEXPERT: parts of the weights' derivatives, [64 columns each][rows], rows dots_ld apart
     int64_t dots_ld = 0;
     Dropout drop;
@@ -274,7 +311,7 @@ struct MaskArgs {
 
 // Matrices whose rows do not lie at multiples of 16 bytes, or end between two, copied to where they do, zeros following.
 struct PackArgs {
-    struct { const void *x; void *y; int64_t ldx; int32_t rows, cols; int64_t first; } m[4];   // first: its first group of eight
+    struct { const void *x; void *y; int64_t ldx; int32_t rows, cols; int64_t first; } m[5];   // first: its first group of eight
     int32_t n;
     int64_t groups;
 };

@@ -99,7 +99,7 @@ struct Beside {
             r = get8<T, ALL>(e.r, m * e.ldr + n, left);
             u = get8<T, ALL>(e.r, m * e.ldr + n + e.half, left);
         }
-        if (EPI == E_DEXPERT) by = e.row_scale[m];
+        if (EPI == E_DEXPERT) by = e.weight[min((uint32_t)max(e.order[m], 0), e.pairs - 1)];
     }
 };
 
@@ -181,6 +181,8 @@ __device__ __forceinline__ void finish8(const Finish &e, const Beside<T, EPI> &s
         store8<T, ALL, ALL>(e.y, m * e.ldy + n + e.half_y, w, left + e.zeros);
         store8<T, ALL, ALL>(e.y2, m * e.ldy2 + n, h, left + e.zeros);
         w[0] = dot;
+    } else if constexpr (EPI == E_PAIR) {
+        store24<ALL>(e.y, e.y2, m * e.ldy + n, v, left);
     } else {
         const int row = m < e.m_split ? m : m - e.m_split;
         if (row >= e.m_valid) return;
@@ -484,7 +486,7 @@ __device__ __forceinline__ GroupTile tile_in_group(const Group &g, const GroupTi
 template <class T, int P, int EPI, class S, bool SUMS, int GROUP = G_NONE>
 __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArgs arg)
 {
-    constexpr bool PAIR = EPI == E_GATED, GATHER = GROUP == G_TOKENS, TERMS = GROUP == G_TERMS_A || GROUP == G_TERMS_B;
+    constexpr bool PAIR = EPI == E_GATED, GATHER = GROUP == G_TOKENS, IDLE = GROUP == G_ROWS || GROUP == G_TOKENS, TERMS = GROUP == G_TERMS_A || GROUP == G_TERMS_B;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int tm, tn, m0;
     ProductArgs mine;   // this expert's product; its operands lie so many bytes on
@@ -512,7 +514,7 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             m0 = t.first;
             mine.M = t.end;
             b_on = t.expert * g.b_stride;
-            if (EPI == E_STORE) mine.f.y = static_cast<char *>(arg.f.y) + blockIdx.y * g.c_stride;   // a part of k has a result of its own
+            if (EPI == E_STORE || EPI == E_PAIR) mine.f.y = static_cast<char *>(arg.f.y) + blockIdx.y * g.c_stride;   // a part of k has a result of its own
         }
     } else {
         tile_of(blockIdx.x, arg.tiles_m, arg.tiles_n, tm, tn);
@@ -616,6 +618,33 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
             __syncthreads();
             t0 = terms / OpA::BK;
             t1 = t0 + (now + OpA::BK - 1) / OpA::BK;
+        }
+        if (IDLE && m0 + wm * S::TM * 16 >= a.M) {   // a wave that has no rows loads its share of the stages, and takes no other part
+            constexpr int LATE = (S::NB - 1) * LOADS;
+            prepare(t0);
+            fetch(stage0);
+            prepare(t0 + 1);
+            fetch(stage1);
+            if (S::NB == 3) {
+                prepare(t0 + 2);
+                fetch(stage2);
+            }
+            arrived<LATE>();
+            auto pass = [&](char *cur, int t) {
+                prepare(t + S::NB);
+                arrived<(S::NB - 2) * LOADS>();
+                fetch(cur);
+            };
+            int t = t0;
+            for (; t + (S::TM == 8 ? 0 : S::NB - 1) < t1; t += S::NB) {
+                pass(stage0, t);
+                pass(stage1, t + 1);
+                if (S::NB == 3) pass(stage2, t + 2);
+            }
+            if (S::TM != 8 && t < t1) pass(stage0, t);
+            if (S::NB == 3 && t + 1 < t1) pass(stage1, t + 1);
+            arrived<0>();
+            return;
         }
         prepare(t0);
         fetch(stage0);
