@@ -52,7 +52,8 @@ hipError_t expert_run(ProductKernel kernel, ProductArgs &a, int64_t tiles, hipSt
         if (kernel == K_TINY) return expert_tiles<T, P, EPI, GROUP, Tiny>(a, tiles, s);
     } else {
         if (kernel == K_MEDIUM) return expert_tiles<T, P, EPI, GROUP, Medium>(a, tiles, s);
-        if (kernel == K_LARGE) return expert_tiles<T, P, EPI, GROUP, Large>(a, tiles, s);
+        if constexpr (EPI != E_DEXPERT)   // (never planned)
+            if (kernel == K_LARGE) return expert_tiles<T, P, EPI, GROUP, Large>(a, tiles, s);
     }
     return hipErrorInvalidValue;
 }
