@@ -62,6 +62,21 @@ __device__ __forceinline__ double total(double v)
     return last_lane(v);
 }
 
+// a lane's logits, -inf behind the last
+template <class T, int V> struct Several { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
+template <class T, int V>
+__device__ __forceinline__ void load_logits(float (&l)[V], const T *p, int first, int experts)
+{
+    if (first + V <= experts) {
+        const auto x = *reinterpret_cast<const typename Several<T, V>::type *>(p + first);
+#pragma unroll
+        for (int i = 0; i < V; ++i) l[i] = (float)x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) l[i] = first + i < experts ? (float)p[first + i] : -INFINITY;
+    }
+}
+
 // 1 / x of an x from 1 on: the hardware's estimate and two Newton steps; 0 of infinity, NaN of NaN
 __device__ __forceinline__ double inverse64(double x)
 {
@@ -130,11 +145,9 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
     const T *p = static_cast<const T *>(a.l) + row * a.ldl;
     float l[V], high = -INFINITY;
     Rank c[V];
+    load_logits<T, V>(l, p, first, a.experts);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        l[i] = first + i < a.experts ? (float)p[first + i] : -INFINITY;
-        high = fmaxf(high, l[i]);
-    }
+    for (int i = 0; i < V; ++i) high = fmaxf(high, l[i]);
     float m = -INFINITY, sum = 1.f;
     if (a.score == DN_SCORE_SOFTMAX) m = wave_max(high);
     if constexpr (WIDE) {
@@ -148,7 +161,7 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
             s = total(s);
             sum = (float)s;
 #pragma unroll
-            for (int i = 0; i < V; ++i) c[i] /= s;
+            for (int i = 0; i < V; ++i) c[i] *= inverse64(s);
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) c[i] = inverse64(1. + exp(-(double)l[i]));
@@ -233,44 +246,51 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
     }
     int chosen = -1;
     float logit = -INFINITY;   // lane j: of choice j
-    Rank b = ninf;
+    // Ranks in 32 bits: rounding keeps their order, so one that is alone the highest there is the highest; only equals are told apart in 64.
+    float c32[V], b = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < V; ++i) b = c[i] > b ? c[i] : b;
+    for (int i = 0; i < V; ++i) {
+        c32[i] = (float)c[i];
+        b = fmaxf(b, c32[i]);
+    }
     for (int j = 0; j < a.k; ++j) {
-        // Rounding keeps the order: a lane that alone has the highest of the ranks rounded to 32 bits has the highest.
-        const float top = wave_max((float)b);
-        if (!(top > -INFINITY)) break;
-        uint64_t have = __ballot((float)b == top);
-        Rank best;
-        if constexpr (WIDE) {
-            if (have & (have - 1)) {   // (every lane takes part)
-                const Rank of_those = highest((float)b == top ? b : ninf);
-                have = __ballot(b == of_those);
-            }
-            best = b;   // (of the lane that has it)
-        } else {
-            best = top;
-        }
-        const int f = __builtin_ctzll(have);
-        int at = 0;
+        const float best = wave_max(b);
+        if (!(best > -INFINITY)) break;
+        int at = 0, equal = 0;
         float mine = l[0];
 #pragma unroll
         for (int i = V - 1; i >= 0; --i)
-            if (c[i] == best) {
+            if (c32[i] == best) {
                 at = i;
                 mine = l[i];
+                ++equal;
             }
-        const int e = f * V + __builtin_amdgcn_readlane(at, f);
+        uint64_t have = __ballot(equal > 0);
+        if constexpr (WIDE) {
+            if (have & (have - 1) || __ballot(equal > 1)) {   // (every lane takes part)
+                Rank r = ninf;
+#pragma unroll
+                for (int i = V - 1; i >= 0; --i)
+                    if (c32[i] == best && c[i] >= r) {
+                        r = c[i];
+                        at = i;
+                        mine = l[i];
+                    }
+                const Rank top = highest(r);
+                have = __ballot(equal > 0 && r == top);
+            }
+        }
+        const int f = __builtin_ctzll(have), e = f * V + __builtin_amdgcn_readlane(at, f);
         const float le = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), f));
         if (lane == j) {
             chosen = e;
             logit = le;
         }
-        b = ninf;
+        b = -INFINITY;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (first + i == e) c[i] = ninf;
-            b = c[i] > b ? c[i] : b;
+            if (first + i == e) c32[i] = -INFINITY;
+            b = fmaxf(b, c32[i]);
         }
     }
     float w = weight_of(a, logit, chosen >= 0, m, sum);
@@ -304,11 +324,9 @@ __global__ __launch_bounds__(kWaves * 64) void route_back_kernel(const RouteArgs
     float s[V], m = 0.f, sum = 1.f, d;
     if (dense) {
         float high = -INFINITY, t = 0.f;
+        load_logits<T, V>(s, p, first, a.experts);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            s[i] = first + i < a.experts ? (float)p[first + i] : -INFINITY;
-            high = fmaxf(high, s[i]);
-        }
+        for (int i = 0; i < V; ++i) high = fmaxf(high, s[i]);
         m = wave_max(high);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -344,9 +362,16 @@ __global__ __launch_bounds__(kWaves * 64) void route_back_kernel(const RouteArgs
         for (int i = 0; i < V; ++i) v[i] = s[i] * (v[i] - dot);
     }
     T *q = static_cast<T *>(a.dl) + (int64_t)row * a.experts + first;
+    if (first + V <= a.experts) {
+        typename Several<T, V>::type x;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (first + i < a.experts) q[i] = (T)v[i];
+        for (int i = 0; i < V; ++i) x[i] = (T)v[i];
+        *reinterpret_cast<typename Several<T, V>::type *>(q) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (first + i < a.experts) q[i] = (T)v[i];
+    }
 }
 
 // ---- lists -----------------------------------------------------------------------------------------------------------
@@ -383,7 +408,14 @@ __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
     for (int w = 0; w < 4; ++w)
         for (int e = threadIdx.x; e < a.experts; e += 256) next[w][e] = 0;
     __syncthreads();
-    for (int i = from + lane; i < to; i += 64) {
+    // the first 256 pairs of the wave stay in registers: all of them, but in chunks of very many pairs
+    int mine_of[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) mine_of[q] = from + q * 64 + lane < to ? a.expert[from + q * 64 + lane] : -1;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if ((uint32_t)mine_of[q] < (uint32_t)a.experts) atomicAdd(&next[wave][mine_of[q]], 1);
+    for (int i = from + 256 + lane; i < to; i += 64) {
         const int e = a.expert[i];
         if ((uint32_t)e < (uint32_t)a.experts) atomicAdd(&next[wave][e], 1);
     }
@@ -400,12 +432,12 @@ __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
             }
             if (a.chunks == 1) sum = own;
             else
-                for (int b0 = 0; b0 < a.chunks; b0 += 16) {   // sixteen loads under way
-                    int n[16];
+                for (int b0 = 0; b0 < a.chunks; b0 += 32) {   // loads under way
+                    int n[32];
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) n[q] = a.counts[min(b0 + q, a.chunks - 1) * a.experts + e];
+                    for (int q = 0; q < 32; ++q) n[q] = a.counts[min(b0 + q, a.chunks - 1) * a.experts + e];
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) {
+                    for (int q = 0; q < 32; ++q) {
                         before += b0 + q < block ? n[q] : 0;
                         sum += b0 + q < a.chunks ? n[q] : 0;
                     }
@@ -449,9 +481,8 @@ __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
     if (block == 0 && threadIdx.x == 0) a.starts[a.experts] = total;
     __syncthreads();
     // sixty-four pairs at a time: a pair's place is its expert's next one and how many lanes below have the same expert
-    for (int i = from; i < to; i += 64) {
+    auto put = [&](int i, int e) {
         const int q = i + lane;
-        const int e = q < to ? a.expert[q] : -1;
         const bool has = (uint32_t)e < (uint32_t)a.experts;
         uint64_t same = __ballot(has);
 #pragma unroll
@@ -474,7 +505,11 @@ __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-    }
+    };
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (from + q * 64 < to) put(from + q * 64, mine_of[q]);
+    for (int i = from + 256; i < to; i += 64) put(i, i + lane < to ? a.expert[i + lane] : -1);
     for (int p = max(from, total) + lane; p < to; p += 64) a.order[p] = -1;
 }
 
