@@ -739,24 +739,27 @@ def dn_clip(grads, max_norm: float, norm, outs=None, workspace=None):
     outs = grads if outs is None else outs
     if len(outs) != len(grads):
         raise TypeError("outs must be as many as grads")
-    spans = (Span * max(len(grads), 1))()
-    for i, (g, o) in enumerate(zip(grads, outs)):
-        kind = _type_of(g, "a gradient")
-        if g.get_device() != dev or not g.is_contiguous():
-            raise TypeError("gradients must be contiguous tensors on device %d" % dev)
-        s = spans[i]
-        s.grad_dev, s.count, s.type, s.out_type = g.data_ptr(), g.numel(), kind, kind
+    # the spans' 32 bytes as four words, the two types in the last: a tensor costs what asking it costs
+    words, kinds = [], _TYPES
+    for g, o in zip(grads, outs):
+        kind = kinds.get(g.dtype)
+        if kind is None or g.get_device() != dev or not g.is_contiguous():
+            raise TypeError("gradients must be contiguous tensors of float32, float16 or bfloat16 on device %d" % dev)
+        at, to, out_kind = g.data_ptr(), None, kind
         if o is g:
-            s.out_dev = s.grad_dev
+            to = at
         elif o is not None:
-            s.out_type = _type_of(o, "a result")
-            if o.get_device() != dev or not o.is_contiguous() or o.shape != g.shape:
+            out_kind = kinds.get(o.dtype)
+            if out_kind is None or o.get_device() != dev or not o.is_contiguous() or o.shape != g.shape:
                 raise TypeError("results must be contiguous tensors of their gradients' shapes on device %d" % dev)
-            s.out_dev = o.data_ptr()
+            to = o.data_ptr()
+        words += (at, to or 0, g.numel(), kind | out_kind << 32)
+    n_spans = len(grads)
+    spans = (C.c_int64 * max(len(words), 1))(*words)
     with _on(dev):
         at = C.addressof(spans)
-        _keep, ws, n = _workspace(l.dn_clip_workspace_bytes(at, len(grads)), workspace, norm)
-        _check(l.dn_clip(at, len(grads), max_norm, at_norm, ws, n, _stream(dev)), "dn_clip")
+        _keep, ws, n = _workspace(l.dn_clip_workspace_bytes(at, n_spans), workspace, norm)
+        _check(l.dn_clip(at, n_spans, max_norm, at_norm, ws, n, _stream(dev)), "dn_clip")
 
 
 class Net:
