@@ -110,7 +110,7 @@ int64_t most_tiles(int64_t pairs, int experts, int rows) { return pairs / rows +
 // product with the activation's derivative moves ten bytes an element beside it, and large tiles have no registers for that: 415 us on
 // medium ones at 8192 tokens, 442 on large ones.  Parts are for the products whose results the pairs' sums read: these add them too.
 struct Plan { ProductKernel kernel = K_SMALL; int parts = 1; };
-Plan plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, int N, int K, int segments)
+Plan plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, int N, int K, int segments, bool few_tokens = false)
 {
     const int planes = e == E_GATED ? 2 : 1, bk = type == DN_F32 ? 32 : 64;
     const double es = (double)size_of(type), met = (double)(pairs < experts ? pairs : experts);
@@ -125,6 +125,7 @@ Plan plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, i
     if (p == P_FWD && (int64_t)K * size_of(type) >= 32 && most_tiles(pairs, experts, 16) * ((N + 15) / 16) < 1 << 23) {   // 2^32 threads
         best = 6 + es * tiles_of(16) * planes * N * K / 5e6;
         plan.kernel = K_FEW;
+        if (few_tokens) return plan;
     }
     struct Way { ProductKernel kernel; int rows, cols, together; double stage, least, round, behind; };
     const Way tiny{K_TINY, 64, 128, 3, 0.9, 0.9, 3, 1}, large{K_LARGE, 256, 256, 1, 1.5, 1.5, 8, 4.6 / 3.8}, medium{K_MEDIUM, 128, 256, 1, 0.8, 0.8, 6, 1};
@@ -145,8 +146,8 @@ Plan plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, i
             const double deep = ceil(tiles * parts / 256), rounds = ceil(deep / w.together);
             const double stage = deep * w.stage > rounds * w.least ? deep * w.stage : rounds * w.least;
             double us = ceil(steps / parts) * stage + rounds * w.round;
-            if (us < weights * w.behind) us = weights * w.behind;
-            us += (parts - 1) * 8. * pairs * N / 4.5e6 + (packed ? 4 + 2 * es * experts * planes * N * K / 4.6e6 : 0);
+            if (us < weights * w.behind + 6) us = weights * w.behind + 6;
+            us += (parts > 1 ? 3 : 0) + (parts - 1) * 8. * pairs * N / 4.5e6 + (packed ? 4 + 2 * es * experts * planes * N * K / 4.6e6 : 0);
             if (us < best) {
                 best = us;
                 plan = {w.kernel, parts};
@@ -187,8 +188,8 @@ dn_status block_of(const dn_experts_desc *d, Block &b)
     if (too_many(b.pairs, d->d) || too_many(b.pairs, 2 * b.ldh) || too_many(n * d->f, d->d) || too_many(n * d->d, d->f)) return DN_ERR_SHAPE;
     const int64_t wide = b.d.ldx > b.ldz ? b.d.ldx : b.ldz, wider = b.d.ldy > wide ? b.d.ldy : wide;
     if (d->rows * wider * e > kMostBytes) return DN_ERR_SHAPE;
-    b.up = plan_experts(d->type, P_FWD, E_GATED, b.pairs, d->experts, d->f, d->d, 1);
-    b.down = plan_experts(d->type, P_FWD, E_STORE, b.pairs, d->experts, d->d, d->f, 1);
+    b.up = plan_experts(d->type, P_FWD, E_GATED, b.pairs, d->experts, d->f, d->d, 1, d->rows <= kFewTokens);
+    b.down = plan_experts(d->type, P_FWD, E_STORE, b.pairs, d->experts, d->d, d->f, 1, d->rows <= kFewTokens);
     b.dh = plan_experts(d->type, P_DELTA, E_DEXPERT, b.pairs, d->experts, d->f, d->d, 1);
     b.dx = plan_experts(d->type, P_DELTA, E_STORE, b.pairs, d->experts, d->d, d->f, 2);
     b.dwgu = plan_experts(d->type, P_GRAD, E_STORE, b.pairs, d->experts, d->d, (int)(2 * b.ldh), 1);
