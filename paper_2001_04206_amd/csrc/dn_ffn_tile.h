@@ -285,15 +285,16 @@ struct Operand {
         const char *from;
         int bytes;
         uint32_t first;   // offset of the lane's first chunk, past every resource if it is not to be read
-        uint32_t row[MC && GATHER ? Q : 1];   // bytes before the row of each chunk
     };
+    struct AimRows : Aim { uint32_t row[Q]; };   // bytes before the row of each chunk
+    typedef typename std::conditional<MC && GATHER, AimRows, Aim>::type Aimed;
     // GATHER, MC: the matrix has `total` rows; `in_lds` holds what lies before each term's row in bytes (2^31 for none)
     typedef const __attribute__((address_space(3))) uint32_t *Rows;
-    __device__ __forceinline__ Aim aim_rows(bool valid, int step, Rows in_lds, int total, int wave, int lane) const
+    __device__ __forceinline__ AimRows aim_rows(bool valid, int step, Rows in_lds, int total, int wave, int lane) const
     {
-        Aim a{base, valid ? (int)((int64_t)(total - 1) * ld + rows * (int)sizeof(T)) : 0, 0, {}};
+        AimRows a{{base, valid ? (int)((int64_t)(total - 1) * ld + rows * (int)sizeof(T)) : 0, 0}, {}};
 #pragma unroll
-        for (int q = 0; q < Q; ++q) a.row[MC && GATHER ? q : 0] = in_lds[step * BK + ((wave + q * NW) * 1024 + lane * 16) / RB];
+        for (int q = 0; q < Q; ++q) a.row[q] = in_lds[step * BK + ((wave + q * NW) * 1024 + lane * 16) / RB];
         return a;
     }
     __device__ __forceinline__ Aim aim(bool valid, bool second, int step, int K) const
@@ -302,20 +303,19 @@ struct Operand {
         const char *b = (second ? next : base) + (MC ? (int64_t)k0 * ld : (int64_t)k0 * (int)sizeof(T));
         const int64_t bytes = MC ? (int64_t)(min(kleft, BK) - 1) * ld + rows * (int)sizeof(T) : (int64_t)(rows - 1) * ld + kleft * (int)sizeof(T);
         const bool in = valid && (MC || (int)kbyte < kleft * (int)sizeof(T));
-        if (GATHER) return {b, valid ? (int)bytes : 0, in ? 0 : 0x80000000u, {}};
-        return {b, valid ? (int)bytes : 0, in ? off[0] : 0x80000000u, {}};
+        if (GATHER) return {b, valid ? (int)bytes : 0, in ? 0 : 0x80000000u};
+        return {b, valid ? (int)bytes : 0, in ? off[0] : 0x80000000u};
     }
-    __device__ __forceinline__ void fetch(lds_char *lds, const Aim &at, int wave) const
+    __device__ __forceinline__ void fetch(lds_char *lds, const Aimed &at, int wave) const
     {
         const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at.from), 0, at.bytes, 0x00020000);
 #pragma unroll
-        for (int q = 0; q < Q; ++q)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * PIECE), 16,
-                                                     (int)(GATHER && MC ? at.row[MC && GATHER ? q : 0] + off[HOP ? 0 : q]
-                                                           : HOP    ? at.first + q * hop
-                                                           : GATHER ? at.first + off[q]
-                                                                    : offset(q)),
-                                                     0, 0, 0);
+        for (int q = 0; q < Q; ++q) {
+            uint32_t from;
+            if constexpr (MC && GATHER) from = at.row[q] + off[HOP ? 0 : q];
+            else from = HOP ? at.first + q * hop : GATHER ? at.first + off[HOP ? 0 : q] : offset(q);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void *)(lds + (wave + q * NW) * PIECE), 16, (int)from, 0, 0, 0);
+        }
     }
 
     // Fragments: sixteen rows from 16 block on, half kk (64 bytes of k) of the stage.  `at` from start(), block a constant
@@ -592,8 +592,8 @@ __global__ __launch_bounds__(S::NW * 64, 2) void product_kernel(const ProductArg
     // fragments, which every row needs, come beforehand and into registers of their own.  The loads from memory have the time of
     // NB - 1 stages.
     Half f0, f1;
-    typename OpA::Aim aim_a;
-    typename OpB::Aim aim_b;
+    typename OpA::Aimed aim_a;
+    typename OpB::Aimed aim_b;
     int terms = 0;   // TERMS: the terms before those in rows_at
     auto prepare = [&](int t) {
         const bool second = !TERMS && t >= per_seg;
