@@ -384,6 +384,8 @@ struct ListArgs {
     int32_t pairs, experts, chunk, chunks;      // pairs of a chunk, a multiple of 1024
 };
 
+constexpr int kPlaceWaves = 16;
+
 __global__ __launch_bounds__(256) void count_kernel(const ListArgs a)
 {
     __shared__ int32_t count[kMostExperts];
@@ -399,19 +401,23 @@ __global__ __launch_bounds__(256) void count_kernel(const ListArgs a)
 }
 
 // one chunk: it counts itself
+template <int WAVES>
 __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
 {
-    __shared__ int32_t next[4][kMostExperts], all[kMostExperts], sums[4];
+    constexpr int THREADS = WAVES * 64, EACH = kMostExperts / THREADS;   // EACH: experts of a thread
+    __shared__ int32_t next[WAVES][kMostExperts], all[kMostExperts], earlier[kMostExperts], sums[WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int from = block * a.chunk + wave * (a.chunk / 4), to = min(from + a.chunk / 4, a.pairs);   // the wave's pairs
-    #pragma unroll
-    for (int w = 0; w < 4; ++w)
-        for (int e = threadIdx.x; e < a.experts; e += 256) next[w][e] = 0;
-    __syncthreads();
-    // the first 256 pairs of the wave stay in registers: all of them, but in chunks of very many pairs
+    const int from = block * a.chunk + wave * (a.chunk / WAVES), to = min(from + a.chunk / WAVES, a.pairs);   // the wave's pairs
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+        for (int e = threadIdx.x; e < a.experts; e += THREADS) next[w][e] = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) all[threadIdx.x + i * THREADS] = earlier[threadIdx.x + i * THREADS] = 0;
+    // the first 256 pairs of the wave stay in registers: most often all of them
     int mine_of[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) mine_of[q] = from + q * 64 + lane < to ? a.expert[from + q * 64 + lane] : -1;
+    __syncthreads();
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         if ((uint32_t)mine_of[q] < (uint32_t)a.experts) atomicAdd(&next[wave][mine_of[q]], 1);
@@ -419,41 +425,45 @@ __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
         const int e = a.expert[i];
         if ((uint32_t)e < (uint32_t)a.experts) atomicAdd(&next[wave][e], 1);
     }
-    __syncthreads();
-    // `all`: an expert's pairs; next[w]: those of earlier chunks and of earlier waves of this one
-    for (int e = threadIdx.x; e < kMostExperts; e += 256) {
-        int own = 0, before = 0, sum = 0;
-        if (e < a.experts) {
-            int32_t c[4];
+    if (a.chunks > 1) {
+        // all chunks' counts: as many threads to an expert as there are, each a run of chunks with its loads under way together
+        const int wide = a.experts <= THREADS / 4 ? THREADS / 4 : a.experts <= THREADS / 2 ? THREADS / 2 : THREADS;
+        const int run = (a.chunks * wide + THREADS - 1) / THREADS, first = (int)threadIdx.x / wide * run, last = min(first + run, a.chunks);
+        for (int e = (int)threadIdx.x % wide; e < a.experts; e += wide) {
+            int before = 0, sum = 0;
+            for (int b0 = first; b0 < last; b0 += 16) {
+                int n[16];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                c[w] = own;
-                own += next[w][e];
-            }
-            if (a.chunks == 1) sum = own;
-            else
-                for (int b0 = 0; b0 < a.chunks; b0 += 32) {   // loads under way
-                    int n[32];
+                for (int q = 0; q < 16; ++q) n[q] = a.counts[min(b0 + q, a.chunks - 1) * a.experts + e];
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) n[q] = a.counts[min(b0 + q, a.chunks - 1) * a.experts + e];
-#pragma unroll
-                    for (int q = 0; q < 32; ++q) {
-                        before += b0 + q < block ? n[q] : 0;
-                        sum += b0 + q < a.chunks ? n[q] : 0;
-                    }
+                for (int q = 0; q < 16; ++q) {
+                    before += b0 + q < min(last, block) ? n[q] : 0;
+                    sum += b0 + q < last ? n[q] : 0;
                 }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) next[w][e] = before + c[w];
+            }
+            atomicAdd(&all[e], sum);
+            atomicAdd(&earlier[e], before);
         }
-        all[e] = sum;
     }
     __syncthreads();
-    // where each expert's pairs begin: four experts a thread
-    int n[4], mine = 0;
+    // `all`: an expert's pairs; next[w]: those of earlier chunks and of earlier waves of this one
+    for (int e = threadIdx.x; e < a.experts; e += THREADS) {
+        int own = earlier[e];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+        for (int w = 0; w < WAVES; ++w) {
+            const int n = next[w][e];
+            next[w][e] = own;
+            own += n;
+        }
+        if (a.chunks == 1) all[e] = own;
+    }
+    __syncthreads();
+    // where each expert's pairs begin
+    int n[EACH], mine = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
         n[i] = mine;
-        mine += all[threadIdx.x * 4 + i];
+        mine += all[threadIdx.x * EACH + i];
     }
     int until = mine;
 #pragma unroll
@@ -465,17 +475,17 @@ __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
     __syncthreads();
     int before = until - mine, total = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         before += w < wave ? sums[w] : 0;
         total += sums[w];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int e = threadIdx.x * 4 + i;
+    for (int i = 0; i < EACH; ++i) {
+        const int e = threadIdx.x * EACH + i;
         if (e >= a.experts) break;
         const int start = before + n[i];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) next[w][e] += start;
+        for (int w = 0; w < WAVES; ++w) next[w][e] += start;
         if (block == 0) a.starts[e] = start;
     }
     if (block == 0 && threadIdx.x == 0) a.starts[a.experts] = total;
@@ -513,9 +523,9 @@ __device__ __forceinline__ void place_chunk(const ListArgs &a, int block)
     for (int p = max(from, total) + lane; p < to; p += 64) a.order[p] = -1;
 }
 
-__global__ __launch_bounds__(256) void place_kernel(const ListArgs a)
+__global__ __launch_bounds__(kPlaceWaves * 64) void place_kernel(const ListArgs a)
 {
-    place_chunk(a, blockIdx.x);
+    place_chunk<kPlaceWaves>(a, blockIdx.x);
 }
 
 // Few rows: choices and lists in one launch of one workgroup, a wave a row at a time.
@@ -525,11 +535,17 @@ __global__ __launch_bounds__(256) void route_few_kernel(const RouteArgs a, const
     for (int row = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); row < a.rows; row += 4) route_row<T, V, WIDE>(a, row, threadIdx.x & 63);
     __threadfence_block();
     __syncthreads();
-    place_chunk(lists, 0);
+    place_chunk<4>(lists, 0);
 }
 
-constexpr int kMostChunks = 128;   // each workgroup reads all counts
-int chunk_of(int pairs) { return (pairs + 1024 * kMostChunks - 1) / (1024 * kMostChunks) * 1024; }
+// Up to 8192 pairs are one workgroup's, which counts them itself (5204 pairs of 60 experts: 9.0 us, in chunks 3.4 and 5.8); of more, chunks of at
+// least 1024, and at most 128 of them, as each workgroup reads all counts.
+constexpr int kMostChunks = 128, kOneChunk = 8192;
+int chunk_of(int pairs)
+{
+    const int n = pairs <= kOneChunk ? 1 : kMostChunks;
+    return (pairs + 1024 * n - 1) / (1024 * n) * 1024;
+}
 
 dn_status sizes(int32_t rows, int32_t experts, int32_t k)
 {
@@ -549,7 +565,7 @@ hipError_t launch_lists(ListArgs a, hipStream_t s)
     a.chunk = chunk_of(a.pairs);
     a.chunks = (a.pairs + a.chunk - 1) / a.chunk;
     if (a.chunks > 1) launch_kernel(count_kernel, dim3(a.chunks), dim3(256), 0, s, a);
-    launch_kernel(place_kernel, dim3(a.chunks), dim3(256), 0, s, a);
+    launch_kernel(place_kernel, dim3(a.chunks), dim3(kPlaceWaves * 64), 0, s, a);
     return hipGetLastError();
 }
 
