@@ -525,7 +525,7 @@ dn_status dn_dropout(int32_t type, const void *X_dev, void *Y_dev, int32_t rows,
  * The experts' calls read the lists on the device.  Whatever numbers they hold, no call reads or writes outside its tensors; what it
  * computes is then meaningless.
  *
- * Limits: experts 1 .. 1024, k 1 .. 32, rows below 2^26, P below 2^30; in dn_experts_* P below 2^24, X and dY within 2^31 bytes, and matrices whose
+ * Limits: experts 1 .. 1024, k 1 .. 32, rows below 2^25, P below 2^30; in dn_experts_* P below 2^24, X and dY within 2^31 bytes, and matrices whose
  * widths are multiples of 16 bytes must begin at one.
  *
  * Errors: as for the block's calls; INVALID_ARG also for a scale, grad_scale or max_norm that is not finite or has no meaning (max_norm:
@@ -600,7 +600,7 @@ dn_status dn_experts_backward(const dn_experts_desc *d, const void *X_dev, const
  * Clipping by the norm of many tensors together:  n = sqrt(the sum of g^2 over all of them),  out = g * min(1, max_norm / n).
  *   spans [n_spans] (host, read before the call returns): count elements of `type` at grad; the result goes to out, of out_type
  *   (`type` or DN_F32): grad itself where out_type is type, or memory apart from every grad and every other out.  count 0: nothing there
- *   norm [1] (device, fp32) receives n.  Squares are added in 64 bits, in an order that depends on the spans alone.
+ *   norm [1] (device, fp32; apart from all of these) receives n.  Squares are added in 64 bits, in an order that depends on the spans alone.
  * An n that is not finite (an element is not) bounds nothing: results are the gradients, and the caller reads it in norm.  max_norm INFINITY
  * and out NULL everywhere: the norm only.  Results in place are written only where they change (n > max_norm).
  */

@@ -145,25 +145,27 @@ dn_status check(const dn_span *spans, int32_t n)
     return DN_OK;
 }
 
-// No result may lie where another tensor's gradient or result does: two workgroups would write there, or one read what the other wrote.
-dn_status apart(const dn_span *spans, int32_t n)
+// No result (nor the norm) may lie where another tensor's gradient or result does: two workgroups would write there, or one read what the
+// other wrote.
+dn_status apart(const dn_span *spans, int32_t n, const float *norm)
 {
-    struct Range { uintptr_t from, to; int32_t span; bool written; };
-    Range *r = static_cast<Range *>(malloc(sizeof(Range) * 2 * (size_t)(n > 0 ? n : 1)));
+    struct Range { uintptr_t from, to; bool written; };
+    Range *r = static_cast<Range *>(malloc(sizeof(Range) * (2 * (size_t)n + 1)));
     if (!r) return DN_ERR_OOM;
     int64_t m = 0;
     bool sorted = true;
-    auto add = [&](const void *p, int64_t bytes, int32_t i, bool written) {
-        r[m] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, i, written};
+    auto add = [&](const void *p, int64_t bytes, bool written) {
+        r[m] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written};
         sorted = sorted && (!m || r[m - 1].from <= r[m].from);
         ++m;
     };
     for (int32_t i = 0; i < n; ++i)
         if (spans[i].count) {
             const bool same = spans[i].out_dev == spans[i].grad_dev && spans[i].out_type == spans[i].type;
-            add(spans[i].grad_dev, spans[i].count * size_of(spans[i].type), i, same);
-            if (spans[i].out_dev && !same) add(spans[i].out_dev, spans[i].count * size_of(spans[i].out_type), i, true);
+            add(spans[i].grad_dev, spans[i].count * size_of(spans[i].type), same);
+            if (spans[i].out_dev && !same) add(spans[i].out_dev, spans[i].count * size_of(spans[i].out_type), true);
         }
+    add(norm, sizeof(float), true);
     if (!sorted) std::sort(r, r + m, [](const Range &x, const Range &y) { return x.from < y.from; });
     // the furthest end so far of what is read, and of what is written
     uintptr_t read = 0, written = 0;
@@ -205,7 +207,7 @@ dn_status dn_clip(const dn_span *spans, int32_t n_spans, float max_norm, float *
     dn_status st = check(spans, n_spans);
     if (st != DN_OK) return st;
     if (!(max_norm >= 0.f) || !norm_dev || !multiples(DN_F32, norm_dev)) return DN_ERR_INVALID_ARG;
-    if ((st = apart(spans, n_spans)) != DN_OK) return st;
+    if ((st = apart(spans, n_spans, norm_dev)) != DN_OK) return st;
     const size_t parts = parts_of(spans, n_spans);
     if ((st = workspace(up256(parts * sizeof(double)), workspace_dev, workspace_bytes)) != DN_OK) return st;
     const hipStream_t s = (hipStream_t)hip_stream;

@@ -7,7 +7,7 @@ namespace dn {
 namespace {
 
 constexpr int kFewTokens = 4, kMostExperts = 1024, kMostChoices = 32;
-constexpr int64_t kMostRows = (int64_t)1 << 26, kMostPairs = (int64_t)1 << 24, kMostBytes = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMostRows = (int64_t)1 << 25, kMostPairs = (int64_t)1 << 24, kMostBytes = ((int64_t)1 << 31) - 1;
 
 // ---- rows ------------------------------------------------------------------------------------------------------------
 

@@ -8,7 +8,7 @@ namespace dn {
 namespace {
 
 constexpr int kMostExperts = 1024, kMostChoices = 32, kWaves = 4;
-constexpr int64_t kMostRows = (int64_t)1 << 26, kMostPairs = (int64_t)1 << 30;
+constexpr int64_t kMostRows = (int64_t)1 << 25, kMostPairs = (int64_t)1 << 30;
 
 struct RouteArgs {
     const void *l;

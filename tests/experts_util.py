@@ -64,13 +64,13 @@ def lists(expert, experts):
     return tuple(torch.tensor(v, dtype=torch.int32) for v in (starts, order, place))
 
 
-def forward64(X, Wg, Wu, Wd, weight, expert, R, act):
-    """Y, and G, U of every pair [rows][k][f]."""
-    X, Wg, Wu, Wd, weight, expert = (t.detach().cpu() for t in (X, Wg, Wu, Wd, weight, expert))
+def forward64(X, Wg, Wu, Wd, weight, expert, R, act, on="cpu"):
+    """Y, and G, U of every pair [rows][k][f]; `on`: where it is computed."""
+    X, Wg, Wu, Wd, weight, expert = (t.detach().to(on) for t in (X, Wg, Wu, Wd, weight, expert))
     rows, k = expert.shape
     f, d = Wg.shape[1:]
-    Y = torch.zeros(rows, d, dtype=torch.float64) if R is None else R.double().cpu().clone()
-    G, U = (torch.zeros(rows, k, f, dtype=torch.float64) for _ in range(2))
+    Y = torch.zeros(rows, d, dtype=torch.float64, device=on) if R is None else R.double().to(on).clone()
+    G, U = (torch.zeros(rows, k, f, dtype=torch.float64, device=on) for _ in range(2))
     for e in range(Wg.shape[0]):
         t, j = (expert == e).nonzero(as_tuple=True)
         if len(t):
@@ -81,11 +81,11 @@ def forward64(X, Wg, Wu, Wd, weight, expert, R, act):
     return Y, G, U
 
 
-def backward64(X, Wg, Wu, Wd, weight, expert, G, U, dY, act, grad_scale=1.0):
+def backward64(X, Wg, Wu, Wd, weight, expert, G, U, dY, act, grad_scale=1.0, on="cpu"):
     """dX, dWg, dWu, dWd, dweight, from G and U [rows][k][f] as the forward call left them."""
-    X, Wg, Wu, Wd, weight, expert, dY = (t.detach().cpu() for t in (X, Wg, Wu, Wd, weight, expert, dY))
-    dX, dweight = torch.zeros(X.shape, dtype=torch.float64), torch.zeros(expert.shape, dtype=torch.float64)
-    dWg, dWu, dWd = (torch.zeros(w.shape, dtype=torch.float64) for w in (Wg, Wu, Wd))
+    X, Wg, Wu, Wd, weight, expert, dY = (t.detach().to(on) for t in (X, Wg, Wu, Wd, weight, expert, dY))
+    dX, dweight = (torch.zeros(t.shape, dtype=torch.float64, device=on) for t in (X, expert))
+    dWg, dWu, dWd = (torch.zeros(w.shape, dtype=torch.float64, device=on) for w in (Wg, Wu, Wd))
     for e in range(Wg.shape[0]):
         t, j = (expert == e).nonzero(as_tuple=True)
         if not len(t):

@@ -41,7 +41,7 @@ int main(int argc, char **argv)
                 s.push_back({at, at, n[1], type, type});
             }
             for (int k = 0; k < 2; ++k) {
-                status[k] = dn_clip(s.data(), n[0], 1.f, f32, ws, dn_clip_workspace_bytes(s.data(), n[0]), nullptr);
+                status[k] = dn_clip(s.data(), n[0], 1.f, (float *)(uintptr_t)0x1000, ws, dn_clip_workspace_bytes(s.data(), n[0]), nullptr);
                 made[k].swap(launches);
                 for (auto &v : s) v.out_dev = nullptr;
             }

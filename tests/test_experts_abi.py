@@ -17,7 +17,7 @@ def lib():
 
 
 def route(**kw):
-    d = dict(type=dn.DN_BF16, score=dn.DN_SCORE_SIGMOID, rows=1000, experts=64, k=8, groups=8, top_groups=4, group_best=2, renorm=1, scale=2.5, ldl=0)
+    d = dict(type=dn.DN_BF16, score=dn.DN_SCORE_SIGMOID, rows=5000, experts=64, k=8, groups=8, top_groups=4, group_best=2, renorm=1, scale=2.5, ldl=0)
     d.update(kw)
     return dn.RouteDesc(**d)
 
@@ -35,9 +35,9 @@ def swap(args, k, v):
 def test_route_refuses(lib):
     at = C.addressof
     ok = route()
-    need = lib.dn_route_workspace_bytes(1000, 64, 8)
+    need = lib.dn_route_workspace_bytes(5000, 64, 8)
     assert 0 < need < BAD and need % 256 == 0
-    assert lib.dn_route_workspace_bytes(128, 1024, 8) == 0
+    assert lib.dn_route_workspace_bytes(1024, 1024, 8) == 0
     fwd, back = [A] * 7, [A] * 4
     assert lib.dn_route_forward(None, *fwd, A, need, None) == ARG and lib.dn_route_backward(None, *back, None) == ARG
     for kw, status in [({"type": 3}, ARG), ({"score": 2}, ARG), ({"score": -1}, ARG), ({"group_best": 0}, ARG), ({"group_best": 3}, ARG),
@@ -135,7 +135,10 @@ def test_clip_refuses(lib):
     for rows in ([ok, ok], [ok, (A + 396, A + 396, 1, f32, f32)], [ok, (A + 4096, A + 200, 10, f32, f32)], [(A, 2 * A, 100, f32, f32), (A + 4096, 2 * A + 4, 9, f32, f32)],
                  [(A, A, 100, f16, f32)], [(A, A + 4, 100, f32, f32)], [(A, 2 * A, 9, f32, f32), (2 * A + 16, None, 9, f32, f32)]):
         s = spans(*rows)
-        assert lib.dn_clip(at(s), len(rows), 1.0, A, A, 1 << 30, None) == ARG, rows
+        assert lib.dn_clip(at(s), len(rows), 1.0, 64 * A, A, 1 << 30, None) == ARG, rows
+    s = spans(ok)
+    for norm in (A, A + 200, A + 396):       # the norm among the results
+        assert lib.dn_clip(at(s), 1, 1.0, norm, A, 1 << 30, None) == ARG
 
 
 def test_workspaces_follow_the_spans(lib):

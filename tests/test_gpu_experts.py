@@ -208,6 +208,22 @@ def test_the_same_bits_and_other_rows():
             assert torch.equal(bad[keep], Y[keep]) and bad[1].isnan().all()
 
 
+def test_the_residual_itself():
+    """Y may be R, and both X: every row is read before it is written."""
+    for name, dtype in TYPES.items():
+        for rows in (2, 30, 700):
+            c = Case(dtype, rows, 6, 2, 64, 72, seed=11)
+            Y, _ = c.forward()
+            R = c.R.clone()
+            dn.dn_experts_forward(c.X, c.Wg, c.Wu, c.Wd, *c.lists, R, R)
+            assert torch.equal(R, Y)
+            c.R = c.X
+            Y, _ = c.forward()
+            X = c.X.clone()
+            dn.dn_experts_forward(X, c.Wg, c.Wu, c.Wd, *c.lists, X, X)
+            assert torch.equal(X, Y)
+
+
 def test_lists_that_are_wrong_stay_inside():
     """Numbers out of range in the lists: no access outside the tensors (what is computed has no meaning), and the next call is right."""
     for rows in (4, 300):
