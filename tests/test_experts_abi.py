@@ -115,27 +115,27 @@ def spans(*rows):
 
 def test_clip_refuses(lib):
     f32, f16, bf16 = dn.DN_F32, dn.DN_F16, dn.DN_BF16
-    at = C.addressof
+    at, N = C.addressof, 64 * A           # N: where the norm goes
     ok = (A, A, 100, f32, f32)
     good = spans(ok, (A + 4096, 2 * A, 50, bf16, f32), (None, None, 0, f16, f16))
     need = lib.dn_clip_workspace_bytes(at(good), 3)
     assert 0 < need < BAD and need % 256 == 0 and 0 < lib.dn_clip_workspace_bytes(None, 0) < BAD
     for bound in (-1.0, math.nan, -math.inf):
-        assert lib.dn_clip(at(good), 3, bound, A, A, need, None) == ARG
+        assert lib.dn_clip(at(good), 3, bound, N, A, need, None) == ARG
     assert lib.dn_clip(at(good), 3, 1.0, None, A, need, None) == ARG and lib.dn_clip(at(good), 3, 1.0, A + 2, A, need, None) == ARG
-    assert lib.dn_clip(at(good), 3, 1.0, A, A, need - 1, None) == SHAPE and lib.dn_clip(at(good), 3, 1.0, A, None, need, None) == ARG
-    assert lib.dn_clip(at(good), -1, 1.0, A, A, need, None) == ARG and lib.dn_clip(None, 1, 1.0, A, A, need, None) == ARG
+    assert lib.dn_clip(at(good), 3, 1.0, N, A, need - 1, None) == SHAPE and lib.dn_clip(at(good), 3, 1.0, N, None, need, None) == ARG
+    assert lib.dn_clip(at(good), -1, 1.0, N, A, need, None) == ARG and lib.dn_clip(None, 1, 1.0, N, A, need, None) == ARG
     for row, status in [((A, A, 100, 3, 3), ARG), ((A, A, 100, f32, f16), ARG), ((A, A, 100, f16, bf16), ARG), ((A, A, -1, f32, f32), SHAPE),
                         ((A, A, 1 << 44, f32, f32), SHAPE), ((None, A, 1, f32, f32), ARG), ((A + 2, A + 2, 1, f32, f32), ARG), ((A, A + 1, 1, f16, f16), ARG),
                         ((A + 1, None, 1, bf16, bf16), ARG), ((A, 2 * A + 2, 1, f16, f32), ARG)]:
         s = spans(ok[:1] + (None,) + ok[2:], row)
         assert lib.dn_clip_workspace_bytes(at(s), 2) == BAD, row
-        assert lib.dn_clip(at(s), 2, 1.0, A, A, 1 << 30, None) == status, row
+        assert lib.dn_clip(at(s), 2, 1.0, N, A, 1 << 30, None) == status, row
     # results over other gradients or results; over their own gradient in another type, or a little further on
     for rows in ([ok, ok], [ok, (A + 396, A + 396, 1, f32, f32)], [ok, (A + 4096, A + 200, 10, f32, f32)], [(A, 2 * A, 100, f32, f32), (A + 4096, 2 * A + 4, 9, f32, f32)],
                  [(A, A, 100, f16, f32)], [(A, A + 4, 100, f32, f32)], [(A, 2 * A, 9, f32, f32), (2 * A + 16, None, 9, f32, f32)]):
         s = spans(*rows)
-        assert lib.dn_clip(at(s), len(rows), 1.0, 64 * A, A, 1 << 30, None) == ARG, rows
+        assert lib.dn_clip(at(s), len(rows), 1.0, N, A, 1 << 30, None) == ARG, rows
     s = spans(ok)
     for norm in (A, A + 200, A + 396):       # the norm among the results
         assert lib.dn_clip(at(s), 1, 1.0, norm, A, 1 << 30, None) == ARG
