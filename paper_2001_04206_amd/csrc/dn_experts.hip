@@ -13,7 +13,8 @@ constexpr int64_t kMostRows = (int64_t)1 << 25, kMostPairs = (int64_t)1 << 24, k
 
 // Y_t = R_t + the sum over its pairs of (weight) z, in the order of the choices.  A thread: eight columns of a row.  z is fp32, or for results of
 // 16 bits (and k in one part) in 24, so that what is rounded is the sum: with z in 16 bits each would be rounded by itself, and results
-// without a residual be off by 0.0029 where they are by 0.0024 (bf16; of which H has a rounding, and the result).
+// without a residual be off by 0.0029 where they are by 0.0024 (bf16; of which H has a rounding, and the result).  Bound by memory: 65536 pairs'
+// rows of 2048 into 8192, 92 us (5.1 TB/s; of fp32 118).
 struct JoinArgs {
     const void *z, *low;       // low: the low bytes of 24 bits, NULL: fp32
     const void *r;
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(256) void join_pairs_kernel(const JoinArgs a)
     store8<T>(a.y, t * a.ldy + n, v, left);
 }
 
-// The weights' derivatives from the parts that the tiles of dh left, one for 64 columns, in order.
+// The weights' derivatives from the parts that the tiles of dh left, one for 64 columns, in order.  65536 pairs, 16 parts: 10 us.
 __global__ __launch_bounds__(256) void dots_kernel(const float *dots, int parts, Group g, const int32_t *place, float *dweight)
 {
     const int i = blockIdx.x * 256 + threadIdx.x;
@@ -106,9 +107,9 @@ int64_t most_tiles(int64_t pairs, int experts, int rows) { return pairs / rows +
 // Which kernel a product of the experts takes, and its k in how many parts: what is expected to take least, by the times that plan_product
 // goes by.  How the pairs are spread is not known here: each expert's last tile is taken to be half full.  Weights come at 4.6 TB/s (large
 // tiles: 3.8; the kernel for few rows: 5): 64 tokens through 8 of 64 experts, 2048 wide with 1024 hidden, take 108 us for the gated product
-// on the kernel for few rows (large tiles 141), 1024 tokens 249 on medium tiles (large ones 313), 128 191 on small ones (few rows 224).  The
-// product with the activation's derivative moves ten bytes an element beside it, and large tiles have no registers for that: 415 us on
-// medium ones at 8192 tokens, 442 on large ones.  Parts are for the products whose results the pairs' sums read: these add them too.
+// on the kernel for few rows (large tiles 141); a whole forward pass of 1024 tokens 234 on medium tiles (large ones 281, small ones 243), of 128
+// 190 (all on the kernel for few rows 242).  The product with the activation's derivative moves ten bytes an element beside it, and large
+// tiles have no registers for that: 409 us on medium ones at 8192 tokens, 442 on large ones.  Parts are for the products whose results the pairs' sums read: these add them too.
 struct Plan { ProductKernel kernel = K_SMALL; int parts = 1; };
 Plan plan_experts(int type, Product p, Epilogue e, int64_t pairs, int experts, int N, int K, int segments, bool few_tokens = false)
 {

@@ -1,4 +1,9 @@
 // Routing of rows to experts: choices and weights from logits, the lists of rows by expert, and the logits' gradient.
+//
+// Bound by instructions, about 1100 a row of 256 experts with groups and eight choices, each of which finds a highest and takes it out: 16384 rows
+// in 27 us with a bias and groups (scores in 64 bits take 8 of them; in 32, with rows that come close done again, it was no faster), 18 without,
+// 7 for one choice.  The lists take 4.8 and 6.6 us more for 131072 pairs.  One row of 128 experts with its lists: one launch, 5.4 us.  Backward,
+// 16384 rows of 128: 8.8 us.
 #include <type_traits>
 
 #include "dn_ffn_host.h"
