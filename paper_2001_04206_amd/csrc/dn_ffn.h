@@ -55,7 +55,7 @@ __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8],
 __device__ __forceinline__ uint32_t upper24(float v)
 {
     const uint32_t u = __builtin_bit_cast(uint32_t, v);
-    return v == v ? u + 0x80 : u & 0xffffff00u | 0x400000u;   // (a carry of NaN's would make a number of it)
+    return v == v ? u + 0x80 : (u & 0xffffff00u) | 0x400000u;   // (a carry of NaN's would make a number of it)
 }
 template <bool ALL>
 __device__ __forceinline__ void store24(void *high, void *low, int64_t at, const float (&v)[8], int left)

@@ -1,9 +1,8 @@
 // Routing of rows to experts: choices and weights from logits, the lists of rows by expert, and the logits' gradient.
 //
-// Bound by instructions, about 1100 a row of 256 experts with groups and eight choices, each of which finds a highest and takes it out: 16384 rows
-// in 27 us with a bias and groups (scores in 64 bits take 8 of them; in 32, with rows that come close done again, it was no faster), 18 without,
-// 7 for one choice.  The lists take 4.8 and 6.6 us more for 131072 pairs.  One row of 128 experts with its lists: one launch, 5.4 us.  Backward,
-// 16384 rows of 128: 8.8 us.
+// Bound by instructions, about 900 a row of 256 experts with groups and eight choices: 16384 rows in 25 us with a bias and groups (scores in
+// 64 bits take 7 of them, groups 4; scores in 32, with rows that come close done again, were no faster), 14 without, 7 for one choice.  The lists
+// take 4.8 and 6.6 us more for 131072 pairs.  One row of 128 experts with its lists: one launch, 5.4 us.  Backward, 16384 rows of 128: 8.8 us.
 #include <type_traits>
 
 #include "dn_ffn_host.h"
@@ -45,6 +44,28 @@ __device__ __forceinline__ double last_lane(double v)
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 __device__ __forceinline__ float highest(float v) { return wave_max(v); }
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int higher(int v)
+{
+    return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, ROW_MASK, 0xf, ROW_MASK == 0xf));   // (lanes that are not moved to keep v)
+}
+__device__ __forceinline__ int highest(int v)
+{
+    v = higher<0xB1, 0xf>(v);    // as wave_max()
+    v = higher<0x4E, 0xf>(v);
+    v = higher<0x141, 0xf>(v);
+    v = higher<0x140, 0xf>(v);
+    v = higher<0x142, 0xa>(v);
+    v = higher<0x143, 0xc>(v);
+    return __builtin_amdgcn_readlane(v, 63);
+}
+// fp32 numbers as whole numbers of the same order, -0 as 0; kNone is that of -inf
+__device__ __forceinline__ int in_order(float v)
+{
+    const int u = __builtin_bit_cast(int, v + 0.f);
+    return u ^ (int)((uint32_t)(u >> 31) >> 1);
+}
+constexpr int kNone = (int)0x807fffff;
 __device__ __forceinline__ double highest(double v)
 {
     const double ninf = -INFINITY;
@@ -251,52 +272,56 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
     }
     int chosen = -1;
     float logit = -INFINITY;   // lane j: of choice j
-    // Ranks in 32 bits: rounding keeps their order, so one that is alone the highest there is the highest; only equals are told apart in 64.
-    float c32[V], b = -INFINITY;
+    // Ranks in 32 bits: rounding keeps their order, so one that is alone the highest there is the highest; only equals are told apart in 64.  As
+    // whole numbers of the same order: a step of the wave's maximum is one instruction, where fp32's is five.  Which of the lane's
+    // experts it is, and taking it out, is a matter of one lane: its ranks are read into scalar registers, whose instructions go beside the
+    // other waves' vector ones.
+    int key[V], b = kNone;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        c32[i] = (float)c[i];
-        b = fmaxf(b, c32[i]);
+        key[i] = in_order((float)c[i]);
+        b = max(b, key[i]);
     }
     for (int j = 0; j < a.k; ++j) {
-        const float best = wave_max(b);
-        if (!(best > -INFINITY)) break;
-        int at = 0, equal = 0;
-        float mine = l[0];
+        const int best = highest(b);
+        if (best == kNone) break;
+        const uint64_t have = __ballot(b == best);
+        int f = __builtin_ctzll(have), at = 0, equal = 0;
 #pragma unroll
         for (int i = V - 1; i >= 0; --i)
-            if (c32[i] == best) {
+            if (__builtin_amdgcn_readlane(key[i], f) == best) {
                 at = i;
-                mine = l[i];
                 ++equal;
             }
-        uint64_t have = __ballot(equal > 0);
         if constexpr (WIDE) {
-            if (have & (have - 1) || __ballot(equal > 1)) {   // (every lane takes part)
+            if (have & (have - 1) || equal > 1) {   // (every lane takes part)
                 Rank r = ninf;
+                int mine = 0;
 #pragma unroll
                 for (int i = V - 1; i >= 0; --i)
-                    if (c32[i] == best && c[i] >= r) {
+                    if (key[i] == best && c[i] >= r) {
                         r = c[i];
-                        at = i;
-                        mine = l[i];
+                        mine = i;
                     }
                 const Rank top = highest(r);
-                have = __ballot(equal > 0 && r == top);
+                f = __builtin_ctzll(__ballot(b == best && r == top));
+                at = __builtin_amdgcn_readlane(mine, f);
             }
         }
-        const int f = __builtin_ctzll(have), e = f * V + __builtin_amdgcn_readlane(at, f);
-        const float le = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), f));
-        if (lane == j) {
-            chosen = e;
-            logit = le;
-        }
-        b = -INFINITY;
+        int le = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (first + i == e) c32[i] = -INFINITY;
-            b = fmaxf(b, c32[i]);
+        for (int i = 0; i < V; ++i)
+            if (at == i) {
+                le = __builtin_amdgcn_readlane(__builtin_bit_cast(int, l[i]), f);
+                key[i] = lane == f ? kNone : key[i];
+            }
+        if (lane == j) {
+            chosen = f * V + at;
+            logit = __builtin_bit_cast(float, le);
         }
+        b = key[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) b = max(b, key[i]);
     }
     float w = weight_of(a, logit, chosen >= 0, m, sum);
     if (!(sum == sum)) w = sum;   // a softmax of NaN or +inf, whose ranks name any expert
