@@ -1,6 +1,6 @@
 // Routing of rows to experts: choices and weights from logits, the lists of rows by expert, and the logits' gradient.
 //
-// Bound by instructions, about 900 a row of 256 experts with groups and eight choices: 16384 rows in 25 us with a bias and groups (scores in
+// Bound by instructions, about 900 a row of 256 experts with groups and eight choices: 16384 rows in 24 us with a bias and groups (scores in
 // 64 bits take 7 of them, groups 4; scores in 32, with rows that come close done again, were no faster), 14 without, 7 for one choice.  The lists
 // take 4.8 and 6.6 us more for 131072 pairs.  One row of 128 experts with its lists: one launch, 5.4 us.  Backward, 16384 rows of 128: 8.8 us.
 #include <type_traits>
