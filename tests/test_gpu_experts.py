@@ -51,13 +51,13 @@ class Case:
         gu = torch.where((place >= 0)[:, None], GU.cpu()[place.clamp(min=0)].double(), 0.0).view(rows, k, 2 * f)
         return gu[..., :f], gu[..., f:]
 
-    def backward(self, GU, grad_dtype=None, grad_scale=1.0, dX=True, dweight=True):
+    def backward(self, GU, grad_dtype=None, grad_scale=1.0, dX=True, dweight=True, workspace=None):
         rows, experts, k, d, f = self.shape
         out = lambda *s, t=None: self.make.out(*s, dtype=t)
         g = {"dX": out(rows, d) if dX else None, "dWg": out(experts, f, d, t=grad_dtype), "dWu": out(experts, f, d, t=grad_dtype),
              "dWd": out(experts, d, f, t=grad_dtype), "dweight": out(rows, k, t=torch.float32) if dweight else None}
         dn.dn_experts_backward(self.X, self.Wg, self.Wu, self.Wd, *self.lists, GU, self.dY, g["dX"], g["dWg"], g["dWu"], g["dWd"], g["dweight"],
-                               act=ACTS[self.act], grad_scale=grad_scale)
+                               act=ACTS[self.act], grad_scale=grad_scale, workspace=workspace)
         return g
 
     def check_forward(self, Y, GU):
@@ -239,3 +239,84 @@ def test_lists_that_are_wrong_stay_inside():
             c.backward(GU)
             c.lists = keep
         assert torch.equal(c.forward()[0], good)
+
+
+WHERE = [(3, 6, 1, 40, 24), (5, 6, 2, 72, 40), (60, 7, 2, 33, 17), (400, 6, 2, 72, 136), (700, 8, 1, 264, 130), (2500, 5, 2, 328, 200), (2048, 4, 1, 64, 264)]
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("rows,experts,k,d,f", WHERE)
+def test_the_weights_derivatives_alone(name, rows, experts, k, d, f):
+    """Without dX they come from a launch of their own, and are the same; so are the matrices' gradients."""
+    c = Case(TYPES[name], rows, experts, k, d, f, none=0.2, seed=12)
+    _, GU = c.forward()
+    GU = torch.where(GU.isnan(), torch.zeros_like(GU), GU)
+    whole, alone, rest = c.backward(GU), c.backward(GU, dX=False), c.backward(GU, dweight=False)
+    c.check_backward(alone, GU)
+    assert all(torch.equal(whole[n], alone[n]) for n in alone if n != "dX")
+    assert all(torch.equal(whole[n], rest[n]) for n in rest if n != "dweight")
+
+
+def filled():
+    return torch.full((64 << 20,), 255, dtype=torch.uint8, device=DEV)
+
+
+@pytest.mark.parametrize("what", ["NaN", "inf"])
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("rows,experts,k,d,f", WHERE)
+def test_what_one_row_holds_stays_with_it(name, what, rows, experts, k, d, f):
+    """A row's NaN or infinity in X, dY or its G and U reaches its own results and its experts' gradients, and no bit of others; a row without
+    an expert reaches nothing, nor do the places behind the last pair.  In workspaces whose every byte is FF."""
+    c = Case(TYPES[name], rows, experts, k, d, f, none=0.3, seed=13)
+    c.expert[rows // 2], c.weight[rows // 2] = -1, 0.0
+    dn.dn_route_lists(c.expert, c.starts, c.order, c.place)
+    Y, GU = c.forward(workspace=filled())
+    c.check_forward(Y, GU)
+    clean = c.backward(torch.where(GU.isnan(), torch.zeros_like(GU), GU))
+    dirty = c.backward(GU, workspace=filled())
+    assert all(torch.equal(clean[n], dirty[n]) for n in clean), "places behind the last pair"
+    value = math.nan if what == "NaN" else math.inf
+    X, dY = c.X.clone(), c.dY.clone()
+    for t in (rows // 2, 0, rows - 1):
+        mine = [int(e) for e in c.expert[t] if e >= 0]
+        others = [e for e in range(experts) if e not in mine]
+        left = [i for i in range(rows) if i != t]
+        c.X[t], c.dY[t] = value, value
+        spoilt = GU.clone()
+        for p in c.place.view(rows, k)[t].tolist():
+            if p >= 0:
+                spoilt[p] = value
+        y, _ = c.forward(workspace=filled())
+        g = c.backward(spoilt, workspace=filled())
+        assert torch.equal(y[left], Y[left])
+        assert torch.equal(g["dX"][left], clean["dX"][left]) and torch.equal(g["dweight"][left], clean["dweight"][left])
+        for n in ("dWg", "dWu", "dWd"):
+            assert torch.equal(g[n][others], clean[n][others]), n
+        if not mine:
+            assert torch.equal(y, Y) and all(torch.equal(g[n], clean[n]) for n in g)
+        c.X.copy_(X)
+        c.dY.copy_(dY)
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("rows,experts,k,d,f", WHERE)
+def test_what_one_expert_holds_stays_with_it(name, rows, experts, k, d, f):
+    """NaN in an expert's matrices reaches the rows that chose it, and no bit of others."""
+    c = Case(TYPES[name], rows, experts, k, d, f, none=0.1, seed=14)
+    Y, GU = c.forward()
+    GU = torch.where(GU.isnan(), torch.zeros_like(GU), GU)
+    clean = c.backward(GU)
+    for e in (0, experts // 2, experts - 1):
+        W = [w[e].clone() for w in (c.Wg, c.Wu, c.Wd)]
+        for w in (c.Wg, c.Wu, c.Wd):
+            w[e] = math.nan
+        y, _ = c.forward()
+        g = c.backward(GU)
+        for w, was in zip((c.Wg, c.Wu, c.Wd), W):
+            w[e] = was
+        off = (c.expert == e).any(1)
+        assert torch.equal(y[~off], Y[~off]) and y[off].isnan().all()
+        assert torch.equal(g["dX"][~off], clean["dX"][~off]) and g["dX"][off].isnan().all()
+        assert torch.equal(g["dweight"][c.expert != e], clean["dweight"][c.expert != e])
+        others = [i for i in range(experts) if i != e]
+        assert all(torch.equal(g[n][others], clean[n][others]) for n in ("dWg", "dWu", "dWd"))
