@@ -320,3 +320,15 @@ def test_what_one_expert_holds_stays_with_it(name, rows, experts, k, d, f):
         assert torch.equal(g["dweight"][c.expert != e], clean["dweight"][c.expert != e])
         others = [i for i in range(experts) if i != e]
         assert all(torch.equal(g[n][others], clean[n][others]) for n in ("dWg", "dWu", "dWd"))
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("rows,d,f", [(2, 40, 24), (9, 33, 17), (300, 72, 136), (1500, 264, 130)])
+def test_the_same_expert_twice(name, rows, d, f):
+    """A row that names an expert more than once has its output with each of the weights, and a gradient for each."""
+    c = Case(TYPES[name], rows, 4, 3, d, f, seed=15)
+    c.expert[::2, 1] = c.expert[::2, 0]
+    c.expert[::3] = c.expert[::3, :1]
+    _, starts, order, place = c.lists
+    dn.dn_route_lists(c.expert, starts, order, place)
+    c.check()

@@ -1,6 +1,8 @@
 """Blocks of experts, routings and clippings of shapes that between them take every kernel that the library's rules choose for them
 (test_experts_kernels.py holds the lists against the rules): each tile with each epilogue, whole and in parts of k, and each kernel for few
 rows.  Against the formulas in 64 bits on the device; every tensor that a call writes starts as NaN."""
+import math
+
 import pytest
 import torch
 
@@ -76,3 +78,27 @@ def test_clip(kind, shape):
     n = norm64(before)
     clipped([t.clone() for t in before], 0.3 * n, None, before)
     clipped(before, 0.3 * n, [None] * shape[0], before)
+
+
+@pytest.mark.parametrize("kind,shape", of(EXPERTS))
+def test_rows_apart(kind, shape):
+    """NaN in rows of X, dY, G and U reaches no bit of other rows' results, nor of the gradients of experts that these rows did not choose."""
+    announce("experts' rows apart %s %s" % (kind, shape))
+    rows, experts, k, d, f = shape
+    c = Case(TYPES[kind], *shape, seed=sum(shape))
+    Y, GU = c.forward()
+    clean = c.backward(GU)
+    bad = torch.tensor(sorted({0, rows // 2, rows - 1}), device=DEV)
+    left = torch.ones(rows, dtype=torch.bool, device=DEV)
+    left[bad] = False
+    others = torch.ones(experts, dtype=torch.bool, device=DEV)
+    others[c.expert[bad].flatten().long()] = False
+    c.X[bad], c.dY[bad] = math.nan, math.nan
+    GU[c.place.view(rows, k)[bad].flatten().long()] = math.nan
+    y, _ = c.forward()
+    g = c.backward(GU)
+    assert torch.equal(y[left], Y[left]) and y[bad].isnan().all()
+    assert torch.equal(g["dX"][left], clean["dX"][left]) and torch.equal(g["dweight"][left], clean["dweight"][left])
+    assert g["dX"][bad].isnan().all() and g["dweight"][bad].isnan().all()
+    for n in ("dWg", "dWu", "dWd"):
+        assert torch.equal(g[n][others], clean[n][others]) and g[n][~others].isnan().all(), n
