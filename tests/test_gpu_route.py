@@ -224,3 +224,20 @@ def test_many_rows_and_the_same_bits():
     first = [t.clone() for t in run(L, bias, 6, SIGMOID, groups=8, top_groups=3, group_best=2)]
     again = run(L, bias, 6, SIGMOID, groups=8, top_groups=3, group_best=2)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("experts,groups,top", [(24, 1, 1), (24, 4, 2), (64, 8, 3), (100, 5, 2), (128, 4, 3), (256, 8, 4), (300, 1, 1), (512, 16, 3), (1024, 8, 5)])
+def test_few_distinct_logits(name, experts, groups, top):
+    """Rows of five numbers, both zeros among them, and of -inf: equal ones everywhere, in a lane's experts and between lanes and groups.  (No two sums of
+    a score and a bias, nor of two scores, are equal but those of equal numbers.)"""
+    values = torch.tensor([0.0, -0.0, 0.5, 1.25, -2.0, -INF])
+    k = min(16, top * (experts // groups))
+    for seed, weights in enumerate(([1.0] * 6, [1, 1, 0, 0, 0, 1], [1, 1, 0.02, 0.02, 0.1, 9], [0.01, 0, 0, 0, 0, 1])):
+        g = torch.Generator().manual_seed(seed)
+        L = values[torch.multinomial(torch.tensor(weights).float(), 12 * experts, replacement=True, generator=g)].view(12, experts).to(TYPES[name]).to(DEV)
+        steps = torch.tensor([0.0, 0.25, -0.125])[torch.randint(3, (experts,), generator=g)].to(DEV)
+        for score in (SOFTMAX, SIGMOID):
+            check(L, None, k, score, groups, top, 1 + seed % 2)
+            check(L, steps, k, score, groups, top, 1, renorm=False)
+            check(L, torch.full((experts,), 0.25, device=DEV), k, score, groups, top, 2)
