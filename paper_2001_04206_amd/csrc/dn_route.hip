@@ -161,7 +161,8 @@ __device__ __forceinline__ float from_lane(float v, int lane)
 }
 
 // A wave takes a row, a lane V neighbouring experts of it.  The highest of all lanes, k times: of equal ones the lowest lane holds the
-// lowest expert.  WIDE: ranks are scores in 64 bits plus the bias; otherwise the logits themselves.
+// lowest expert.  WIDE: ranks are scores in 64 bits plus the bias; otherwise the logits themselves.  WIDE without a bias: groups are chosen by
+// sums of two scores, experts by their logits all the same, as scores run together where logits do not (a sigmoid is 1 from 37 on).
 template <class T, int V, bool WIDE>
 __device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
 {
@@ -276,10 +277,11 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
     // whole numbers of the same order: a step of the wave's maximum is one instruction, where fp32's is five.  Which of the lane's
     // experts it is, and taking it out, is a matter of one lane: its ranks are read into scalar registers, whose instructions go beside the
     // other waves' vector ones.
+    const bool by_score = WIDE && a.bias;
     int key[V], b = kNone;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        key[i] = in_order((float)c[i]);
+        key[i] = by_score ? in_order((float)c[i]) : c[i] == ninf ? kNone : in_order(l[i] == l[i] ? l[i] : INFINITY);
         b = max(b, key[i]);
     }
     for (int j = 0; j < a.k; ++j) {
@@ -294,7 +296,7 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, int lane)
                 ++equal;
             }
         if constexpr (WIDE) {
-            if (have & (have - 1) || equal > 1) {   // (every lane takes part)
+            if (by_score && (have & (have - 1) || equal > 1)) {   // (every lane takes part)
                 Rank r = ninf;
                 int mine = 0;
 #pragma unroll
