@@ -103,13 +103,14 @@ __device__ __forceinline__ void load_logits(float (&l)[V], const T *p, int first
     }
 }
 
-// 1 / x of an x from 1 on: the hardware's estimate and two Newton steps; 0 of infinity, NaN of NaN
+// 1 / x of an x from 1 on: the hardware's estimate and two Newton steps.  Near the end of the range (sigmoids of logits below -690), of infinity and
+// of NaN, where the steps fail, a division.
 __device__ __forceinline__ double inverse64(double x)
 {
     double r = __builtin_amdgcn_rcp(x);
     r = fma(fma(-x, r, 1.), r, r);
     r = fma(fma(-x, r, 1.), r, r);
-    return x < 1e300 ? r : x == x ? 0. : x;
+    return x < 1e300 ? r : 1. / x;
 }
 
 // sigmoid(l) e^-low, low <= 0 and not below the largest of the logits that are compared (or 0): ratios of small scores keep their bits

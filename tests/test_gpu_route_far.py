@@ -1,4 +1,5 @@
-"""Routing of logits whose scores run together: beyond 37 a sigmoid is 1 in 64 bits, some 745 below the row's highest a softmax is 0."""
+"""Routing of logits whose scores run together: beyond 37 a sigmoid is 1 in 64 bits, some 745 below the row's highest a softmax is 0, and below -690
+a sigmoid comes near the smallest numbers of 64 bits."""
 import math
 
 import pytest
@@ -71,3 +72,18 @@ def test_not_a_number_among_groups():
         assert torch.equal(expert[:, 0].cpu().long(), at) and weight.isnan().all()
         rest = L.gather(1, expert[:, 1:].long())
         assert (rest[:, :-1] >= rest[:, 1:]).all() and len(set(expert[0].tolist())) == 4
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("experts,groups,top", [(12, 1, 1), (100, 1, 1), (256, 8, 3), (1000, 10, 4)])
+def test_scores_near_the_smallest_numbers(name, experts, groups, top):
+    """Sigmoids of logits from -708 to -680 and a bias of zeros: their scores, 1e-296 to 3e-308, are told apart in 64 bits."""
+    g = torch.Generator().manual_seed(experts)
+    L = (-708 + 28 * torch.rand(20, experts, generator=g)).to(TYPES[name]).to(DEV)
+    k = min(8, top * (experts // groups))
+    expert, *_ = run(L, torch.zeros(experts, device=DEV), k, SIGMOID, groups=groups, top_groups=top, group_best=1)
+    chosen = L.float().gather(1, expert.long())
+    assert (chosen[:, :-1] >= chosen[:, 1:]).all()
+    if groups == 1:
+        assert torch.equal(chosen, L.float().sort(1, descending=True)[0][:, :k])
+    check(L, torch.zeros(experts, device=DEV), k, SIGMOID, groups, top, 1, renorm=True)
