@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void squares_kernel(const ClipArgs a)
 }
 
 template <class T, class U>
-__device__ __forceinline__ void times(const ClipArgs::Span &s, int64_t at, float by)
+__device__ __forceinline__ void times(const ClipArgs::Span &s, int64_t at, float by, double small)
 {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -84,7 +84,7 @@ __device__ __forceinline__ void times(const ClipArgs::Span &s, int64_t at, float
         float v[8];
         load8<T>(v, s.g, i, left);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= by;
+        for (int j = 0; j < 8; ++j) v[j] = small != 0. ? (float)((double)v[j] * small) : v[j] * by;
         store8<U>(s.y, i, v, left);
     }
 }
@@ -97,14 +97,17 @@ __global__ __launch_bounds__(256) void times_kernel(const ClipArgs a)
     const double norm = sqrt(sum_of_block(sum, share));
     if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
     const bool clip = norm > (double)a.max_norm && norm < (double)INFINITY;
-    const float by = clip ? (float)((double)a.max_norm / norm) : 1.f;
+    // Below the normal numbers of fp32 a factor would have few bits or none where results do not (gradients near 1e38, max_norm 1e-3): there
+    // products are formed in 64 bits.
+    const double ratio = clip ? (double)a.max_norm / norm : 1., small = ratio < 0x1p-126 ? ratio : 0.;
+    const float by = (float)ratio;
     for (int p = a.pieces - 1 - (int)blockIdx.x; p >= 0; p -= gridDim.x) {   // what was read last may still be near
         const ClipArgs::Span &s = a.s[span_of(a, p)];
         if (!s.y || (!clip && s.y == s.g)) continue;
         const int64_t at = (int64_t)(p - s.first) * kPiece;
-        if (s.type == DN_F32) times<float, float>(s, at, by);
-        else if (s.type == DN_F16) s.out_type == DN_F32 ? times<f16, float>(s, at, by) : times<f16, f16>(s, at, by);
-        else s.out_type == DN_F32 ? times<bf16, float>(s, at, by) : times<bf16, bf16>(s, at, by);
+        if (s.type == DN_F32) times<float, float>(s, at, by, small);
+        else if (s.type == DN_F16) s.out_type == DN_F32 ? times<f16, float>(s, at, by, small) : times<f16, f16>(s, at, by, small);
+        else s.out_type == DN_F32 ? times<bf16, float>(s, at, by, small) : times<bf16, bf16>(s, at, by, small);
     }
 }
 
