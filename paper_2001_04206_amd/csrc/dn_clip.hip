@@ -19,7 +19,7 @@ constexpr int kGroups = 1024;         // workgroups of a launch, four a compute 
 
 struct ClipArgs {
     struct Span { const void *g; void *y; int64_t n; int32_t first; int16_t type, out_type; } s[kSpans];   // first: its first piece
-    double *parts;         // this launch's (squares); all of them (products)
+    double *parts;         // this launch's (squares); all of them, or their sum (products)
     float *norm;           // written by one workgroup, NULL: not by this launch
     int32_t n, pieces, all_parts;
     float max_norm;
@@ -72,6 +72,26 @@ __global__ __launch_bounds__(256) void squares_kernel(const ClipArgs a)
     }
     sum = sum_of_block(sum, share);
     if (threadIdx.x == 0) a.parts[blockIdx.x] = sum;
+}
+
+// The sum of many launches' parts, formed once, in the order in which the workgroups of a single launch form it.  Where every workgroup of every
+// launch does, that grows with the square of the number of tensors: 8000 of 100 000 bf16 elements into fp32 take 12.6 ms so, 6.0 with this (the call, 0.75 us
+// a tensor), 336 of 2.4 million 1.39 and 1.36.
+__global__ __launch_bounds__(256) void total_kernel(const double *parts, int n, double *total, float *norm)
+{
+    __shared__ double share[4];
+    double sum = 0.;
+    for (int i = threadIdx.x; i < n; i += 256 * 16) {
+        double v[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) v[q] = i + q * 256 < n ? parts[i + q * 256] : 0.;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) sum += v[q];
+    }
+    sum = sum_of_block(sum, share);
+    if (threadIdx.x) return;
+    *total = sum;
+    *norm = (float)sqrt(sum);
 }
 
 template <class T, class U>
@@ -183,14 +203,20 @@ dn_status apart(const dn_span *spans, int32_t n, const float *norm)
     return s;
 }
 
-size_t parts_of(const dn_span *spans, int32_t n)
+struct Parts {
+    size_t n = 0;       // of all launches
+    bool many = false;  // launches
+    size_t bytes() const { return up256((n + many) * sizeof(double)); }   // their sum behind them
+};
+Parts parts_of(const dn_span *spans, int32_t n)
 {
-    size_t parts = 0;
-    runs(spans, n, [&](const ClipArgs &a, int) {
-        parts += (size_t)groups_of(a.pieces);
+    Parts p;
+    runs(spans, n, [&](const ClipArgs &a, int run) {
+        p.n += (size_t)groups_of(a.pieces);
+        p.many = run > 0;
         return true;
     });
-    return parts;
+    return p;
 }
 
 }  // namespace
@@ -202,7 +228,7 @@ extern "C" {
 
 size_t dn_clip_workspace_bytes(const dn_span *spans, int32_t n_spans)
 {
-    return check(spans, n_spans) == DN_OK ? up256(parts_of(spans, n_spans) * sizeof(double)) : kBad;
+    return check(spans, n_spans) == DN_OK ? parts_of(spans, n_spans).bytes() : kBad;
 }
 
 dn_status dn_clip(const dn_span *spans, int32_t n_spans, float max_norm, float *norm_dev, void *workspace_dev,
@@ -212,8 +238,8 @@ dn_status dn_clip(const dn_span *spans, int32_t n_spans, float max_norm, float *
     if (st != DN_OK) return st;
     if (!(max_norm >= 0.f) || !norm_dev || !multiples(DN_F32, norm_dev)) return DN_ERR_INVALID_ARG;
     if ((st = apart(spans, n_spans, norm_dev)) != DN_OK) return st;
-    const size_t parts = parts_of(spans, n_spans);
-    if ((st = workspace(up256(parts * sizeof(double)), workspace_dev, workspace_bytes)) != DN_OK) return st;
+    const Parts parts = parts_of(spans, n_spans);
+    if ((st = workspace(parts.bytes(), workspace_dev, workspace_bytes)) != DN_OK) return st;
     const hipStream_t s = (hipStream_t)hip_stream;
     double *ws = static_cast<double *>(workspace_dev), *at = ws;
     const bool summed = runs(spans, n_spans, [&](ClipArgs &a, int) {
@@ -223,13 +249,17 @@ dn_status dn_clip(const dn_span *spans, int32_t n_spans, float max_norm, float *
         return hipGetLastError() == hipSuccess;
     });
     if (!summed) return DN_ERR_DEVICE;
-    const bool done = runs(spans, n_spans, [&](ClipArgs &a, int run) {
-        bool any = run == 0;
+    if (parts.many) {
+        launch_kernel(total_kernel, dim3(1), dim3(256), 0, s, (const double *)ws, (int)parts.n, at, norm_dev);
+        if (hipGetLastError() != hipSuccess) return DN_ERR_DEVICE;
+    }
+    const bool done = runs(spans, n_spans, [&](ClipArgs &a, int) {
+        bool any = !parts.many;   // to write the norm
         for (int i = 0; i < a.n; ++i) any = any || a.s[i].y;
         if (!any) return true;
-        a.parts = ws;
-        a.all_parts = (int32_t)parts;
-        a.norm = run == 0 ? norm_dev : nullptr;
+        a.parts = parts.many ? at : ws;
+        a.all_parts = parts.many ? 1 : (int32_t)parts.n;
+        a.norm = parts.many ? nullptr : norm_dev;
         a.max_norm = max_norm;
         launch_kernel(times_kernel, dim3(groups_of(a.pieces)), dim3(256), 0, s, a);
         return hipGetLastError() == hipSuccess;
