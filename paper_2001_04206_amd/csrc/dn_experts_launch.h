@@ -45,7 +45,7 @@ hipError_t expert_few(const ProductArgs &a, int64_t tiles, hipStream_t s)
 template <class T, int P, int EPI, int GROUP>
 hipError_t expert_run(ProductKernel kernel, ProductArgs &a, int64_t tiles, hipStream_t s)
 {
-    if constexpr (P == P_FWD)
+    if constexpr (P == P_FWD && EPI != E_PAIR)   // (few rows leave pairs' results in fp32)
         if (kernel == K_FEW) return expert_few<T, EPI, GROUP>(a, tiles, s);
     if (kernel == K_SMALL) return expert_tiles<T, P, EPI, GROUP, Small>(a, tiles, s);
     if constexpr (sizeof(T) == 4) {
