@@ -576,7 +576,9 @@ dn_status dn_route_backward(const dn_route_desc *d, const void *L_dev, const int
  * Backward, with dh = dY_t Wd[e]:  dG = w dh * U * act'(G),  dU = w dh * act(G),  dX_t = the sum of dG Wg[e] + dU Wu[e] over its
  * pairs,  dweight = the sum of dh * H over f (0 for a pair without an expert), and grad_scale times dWg[e] = dG^T X,  dWu[e] = dU^T X,
  * dWd[e] = dY^T (w H) over the expert's pairs (0 for an expert without any).  dX and dweight may be NULL (not computed).
- * H, dG, dU and w H are rounded to `type`, as operands of the next product; z and each pair's dX are added in fp32.
+ * H, dG, dU and w H are rounded to `type`, as operands of the next product, the last three with the weight in them (f16: a dY that is scaled up
+ * keeps products with small weights off the type's smallest numbers).  z and each pair's dX are added in fp32; for a `type` of 16 bits each
+ * of them may be rounded to 16 significant bits first, 2^-17 of it, where tiles form it.
  */
 typedef struct {
     int32_t type, grad_type; /* dn_type */
