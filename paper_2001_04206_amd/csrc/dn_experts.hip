@@ -1,11 +1,14 @@
-// A block of experts: checks, plans, workspaces and launches, and what lies between its products: rows into the experts' order, and the
-// pairs' results back together.
+// A block of experts: checks, plans, workspaces and launches, and what follows its products: the pairs' results back together.
 #include "dn_experts.h"
 #include "dn_ffn_host.h"
 
 namespace dn {
 namespace {
 
+// Up to so many tokens the last product forms the sums itself.  Forward pass so, and with a launch for the sums, in us, one token: 22.2 and 27.5 (8 of
+// 64 experts, 2048 wide, 1024 hidden, bf16), 13.8 and 17.0 (2 of 8, 512, 1024), 13.7 and 16.9 (2 of 16, 1021, 555, f16), 13.7 and 17.9 (4 of
+// 128, 1024, 512, fp32), 25.7 and 28.2 (2 of 8, 2048, 4096); four tokens: 68.3 and 73.8, 13.8 and 17.1, 13.7 and 18.1, 24.4 and 29.2, 65.0 and 63.5; eight:
+// 107.9 and 104.4, 13.8 and 17.1, 19.3 and 21.5, 40.8 and 46.2, 87.3 and 75.1, as an expert that several rows share is read by each.
 constexpr int kFewTokens = 4, kMostExperts = 1024, kMostChoices = 32;
 constexpr int64_t kMostRows = (int64_t)1 << 25, kMostPairs = (int64_t)1 << 24, kMostBytes = ((int64_t)1 << 31) - 1;
 

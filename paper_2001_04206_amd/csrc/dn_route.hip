@@ -638,7 +638,10 @@ dn_status route_of(const dn_route_desc *d, RouteArgs &a)
     return DN_OK;
 }
 
-constexpr int kOneLaunchRows = 8;   // of one workgroup
+// Rows of one workgroup, a wave a row at a time.  So, and in launches of their own, us: up to four rows 8.2 and 10.8 (128 experts, 8 choices; 256 with a
+// bias; 16), 20.3 to 21.0 and 21.0 to 21.7 (1024 experts, 16 choices, a bias); eight rows 8.1 and 10.7, 11.7 and 11.0, 8.1 and 10.8, 37.4 and 22.2: five to
+// eight rows of many experts lose by it.  Sixteen: 12.3 and 10.8, 20.1 and 11.0, 7.9 and 10.8, 70 and 22.
+constexpr int kOneLaunchRows = 8;
 
 template <class T, int V, bool WIDE>
 void choose_as(const RouteArgs &a, const ListArgs *lists, hipStream_t s)
